@@ -1,5 +1,5 @@
-"""Compile in-tree: csrc/zvc.hip -> paper_1705_01626_amd/libzvc.so (the HIP library) and
-csrc/calls.cpp -> paper_1705_01626_amd/_calls.<interpreter's tag>.so (its entry from Python,
+"""Compile in-tree: csrc/zvc.hip -> paper_1705_01626_amd/libzvc.so (the HIP library of the codec),
+csrc/ffn.hip -> libzvc_ffn.so (that of the training operators) and csrc/calls.cpp -> paper_1705_01626_amd/_calls.<interpreter's tag>.so (their entry from Python,
 which is left out where the interpreter's headers are not installed).
 
 Usage: python -m paper_1705_01626_amd.build
@@ -17,6 +17,9 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SOURCE = os.path.join(PKG, "csrc", "zvc.hip")
 LIBRARY = os.path.join(PKG, "libzvc.so")
+FFN_SOURCE = os.path.join(PKG, "csrc", "ffn.hip")
+FFN_LIBRARY = os.path.join(PKG, "libzvc_ffn.so")
+FFN_HEADER = os.path.join(ROOT, "include", "zvc_ffn.h")
 CALLS_SOURCE = os.path.join(PKG, "csrc", "calls.cpp")
 HEADER = os.path.join(ROOT, "include", "zvc.h")
 CALLS = os.path.join(PKG, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))   # no other interpreter loads it
@@ -33,6 +36,12 @@ FLAGS = [
 
 def build(output: str = LIBRARY, extra=()) -> str:
     cmd = [HIPCC, *FLAGS, *extra, "-I", os.path.join(ROOT, "include"), "-o", output, SOURCE]
+    subprocess.run(cmd, check=True)
+    return output
+
+
+def build_ffn(output: str = FFN_LIBRARY, extra=()) -> str:
+    cmd = [HIPCC, *FLAGS, *extra, "-I", os.path.join(ROOT, "include"), "-o", output, FFN_SOURCE]
     subprocess.run(cmd, check=True)
     return output
 
@@ -58,11 +67,14 @@ def ensure_built() -> str:
     """Build only what is not built yet (or whose sources are newer)."""
     if _older(LIBRARY, SOURCE, HEADER):
         build()
-    if _older(CALLS, CALLS_SOURCE, HEADER):
+    if _older(FFN_LIBRARY, FFN_SOURCE, FFN_HEADER, HEADER):
+        build_ffn()
+    if _older(CALLS, CALLS_SOURCE, HEADER, FFN_HEADER):
         build_calls()
     return LIBRARY
 
 
 if __name__ == "__main__":
     print(build(extra=sys.argv[1:]))
+    print(build_ffn(extra=sys.argv[1:]))
     print(build_calls())

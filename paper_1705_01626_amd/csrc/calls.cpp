@@ -1,4 +1,4 @@
-// Python entry to the device calls of libzvc (include/zvc.h): the same arguments as
+// Python entry to the device calls of libzvc (include/zvc.h) and libzvc_ffn (include/zvc_ffn.h): the same arguments as
 // the C functions, as integers, and the status as the result.  A call through
 // ctypes converts its nine or ten arguments one object at a time, 3 us of a call
 // whose kernel takes 4; here they are read from the interpreter's argument array.
@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include "zvc.h"
+#include "zvc_ffn.h"
 
 #include <dlfcn.h>
 
@@ -39,7 +40,7 @@ template <auto F, typename R, typename... Params>
 PyObject* forward(R (*)(Params...), PyObject* const* args, Py_ssize_t count) {
     constexpr Py_ssize_t kParams = sizeof...(Params);
     if (g_function<F> == nullptr) {
-        PyErr_SetString(PyExc_RuntimeError, "open() has not been called");
+        PyErr_SetString(PyExc_RuntimeError, "the function's library has not been opened");
         return nullptr;
     }
     if (count != kParams) {
@@ -82,28 +83,43 @@ bool bind(void* library, const char* name) {
     DO(zvc_compress_bounded) DO(zvc_decompress) DO(zvc_window_elements) DO(zvc_window_count)    \
     DO(zvc_window_compress) DO(zvc_window_decompress) DO(zvc_offload) DO(zvc_relu_offload)      \
     DO(zvc_prefetch)
+#define ZVC_FFN_FUNCTIONS(DO) \
+    DO(zvc_dropout) DO(zvc_glu_workspace_bytes) DO(zvc_glu_forward) DO(zvc_glu_backward)
 
-// open(path): take the functions from the library at `path` (normally one that is loaded already).
-PyObject* open_library(PyObject*, PyObject* path) {
+void* library_at(PyObject* path) {
     PyObject* bytes = nullptr;
     if (!PyUnicode_FSConverter(path, &bytes)) return nullptr;
     void* library = dlopen(PyBytes_AS_STRING(bytes), RTLD_NOW | RTLD_LOCAL);
     Py_DECREF(bytes);
-    if (library == nullptr) {
-        PyErr_SetString(PyExc_ImportError, dlerror());
-        return nullptr;
-    }
+    if (library == nullptr) PyErr_SetString(PyExc_ImportError, dlerror());
+    return library;
+}
+
 #define ZVC_BIND(NAME) if (!bind<&NAME>(library, #NAME)) return nullptr;
+// open(path): take the codec's functions from the library at `path` (normally one that is loaded already).
+PyObject* open_library(PyObject*, PyObject* path) {
+    void* library = library_at(path);
+    if (library == nullptr) return nullptr;
     ZVC_FUNCTIONS(ZVC_BIND)
-#undef ZVC_BIND
     Py_RETURN_NONE;
 }
 
+// open_ffn(path): the same for the training operators.
+PyObject* open_ffn_library(PyObject*, PyObject* path) {
+    void* library = library_at(path);
+    if (library == nullptr) return nullptr;
+    ZVC_FFN_FUNCTIONS(ZVC_BIND)
+    Py_RETURN_NONE;
+}
+#undef ZVC_BIND
+
 PyMethodDef methods[] = {
     {"open", open_library, METH_O, nullptr},
+    {"open_ffn", open_ffn_library, METH_O, nullptr},
 #define ZVC_ENTRY(NAME) \
     {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<&NAME>)), METH_FASTCALL, nullptr},
     ZVC_FUNCTIONS(ZVC_ENTRY)
+    ZVC_FFN_FUNCTIONS(ZVC_ENTRY)
 #undef ZVC_ENTRY
     {nullptr, nullptr, 0, nullptr}};
 
