@@ -49,32 +49,32 @@ __device__ __forceinline__ Words philox(uint64_t index, uint64_t offset, uint64_
     return {{c0, c1, c2, c3}};
 }
 
+__device__ __forceinline__ unsigned half_of(const Words& r, int j) { return (r.w[j / 2] >> (16 * (j % 2))) & 0xFFFFu; }
+
 // Bit j: element 8 * group + j stays.  16 bits decide, but for one in 65536 elements, where 16 more do.
 __device__ __forceinline__ unsigned keep_group(const Drop& d, uint64_t offset, uint64_t group) {
     const Words r = philox(group, offset, d.seed);
     unsigned keep = 0, tie = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const unsigned half = (r.w[j / 2] >> (16 * (j % 2))) & 0xFFFFu;
-        keep |= static_cast<unsigned>(half >= d.high) << j;
-        tie |= static_cast<unsigned>(half == d.high) << j;
+        keep |= static_cast<unsigned>(half_of(r, j) >= d.high) << j;
+        tie |= static_cast<unsigned>(half_of(r, j) == d.high) << j;
     }
     if (d.low != 0 && tie != 0) {
         const Words more = philox(group | (uint64_t{1} << 63), offset, d.seed);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const unsigned half = (more.w[j / 2] >> (16 * (j % 2))) & 0xFFFFu;
-            if ((tie >> j & 1u) != 0 && half < d.low) keep &= ~(1u << j);
-        }
+        for (int j = 0; j < 8; ++j)
+            if ((tie >> j & 1u) != 0 && half_of(more, j) < d.low) keep &= ~(1u << j);
     }
     return keep;
 }
 
 // Bits for elements first .. first + 7, wherever they begin.
 __device__ __forceinline__ unsigned keep_span(const Drop& d, uint64_t offset, uint64_t first) {
-    const unsigned shift = static_cast<unsigned>(first & 7);
-    unsigned keep = keep_group(d, offset, first >> 3);
-    if (shift != 0) keep |= keep_group(d, offset, (first >> 3) + 1) << 8;
+    const unsigned shift = static_cast<unsigned>(first & 7), groups = shift != 0 ? 2 : 1;
+    unsigned keep = 0;
+#pragma unroll 1                       // (one copy of the generator: the products' code has to stay small)
+    for (unsigned i = 0; i < groups; ++i) keep |= keep_group(d, offset, (first >> 3) + i) << (8 * i);
     return (keep >> shift) & 0xFFu;
 }
 
@@ -172,112 +172,423 @@ __device__ __forceinline__ ActValue activate(int act, float g) {
     return {g * s, s + g * s * (1.f - s) * 1.5957691f * (1.f + 0.134145f * g * g)};
 }
 
-// ------------------------------------------------------------------ the block
-constexpr int kTile = 64, kStep = 16, kTileThreads = 256;
+// ------------------------------------------------------------------ products on the matrix cores
+//
+// Every product here is  out[row][col] = sum over t of Q(row, t) P(col, t),  with `col` the output's contiguous
+// index:  forward  P = Wg and Wu, Q = x;  dx  P = Wg then Wu by columns, Q = dg then du;  dW  P = x by columns,
+// Q = dg or du by columns.  P is the matrix instruction's first operand, so a lane holds four neighbouring columns
+// of one row and stores them together.
+//
+// An operand lies either along the reduction (its rows are contiguous in t) or across it (its rows are the t).
+// Both are staged as they lie, 128 bytes of reduction or as many of its rows at a time, straight from memory to LDS,
+// and read from LDS as the instruction wants them: along by 16-byte reads, across by reads that transpose (16-bit
+// types) or by element (fp32).  Units are exchanged within LDS rows so that the lanes of a read hit different banks;
+// since the hardware writes a wave's 64 x 16 bytes in lane order, it is the lanes' global addresses that carry the exchange.
+using float4v = float __attribute__((ext_vector_type(4)));
+using int4v = int __attribute__((ext_vector_type(4)));
+using short4v = short __attribute__((ext_vector_type(4)));
+using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
+using fp16x8 = _Float16 __attribute__((ext_vector_type(8)));
 
-// An operand of a product: element (index, reduction) at at[index * by_index + reduction * by_step].
-template <typename T>
-struct Operand {
-    const T* at;
-    size_t by_index, by_step;
+template <typename T> struct Fragment;
+template <> struct Fragment<bf16> { using type = bf16x8; };
+template <> struct Fragment<fp16> { using type = fp16x8; };
+template <> struct Fragment<float> { using type = float4v; };
+
+__device__ __forceinline__ float4v multiply(bf16x8 p, bf16x8 q, float4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, q, c, 0, 0, 0);
+}
+__device__ __forceinline__ float4v multiply(fp16x8 p, fp16x8 q, float4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(p, q, c, 0, 0, 0);
+}
+__device__ __forceinline__ float4v multiply(float4v p, float4v q, float4v c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(p[i], q[i], c, 0, 0, 0);
+    return c;
+}
+
+constexpr unsigned kReach = 0x80000000u;       // bytes behind a tile's base that loads may reach
+constexpr unsigned kNowhere = 0xC0000000u;     // an offset past that: such a load brings zeros
+constexpr int kRawBuffer = 0x00020000;
+constexpr int kStageBytes = 128;               // bytes of reduction per stage and row
+
+// `address` is the same in all of a wave's lanes.
+__device__ __forceinline__ int4v buffer_at(uint64_t address) {
+    return int4v{__builtin_amdgcn_readfirstlane(static_cast<int>(address)),
+                 __builtin_amdgcn_readfirstlane(static_cast<int>(address >> 32 & 0xFFFF)), static_cast<int>(kReach), kRawBuffer};
+}
+
+// 16 bytes a lane from memory to LDS, lane l's at lds + 16 l.  (No register is written: the wait is wait_loads()'s.)
+__device__ __forceinline__ void load_to_lds(int4v buffer, unsigned offset, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(buffer)
+                 : "memory");
+}
+
+using LdsByte = __attribute__((address_space(3))) unsigned char;
+__device__ __forceinline__ LdsByte* lds_at(unsigned offset) { return (LdsByte*)static_cast<uintptr_t>(offset); }
+
+template <int LEFT>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+}
+__device__ __forceinline__ void group_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+enum class Lies { kAlong, kAcross };
+
+// The workgroup's tile: WP x WQ waves of PB x QB blocks of 16 x 16.
+template <int WP_, int WQ_, int PB_, int QB_>
+struct Shape {
+    static constexpr int WP = WP_, WQ = WQ_, PB = PB_, QB = QB_;
+    static constexpr int kWavesAll = WP * WQ, kThreads = 64 * kWavesAll;
+    static constexpr int PT = WP * PB * 16, QT = WQ * QB * 16;
+    static constexpr int kStage = (PT + QT) * kStageBytes;
 };
 
-// acc[i][j] += sum over the reduction of rows (4 ty + i) x columns (4 tx + j) of a 64 x 64 tile.
-template <typename T>
-__device__ void tile_product(float (&acc)[4][4], Operand<T> rows, size_t row0, size_t m, Operand<T> cols, size_t col0,
-                             size_t n, size_t steps) {
-    __shared__ float a[kStep][kTile + 1], b[kStep][kTile + 1];
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    for (size_t s0 = 0; s0 < steps; s0 += kStep) {
-        for (int i = threadIdx.x; i < kTile * kStep; i += kTileThreads) {
-            const int t = rows.by_step == 1 ? i % kStep : i / kTile, r = rows.by_step == 1 ? i / kStep : i % kTile;
-            a[t][r] = row0 + r < m && s0 + t < steps
-                          ? static_cast<float>(rows.at[(row0 + r) * rows.by_index + (s0 + t) * rows.by_step]) : 0.f;
+// How one operand's tile of SIDE rows (kAlong) or columns (kAcross) is staged and read.  FOLD: the projections' P, in
+// which 32 rows of Wg and 32 of Wu take turns, and a 16 x 16 block takes rows {8 a + 4 j + b : a, b < 4} of the 32, j = 0 | 1, so
+// that a lane's two blocks are eight neighbouring columns.
+template <typename T, Lies LIES, int SIDE, int WAVES, bool FOLD>
+struct Operand {
+    static constexpr int W = sizeof(T);
+    static constexpr int kSteps = kStageBytes / W;                    // reduction per stage: 64 | 32
+    static constexpr int kLoads = SIDE * kStageBytes / 1024 / WAVES;  // per wave and stage
+    static constexpr int kRowBytes = LIES == Lies::kAlong ? kStageBytes : SIDE * W;
+    static constexpr int kLanesPerRow = kRowBytes / 16;
+    static constexpr int kRowsPerLoad = 1024 / kRowBytes;
+    static constexpr int kUnit = LIES == Lies::kAlong ? 16 : W == 2 ? 32 : 64;   // what is exchanged within a row
+    static constexpr int kUnitMask = kRowBytes / kUnit - 1;
+    static_assert(kLoads * WAVES * 1024 == SIDE * kStageBytes, "whole loads");
+
+    static __device__ __forceinline__ int exchange(int row) {
+        if constexpr (LIES == Lies::kAlong)
+            return FOLD ? (row & 3) | (row >> 3 & 1) << 2 : row & 7;
+        else
+            return (W == 2 ? (row & 3) | (row >> 3 & 3) << 2 : row >> 2 & 3) & kUnitMask;
+    }
+
+    unsigned offset[kLoads];            // of this lane's 16 bytes from the tile's base
+    int first, lane_row, unit16;        // this wave's first load; the lane's row within a load, its 16 bytes' place
+
+    // `left`: rows (kAlong) or columns (kAcross) of the tile that exist.  `ld` in elements.
+    __device__ __forceinline__ void init(int wave, int lane, unsigned ld, unsigned left) {
+        first = wave * kLoads;
+        lane_row = lane / kLanesPerRow;
+        unit16 = lane % kLanesPerRow;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int row = (first + i) * kRowsPerLoad + lane_row;
+            const int place = logical(row);
+            if constexpr (LIES == Lies::kAlong) {
+                const unsigned r = FOLD ? (row >> 6) * 32 + (row & 31) : row;
+                offset[i] = r < left ? r * ld * W + place : kNowhere;
+            } else {
+                offset[i] = place / W < static_cast<int>(left) ? row * ld * W + place : kNowhere;
+            }
         }
-        for (int i = threadIdx.x; i < kTile * kStep; i += kTileThreads) {
-            const int t = cols.by_step == 1 ? i % kStep : i / kTile, c = cols.by_step == 1 ? i / kStep : i % kTile;
-            b[t][c] = col0 + c < n && s0 + t < steps
-                          ? static_cast<float>(cols.at[(col0 + c) * cols.by_index + (s0 + t) * cols.by_step]) : 0.f;
+    }
+    // The byte within the row that the lane fetches for the place that it fills.
+    __device__ __forceinline__ int logical(int row) const {
+        const int place = unit16 * 16;
+        return ((place / kUnit) ^ exchange(row)) * kUnit + place % kUnit;
+    }
+    // Whether load i of a stage with `left` of the reduction brings something.
+    __device__ __forceinline__ bool within(int i, int left) const {
+        const int row = (first + i) * kRowsPerLoad + lane_row;
+        return LIES == Lies::kAlong ? logical(row) / W < left : row < left;
+    }
+    // Stage: `left` of the reduction remain at `base`.
+    __device__ __forceinline__ void fetch(uint64_t base, int64_t left, unsigned lds) const {
+        const int4v buffer = buffer_at(base);
+        if (left >= kSteps) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) load_to_lds(buffer, offset[i], lds + (first + i) * 1024);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                load_to_lds(buffer, within(i, static_cast<int>(left)) ? offset[i] : kNowhere, lds + (first + i) * 1024);
         }
-        __syncthreads();
-        for (int t = 0; t < kStep; ++t)
+    }
+};
+
+// A wave's reads of its strip of an operand from LDS: block b, half s of the stage.
+template <typename T, Lies LIES, int SIDE, int BLOCKS, bool FOLD>
+struct Reader {
+    using Frag = typename Fragment<T>::type;
+    using Op = Operand<T, LIES, SIDE, 1, FOLD>;
+    static constexpr int W = sizeof(T);
+    unsigned at[LIES == Lies::kAlong ? 2 : BLOCKS];
+
+    __device__ __forceinline__ void init(unsigned lds, int strip, int lane) {
+        const int r = lane & 15, q = lane >> 4;
+        if constexpr (LIES == Lies::kAlong) {
+            const int row = strip * BLOCKS * 16 + (FOLD ? (r >> 2) * 8 + (r & 3) : r);
+            at[0] = lds + row * kStageBytes + (q ^ Op::exchange(row)) * 16;
+            at[1] = lds + row * kStageBytes + ((q + 4) ^ Op::exchange(row)) * 16;
+        } else {
+            const int row = W == 2 ? q * 8 + (r >> 2) : q * 4;
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+                at[b] = lds + row * Op::kRowBytes + ((strip * BLOCKS + b) ^ Op::exchange(row)) * Op::kUnit + (W == 2 ? (r & 3) * 8 : r * 4);
+        }
+    }
+    __device__ __forceinline__ Frag read(int b, int s, unsigned stage) const {
+        if constexpr (LIES == Lies::kAlong) {
+            const int rows = FOLD ? (b >> 1) * 32 + (b & 1) * 4 : b * 16;
+            return *reinterpret_cast<__attribute__((address_space(3))) Frag*>(lds_at(at[s] + stage + rows * kStageBytes));
+        } else if constexpr (W == 2) {
+            LdsByte* const p = lds_at(at[b] + stage + s * 32 * Op::kRowBytes);
+            const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)p);
+            const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(p + 4 * Op::kRowBytes));
+            return __builtin_bit_cast(Frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            Frag f;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] += a[t][4 * ty + i] * b[t][4 * tx + j];
-        __syncthreads();
+                f[i] = *reinterpret_cast<__attribute__((address_space(3))) float*>(lds_at(at[b] + stage + (s * 16 + i) * Op::kRowBytes));
+            return f;
+        }
     }
-}
+};
+
+enum class Does { kForward, kSlope, kDx, kDw };
 
 template <typename T>
 struct GluArgs {
     const T *x, *wg, *wu, *dh;
     const T *gate_in, *up_in;
     T *h, *gate, *up, *dg, *du;
-    size_t ldx, ldw, lddh, ldh, ldp, ldd, m, n, k;
+    T *out, *out2;                      // dx; dwg and dwu
+    size_t ldx, ldw, lddh, ldh, ldp, ldd, ldo, m, n, k;
     int act;
     Drop d;
+    bool wide;                          // the outputs' and dh's rows take 16-byte (dx, dw: four-element) accesses
 };
 
-// Forward (dh null): h, and gate and up where wanted.  Backward (dh not null): dg and du.
-template <typename T>
-__device__ void finish_element(const GluArgs<T>& p, uint64_t offset, size_t row, size_t col, float g, float u) {
+// What becomes of eight neighbouring columns' projections, col a multiple of eight.
+template <typename T, Does DOES>
+__device__ __forceinline__ void finish8(const GluArgs<T>& p, uint64_t offset, size_t row, size_t col, const Eight& g, const Eight& u) {
     const uint64_t i = static_cast<uint64_t>(row) * p.n + col;
-    const bool keep = !p.d.active || (keep_group(p.d, offset, i >> 3) >> (i & 7) & 1u);
-    const ActValue a = activate(p.act, g);
-    if (p.dh != nullptr) {
-        const float dh = keep ? static_cast<float>(p.dh[row * p.lddh + col]) * p.d.scale : 0.f;
-        p.dg[row * p.ldd + col] = static_cast<T>(p.act == ZVC_RELU ? (g <= 0.f ? 0.f : dh * u) : dh * u * a.slope);
-        p.du[row * p.ldd + col] = static_cast<T>(dh * a.value);
-        return;
-    }
-    p.h[row * p.ldh + col] = static_cast<T>(keep ? a.value * u * p.d.scale : 0.f);
-    if (p.gate != nullptr) {
-        const bool relu = p.act == ZVC_RELU;
-        p.gate[row * p.ldp + col] = static_cast<T>(!keep ? 0.f : relu ? a.value : g);
-        p.up[row * p.ldp + col] = static_cast<T>(!keep || (relu && g <= 0.f) ? 0.f : u);
-    }
-}
-
-template <typename T>
-__global__ __launch_bounds__(kTileThreads) void glu_project_kernel(GluArgs<T> p) {
-    const size_t row0 = static_cast<size_t>(blockIdx.y) * kTile, col0 = static_cast<size_t>(blockIdx.x) * kTile;
-    float g[4][4] = {}, u[4][4] = {};
-    tile_product<T>(g, {p.x, p.ldx, 1}, row0, p.m, {p.wg, p.ldw, 1}, col0, p.n, p.k);
-    tile_product<T>(u, {p.x, p.ldx, 1}, row0, p.m, {p.wu, p.ldw, 1}, col0, p.n, p.k);
-    const uint64_t offset = effective_offset(p.d);
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const size_t row = row0 + 4 * (threadIdx.x / 16) + i, col = col0 + 4 * (threadIdx.x % 16) + j;
-            if (row < p.m && col < p.n) finish_element(p, offset, row, col, g[i][j], u[i][j]);
+    const unsigned keep = p.d.active ? keep_span(p.d, offset, i) : 0xFFu;
+    const bool relu = p.act == ZVC_RELU;
+    const int there = static_cast<int>(p.n - col < 8 ? p.n - col : 8);
+    const bool wide = p.wide && there == 8;
+    if constexpr (DOES == Does::kSlope) {
+        Eight dh, dg, du;
+        if (wide) {
+            dh = load8(p.dh + row * p.lddh + col);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) dh.v[j] = j < there ? static_cast<float>(p.dh[row * p.lddh + col + j]) : 0.f;
         }
-}
-
-// dg and du from kept projections.
-template <typename T>
-__global__ __launch_bounds__(256) void glu_slope_kernel(GluArgs<T> p) {
-    const uint64_t offset = effective_offset(p.d);
-    const uint64_t step = static_cast<uint64_t>(gridDim.x) * 256;
-    for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < static_cast<uint64_t>(p.m) * p.n; i += step) {
-        const size_t row = i / p.n, col = i - row * p.n;
-        finish_element(p, offset, row, col, static_cast<float>(p.gate_in[row * p.ldp + col]),
-                       static_cast<float>(p.up_in[row * p.ldp + col]));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const ActValue a = activate(p.act, g.v[j]);
+            const float d = (keep >> j & 1u) ? dh.v[j] * p.d.scale : 0.f;
+            dg.v[j] = relu && g.v[j] <= 0.f ? 0.f : d * u.v[j] * a.slope;
+            du.v[j] = d * a.value;
+            if (j >= there) dg.v[j] = du.v[j] = 0.f;
+        }
+        store8(p.dg + row * p.ldd + col, dg);
+        store8(p.du + row * p.ldd + col, du);
+    } else {
+        Eight h, gate, up;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const ActValue a = activate(p.act, g.v[j]);
+            const bool stays = keep >> j & 1u;
+            h.v[j] = stays ? a.value * u.v[j] * p.d.scale : 0.f;
+            gate.v[j] = !stays ? 0.f : relu ? a.value : g.v[j];
+            up.v[j] = !stays || (relu && g.v[j] <= 0.f) ? 0.f : u.v[j];
+        }
+        T* const out[] = {p.h + row * p.ldh + col, p.gate == nullptr ? nullptr : p.gate + row * p.ldp + col,
+                          p.gate == nullptr ? nullptr : p.up + row * p.ldp + col};
+        const Eight* const from[] = {&h, &gate, &up};
+#pragma unroll
+        for (int o = 0; o < 3; ++o) {
+            if (out[o] == nullptr) continue;
+            if (wide) {
+                store8(out[o], *from[o]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j < there) out[o][j] = static_cast<T>(from[o]->v[j]);
+            }
+        }
     }
 }
 
-// out (rows x cols, stride ld) = a1 b1 + a2 b2, the second where a2.at is not null.
-template <typename T>
-__global__ __launch_bounds__(kTileThreads) void product_kernel(Operand<T> a1, Operand<T> b1, Operand<T> a2, Operand<T> b2,
-                                                               T* out, size_t ld, size_t rows, size_t cols, size_t steps) {
-    const size_t row0 = static_cast<size_t>(blockIdx.y) * kTile, col0 = static_cast<size_t>(blockIdx.x) * kTile;
-    float acc[4][4] = {};
-    tile_product<T>(acc, a1, row0, rows, b1, col0, cols, steps);
-    if (a2.at != nullptr) tile_product<T>(acc, a2, row0, rows, b2, col0, cols, steps);
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const size_t row = row0 + 4 * (threadIdx.x / 16) + i, col = col0 + 4 * (threadIdx.x % 16) + j;
-            if (row < rows && col < cols) out[row * ld + col] = static_cast<T>(acc[i][j]);
+// The tile of workgroup `id` of tp x tq: workgroups go to the eight XCDs in turn, so each takes a contiguous run of the
+// order in which eight rows of tiles are walked together (what 32 workgroups of an XCD read at a time then fits its L2).
+__device__ __forceinline__ void tile_of(unsigned id, unsigned tp, unsigned tq, unsigned* p, unsigned* q) {
+    const unsigned count = tp * tq, xcd = id % 8, per = count / 8, more = count % 8;
+    const unsigned at = xcd * per + (xcd < more ? xcd : more) + id / 8;
+    const unsigned band = at / (8 * tp), in_band = at % (8 * tp);
+    const unsigned height = tq - band * 8 < 8 ? tq - band * 8 : 8;
+    *q = band * 8 + in_band % height;
+    *p = in_band / height;
+}
+
+template <typename T, Does DOES, class S>
+__global__ __launch_bounds__(S::kThreads, S::kThreads == 256 ? 2 : 1) void product_kernel(GluArgs<T> p, unsigned tp, unsigned tq) {
+    constexpr bool kFold = DOES == Does::kForward || DOES == Does::kSlope;
+    constexpr Lies kP = kFold ? Lies::kAlong : Lies::kAcross, kQ = DOES == Does::kDw ? Lies::kAcross : Lies::kAlong;
+    constexpr int W = sizeof(T), kSteps = kStageBytes / W;
+    __shared__ alignas(1024) unsigned char lds[2 * S::kStage];
+    const unsigned base = static_cast<unsigned>(reinterpret_cast<uintptr_t>((LdsByte*)lds));
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wp = wave % S::WP, wq = wave / S::WP;
+    unsigned tile_p, tile_q;
+    tile_of(blockIdx.x, tp, tq, &tile_p, &tile_q);
+
+    // The tile's place, the operands' bases and the stages of the reduction.
+    constexpr int kCols = kFold ? S::PT / 2 : S::PT;
+    const size_t col0 = static_cast<size_t>(tile_p) * kCols;
+    const unsigned halves = DOES == Does::kDw ? tq / 2 : 0;              // dW: tiles of dWg, then of dWu
+    const bool second = DOES == Does::kDw && tile_q >= halves;
+    const size_t row0 = static_cast<size_t>(second ? tile_q - halves : tile_q) * S::QT;
+    const size_t rows = DOES == Does::kDw ? p.n : p.m, cols = kFold ? p.n : p.k;
+    const size_t length = kFold ? p.k : DOES == Does::kDx ? p.n : p.m;   // dx: twice
+    const unsigned once = static_cast<unsigned>((length + kSteps - 1) / kSteps), stages = DOES == Does::kDx ? 2 * once : once;
+
+    Operand<T, kP, S::PT, S::kWavesAll, kFold> in_p;
+    Operand<T, kQ, S::QT, S::kWavesAll, false> in_q;
+    in_p.init(wave, lane, static_cast<unsigned>(kFold || DOES == Does::kDx ? p.ldw : p.ldx), static_cast<unsigned>(cols - col0 < S::PT ? cols - col0 : S::PT));
+    in_q.init(wave, lane, static_cast<unsigned>(kFold ? p.ldx : p.ldd), static_cast<unsigned>(rows - row0 < S::QT ? rows - row0 : S::QT));
+    const T* const dd = second ? p.du : p.dg;
+    const uint64_t p0 = reinterpret_cast<uint64_t>(kFold ? ((wave & 1) ? p.wu : p.wg) + col0 * p.ldw : DOES == Does::kDx ? p.wg + col0 : p.x + col0);
+    const uint64_t p1 = reinterpret_cast<uint64_t>(p.wu + col0);
+    const uint64_t q0 = reinterpret_cast<uint64_t>(kFold ? p.x + row0 * p.ldx : DOES == Does::kDx ? p.dg + row0 * p.ldd : dd + row0);
+    const uint64_t q1 = reinterpret_cast<uint64_t>(p.du + row0 * p.ldd);
+    const uint64_t step_p = kFold ? kStageBytes : kSteps * W * (DOES == Does::kDx ? p.ldw : p.ldx);
+    const uint64_t step_q = DOES == Does::kDw ? kSteps * W * p.ldd : kStageBytes;
+    static_assert(!kFold || Operand<T, kP, S::PT, S::kWavesAll, kFold>::kLoads == 4, "a wave fetches 32 rows of one weight");
+    static_assert(!kFold || S::PB == 4, "a wave's strip is 32 rows of each weight");
+
+    const auto fetch = [&](unsigned s) {
+        const unsigned lds_at = base + (s & 1) * S::kStage;
+        const bool late = DOES == Does::kDx && s >= once;
+        const unsigned t = late ? s - once : s;
+        const int64_t left = static_cast<int64_t>(length) - static_cast<int64_t>(t) * kSteps;
+        in_p.fetch((late ? p1 : p0) + t * step_p, left, lds_at);
+        // (dx: the columns of dg and du behind the last are zeros, up to a whole stage)
+        in_q.fetch((late ? q1 : q0) + t * step_q, DOES == Does::kDx ? kSteps : left, lds_at + S::PT * kStageBytes);
+    };
+
+    Reader<T, kP, S::PT, S::PB, kFold> out_p;
+    Reader<T, kQ, S::QT, S::QB, false> out_q;
+    out_p.init(base, wp, lane);
+    out_q.init(base + S::PT * kStageBytes, wq, lane);
+
+    float4v acc[S::PB][S::QB];
+#pragma unroll
+    for (int i = 0; i < S::PB; ++i)
+#pragma unroll
+        for (int j = 0; j < S::QB; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
+
+    if (stages != 0) fetch(0);
+    for (unsigned s = 0; s < stages; ++s) {
+        wait_loads<0>();
+        group_barrier();                     // stage s is there, and everyone has read stage s - 1
+        if (s + 1 < stages) fetch(s + 1);
+        const unsigned stage = (s & 1) * S::kStage;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            typename Fragment<T>::type a[S::PB], b[S::QB];
+#pragma unroll
+            for (int i = 0; i < S::PB; ++i) a[i] = out_p.read(i, half, stage);
+#pragma unroll
+            for (int j = 0; j < S::QB; ++j) b[j] = out_q.read(j, half, stage);
+#pragma unroll
+            for (int j = 0; j < S::QB; ++j)
+#pragma unroll
+                for (int i = 0; i < S::PB; ++i) acc[i][j] = multiply(a[i], b[j], acc[i][j]);
         }
+    }
+
+    const int r = lane & 15, quarter = lane >> 4;
+    if constexpr (kFold) {
+        const uint64_t offset = effective_offset(p.d);
+        const size_t end = DOES == Does::kSlope ? p.ldd : p.n;      // dg and du are written up to their rows' ends
+        // One copy of the code for all blocks: each turn takes the first ones, and the others move up.
+#pragma unroll 1
+        for (int j = 0; j < S::QB; ++j) {
+            const size_t row = row0 + (wq * S::QB + j) * 16 + r, col = col0 + wp * 32 + quarter * 8;
+            Eight g, u;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g.v[e] = acc[e / 4][0][e % 4], u.v[e] = acc[2 + e / 4][0][e % 4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int next = 1; next < S::QB; ++next) acc[i][next - 1] = acc[i][next];
+            if (row >= p.m || col >= end) continue;
+            if (col < p.n) {
+                finish8<T, DOES>(p, offset, row, col, g, u);
+            } else if constexpr (DOES == Does::kSlope) {
+                const Eight zero = {};
+                store8(p.dg + row * p.ldd + col, zero), store8(p.du + row * p.ldd + col, zero);
+            }
+        }
+    } else {
+        T* const out = second ? p.out2 : p.out;
+#pragma unroll
+        for (int j = 0; j < S::QB; ++j) {
+            const size_t row = row0 + (wq * S::QB + j) * 16 + r;
+            if (row >= rows) continue;
+#pragma unroll
+            for (int i = 0; i < S::PB; ++i) {
+                const size_t col = col0 + (wp * S::PB + i) * 16 + quarter * 4;
+                T* const at = out + row * p.ldo + col;
+                if (p.wide && col + 4 <= cols) {
+                    struct alignas(4 * W) { T v[4]; } four;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) four.v[e] = static_cast<T>(acc[i][j][e]);
+                    __builtin_memcpy(__builtin_assume_aligned(at, 4 * W), &four, sizeof four);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (col + e < cols) at[e] = static_cast<T>(acc[i][j][e]);
+                }
+            }
+        }
+    }
+}
+
+// dg and du from kept projections; their rows are filled with zeros up to ldd.
+template <typename T>
+__global__ __launch_bounds__(256) void slope_kernel(GluArgs<T> p) {
+    const uint64_t offset = effective_offset(p.d);
+    const uint64_t groups = p.ldd / 8, total = groups * p.m, step = static_cast<uint64_t>(gridDim.x) * 256;
+    for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += step) {
+        const size_t row = i / groups, col = (i - row * groups) * 8;
+        Eight g = {}, u = {};
+        if (col >= p.n) {
+            store8(p.dg + row * p.ldd + col, g), store8(p.du + row * p.ldd + col, u);
+            continue;
+        }
+        const T *gate = p.gate_in + row * p.ldp + col, *up = p.up_in + row * p.ldp + col;
+        if (p.wide && col + 8 <= p.n) {
+            g = load8(gate), u = load8(up);
+        } else {
+            for (int j = 0; j < 8 && col + j < p.n; ++j) g.v[j] = static_cast<float>(gate[j]), u.v[j] = static_cast<float>(up[j]);
+        }
+        finish8<T, Does::kSlope>(p, offset, row, col, g, u);
+    }
+}
+
+// A copy of a rows x cols matrix whose rows are filled with zeros up to a multiple of 16 bytes.
+template <typename T>
+__global__ __launch_bounds__(256) void align_kernel(const T* from, size_t ld, T* to, size_t ld_to, size_t rows, size_t cols) {
+    constexpr int kPer = 16 / sizeof(T);
+    const uint64_t groups = ld_to / kPer, total = groups * rows, step = static_cast<uint64_t>(gridDim.x) * 256;
+    for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += step) {
+        const size_t row = i / groups, col = (i - row * groups) * kPer;
+        Pack<T> p;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) p.v[j] = col + j < cols ? from[row * ld + col + j] : static_cast<T>(0.f);
+        *reinterpret_cast<Pack<T>*>(to + row * ld_to + col) = p;
+    }
 }
 
 // ------------------------------------------------------------------ host side
@@ -331,15 +642,28 @@ zvc_status dropout_as(const void* x, size_t ldx, const void* residual, size_t ld
                   static_cast<const T*>(x), ldx, static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy, cols, total, d);
 }
 
+constexpr size_t kColumnsUp = 64;               // dg's and du's rows are filled up to a multiple of this
+
 // Where the parts of a workspace begin.
 struct Layout {
-    size_t dg, du, bytes;
+    size_t dg, du, x, wg, wu, bytes;
+    size_t ldd, aligned_k;              // row strides of dg and du, and of the copies of x, Wg and Wu
 };
 
-Layout layout_of(size_t m, size_t n, size_t k, size_t w, bool backward) {
-    (void)k;
-    const size_t part = backward ? round_up(m * n * w, 256) : 0;
-    return {0, part, 2 * part};
+// `copies`: x, Wg and Wu do not all take 16-byte accesses.
+Layout layout_of(size_t m, size_t n, size_t k, size_t w, bool backward, bool copies) {
+    Layout at{};
+    at.ldd = round_up(n, kColumnsUp);
+    at.aligned_k = round_up(k, 16 / w);
+    const auto part = [&](size_t bytes) {
+        const size_t begin = at.bytes;
+        at.bytes += round_up(bytes, 256);
+        return begin;
+    };
+    if (backward) at.dg = part(m * at.ldd * w), at.du = part(m * at.ldd * w);
+    if (copies) at.x = part(m * at.aligned_k * w), at.wg = part(n * at.aligned_k * w), at.wu = part(n * at.aligned_k * w);
+    at.bytes += 256;
+    return at;
 }
 
 bool sizes_ok(size_t m, size_t n, size_t k) {
@@ -348,37 +672,85 @@ bool sizes_ok(size_t m, size_t n, size_t k) {
 
 bool stride_ok(size_t ld, size_t cols) { return ld >= cols && ld <= ZVC_FFN_MAX_COLUMNS; }
 
+using Large = Shape<4, 2, 4, 8>;                // 256 x 256, eight waves
+using Small = Shape<2, 2, 4, 4>;                // 128 x 128, four waves
+
+template <typename T, Does DOES, class S>
+zvc_status product_of(const GluArgs<T>& p, hipStream_t stream) {
+    constexpr bool kFold = DOES == Does::kForward || DOES == Does::kSlope;
+    const size_t cols = kFold ? div_up(p.n, S::PT / 2) : div_up(p.k, S::PT);
+    const size_t rows = DOES == Does::kDw ? 2 * div_up(p.n, S::QT) : div_up(p.m, S::QT);
+    if (cols * rows > 0x7FFFFFFF) return ZVC_E_ARG;
+    return launch(product_kernel<T, DOES, S>, dim3(cols * rows), S::kThreads, stream, p, static_cast<unsigned>(cols),
+                  static_cast<unsigned>(rows));
+}
+
+template <typename T, Does DOES>
+zvc_status product(const GluArgs<T>& p, hipStream_t stream) {
+    constexpr bool kFold = DOES == Does::kForward || DOES == Does::kSlope;
+    const size_t tiles = (kFold ? div_up(p.n, Large::PT / 2) : div_up(p.k, Large::PT)) *
+                         (DOES == Does::kDw ? 2 * div_up(p.n, Large::QT) : div_up(p.m, Large::QT));
+    return tiles >= 192 ? product_of<T, DOES, Large>(p, stream) : product_of<T, DOES, Small>(p, stream);
+}
+
+// Copies of x and the weights where they do not take 16-byte accesses as they lie.
 template <typename T>
-zvc_status product(Operand<T> a1, Operand<T> b1, Operand<T> a2, Operand<T> b2, void* out, size_t ld, size_t rows,
-                   size_t cols, size_t steps, hipStream_t stream) {
-    return launch(product_kernel<T>, dim3(div_up(cols, kTile), div_up(rows, kTile)), kTileThreads, stream, a1, b1, a2, b2,
-                  static_cast<T*>(out), ld, rows, cols, steps);
+zvc_status align_inputs(GluArgs<T>* p, const Layout& at, unsigned char* base, hipStream_t stream) {
+    const auto copy = [&](const T** from, size_t* ld, size_t rows, size_t to) {
+        if (rows == 0 || p->k == 0) return ZVC_OK;
+        T* const out = reinterpret_cast<T*>(base + to);
+        const size_t blocks = div_up(rows * at.aligned_k * sizeof(T) / 16, 256);
+        const zvc_status st = launch(align_kernel<T>, dim3(blocks < 65536 ? blocks : 65536), 256, stream, *from, *ld, out,
+                                     at.aligned_k, rows, p->k);
+        *from = out;
+        *ld = at.aligned_k;
+        return st;
+    };
+    const bool odd = p->k * sizeof(T) % 16 != 0;
+    if (odd || !aligned_to(p->x, 16) || p->ldx * sizeof(T) % 16 != 0)
+        if (zvc_status st = copy(&p->x, &p->ldx, p->m, at.x)) return st;
+    if (odd || !aligned_to(p->wg, 16) || !aligned_to(p->wu, 16) || p->ldw * sizeof(T) % 16 != 0) {
+        size_t ld = p->ldw;
+        if (zvc_status st = copy(&p->wg, &ld, p->n, at.wg)) return st;
+        return copy(&p->wu, &p->ldw, p->n, at.wu);
+    }
+    return ZVC_OK;
+}
+
+// Whether rows at this address and stride take accesses of `bytes`.
+template <typename T>
+bool takes(const T* at, size_t ld, size_t bytes) { return aligned_to(at, bytes) && ld * sizeof(T) % bytes == 0; }
+
+template <typename T>
+zvc_status forward_as(GluArgs<T> p, const Layout& at, unsigned char* base, hipStream_t stream) {
+    if (zvc_status st = align_inputs(&p, at, base, stream)) return st;
+    p.wide = takes(p.h, p.ldh, 16) && (p.gate == nullptr || (takes(p.gate, p.ldp, 16) && takes(p.up, p.ldp, 16)));
+    return product<T, Does::kForward>(p, stream);
 }
 
 template <typename T>
-zvc_status project(const GluArgs<T>& p, hipStream_t stream) {
-    return launch(glu_project_kernel<T>, dim3(div_up(p.n, kTile), div_up(p.m, kTile)), kTileThreads, stream, p);
-}
-
-template <typename T>
-zvc_status backward_as(GluArgs<T> p, void* dx, size_t lddx, void* dwg, void* dwu, size_t lddw, hipStream_t stream) {
+zvc_status backward_as(GluArgs<T> p, T* dx, size_t lddx, T* dwg, T* dwu, size_t lddw, const Layout& at, unsigned char* base,
+                       hipStream_t stream) {
+    if (zvc_status st = align_inputs(&p, at, base, stream)) return st;
     if (p.m != 0 && p.n != 0) {
         zvc_status st;
+        p.wide = takes(p.dh, p.lddh, 16);
         if (p.gate_in == nullptr) {
-            st = project(p, stream);
+            st = product<T, Does::kSlope>(p, stream);
         } else {
-            const size_t blocks = div_up(p.m * p.n, 256);
-            st = launch(glu_slope_kernel<T>, dim3(blocks < 65536 ? blocks : 65536), 256, stream, p);
+            p.wide = p.wide && takes(p.gate_in, p.ldp, 16) && takes(p.up_in, p.ldp, 16);
+            const size_t blocks = div_up(p.m * (p.ldd / 8), 256);
+            st = launch(slope_kernel<T>, dim3(blocks < 65536 ? blocks : 65536), 256, stream, p);
         }
         if (st != ZVC_OK) return st;
     }
-    const Operand<T> none = {nullptr, 0, 0};
-    if (dx != nullptr && p.m != 0 && p.k != 0)
-        if (zvc_status st = product<T>({p.dg, p.ldd, 1}, {p.wg, 1, p.ldw}, {p.du, p.ldd, 1}, {p.wu, 1, p.ldw}, dx, lddx, p.m,
-                                       p.k, p.n, stream)) return st;
-    if (dwg == nullptr || p.n == 0 || p.k == 0) return ZVC_OK;
-    if (zvc_status st = product<T>({p.dg, 1, p.ldd}, {p.x, 1, p.ldx}, none, none, dwg, lddw, p.n, p.k, p.m, stream)) return st;
-    return product<T>({p.du, 1, p.ldd}, {p.x, 1, p.ldx}, none, none, dwu, lddw, p.n, p.k, p.m, stream);
+    if (dx != nullptr && p.m != 0) {
+        p.out = dx, p.ldo = lddx, p.wide = takes(dx, lddx, 4 * sizeof(T));
+        if (zvc_status st = product<T, Does::kDx>(p, stream)) return st;
+    }
+    if (dwg == nullptr || p.n == 0) return ZVC_OK;
+    p.out = dwg, p.out2 = dwu, p.ldo = lddw, p.wide = takes(dwg, lddw, 4 * sizeof(T)) && takes(dwu, lddw, 4 * sizeof(T));
+    return product<T, Does::kDw>(p, stream);
 }
 
 }  // namespace
@@ -417,8 +789,7 @@ zvc_status zvc_dropout(const void* d_x, size_t ldx, const void* d_residual, size
 
 size_t zvc_glu_workspace_bytes(size_t m, size_t n, size_t k, int type, int backward, int loose) {
     const size_t w = type_bytes(type);
-    (void)loose;
-    return w == 0 || !sizes_ok(m, n, k) ? 0 : layout_of(m, n, k, w, backward != 0).bytes + 256;
+    return w == 0 || !sizes_ok(m, n, k) ? 0 : layout_of(m, n, k, w, backward != 0, loose != 0 || k * w % 16 != 0).bytes;
 }
 
 zvc_status zvc_glu_forward(const void* d_x, size_t ldx, const void* d_wg, const void* d_wu, size_t ldw, void* d_h,
@@ -448,11 +819,14 @@ zvc_status zvc_glu_forward(const void* d_x, size_t ldx, const void* d_wg, const 
         for (int j = 0; j < i; ++j)
             if (overlap(out[i], out[j])) return ZVC_E_ARG;
     }
+    const Layout at = layout_of(m, n, k, w, false, loose || k * w % 16 != 0);
     const auto as = [&](auto zero) {
         using T = decltype(zero);
-        return project(GluArgs<T>{static_cast<const T*>(d_x), static_cast<const T*>(d_wg), static_cast<const T*>(d_wu), nullptr,
-                                  nullptr, nullptr, static_cast<T*>(d_h), static_cast<T*>(d_gate), static_cast<T*>(d_up), nullptr,
-                                  nullptr, ldx, ldw, 0, ldh, ldp, 0, m, n, k, activation, d}, stream);
+        GluArgs<T> p{};
+        p.x = static_cast<const T*>(d_x), p.wg = static_cast<const T*>(d_wg), p.wu = static_cast<const T*>(d_wu);
+        p.h = static_cast<T*>(d_h), p.gate = static_cast<T*>(d_gate), p.up = static_cast<T*>(d_up);
+        p.ldx = ldx, p.ldw = ldw, p.ldh = ldh, p.ldp = ldp, p.m = m, p.n = n, p.k = k, p.act = activation, p.d = d;
+        return forward_as(p, at, static_cast<unsigned char*>(d_ws), stream);
     };
     return type == ZVC_FP32 ? as(0.f) : type == ZVC_FP16 ? as(fp16{}) : as(bf16{});
 }
@@ -488,15 +862,16 @@ zvc_status zvc_glu_backward(const void* d_dh, size_t lddh, const void* d_x, size
         for (int j = 0; j < i; ++j)
             if (overlap(out[i], out[j])) return ZVC_E_ARG;
     }
-    const Layout at = layout_of(m, n, k, w, true);
+    const Layout at = layout_of(m, n, k, w, true, loose || k * w % 16 != 0);
     const auto as = [&](auto zero) {
         using T = decltype(zero);
-        unsigned char* base = static_cast<unsigned char*>(d_ws);
-        GluArgs<T> p{static_cast<const T*>(d_x), static_cast<const T*>(d_wg), static_cast<const T*>(d_wu),
-                     static_cast<const T*>(d_dh), static_cast<const T*>(d_gate), static_cast<const T*>(d_up), nullptr, nullptr,
-                     nullptr, reinterpret_cast<T*>(base + at.dg), reinterpret_cast<T*>(base + at.du), ldx, ldw, lddh, 0, ldp, n,
-                     m, n, k, activation, d};
-        return backward_as(p, d_dx, lddx, d_dwg, d_dwu, lddw, stream);
+        unsigned char* const base = static_cast<unsigned char*>(d_ws);
+        GluArgs<T> p{};
+        p.x = static_cast<const T*>(d_x), p.wg = static_cast<const T*>(d_wg), p.wu = static_cast<const T*>(d_wu);
+        p.dh = static_cast<const T*>(d_dh), p.gate_in = static_cast<const T*>(d_gate), p.up_in = static_cast<const T*>(d_up);
+        p.dg = reinterpret_cast<T*>(base + at.dg), p.du = reinterpret_cast<T*>(base + at.du);
+        p.ldx = ldx, p.ldw = ldw, p.lddh = lddh, p.ldp = ldp, p.ldd = at.ldd, p.m = m, p.n = n, p.k = k, p.act = activation, p.d = d;
+        return backward_as(p, static_cast<T*>(d_dx), lddx, static_cast<T*>(d_dwg), static_cast<T*>(d_dwu), lddw, at, base, stream);
     };
     return type == ZVC_FP32 ? as(0.f) : type == ZVC_FP16 ? as(fp16{}) : as(bf16{});
 }
