@@ -318,6 +318,7 @@ struct Reader {
     using Frag = typename Fragment<T>::type;
     using Op = Operand<T, LIES, SIDE, 1, FOLD>;
     static constexpr int W = sizeof(T);
+    static constexpr int kReads = BLOCKS * (LIES == Lies::kAlong ? 1 : W);       // LDS instructions per half
     unsigned at[LIES == Lies::kAlong ? 2 : BLOCKS];
 
     __device__ __forceinline__ void init(unsigned lds, int strip, int lane) {
@@ -351,6 +352,18 @@ struct Reader {
         }
     }
 };
+
+// Asks the compiler to put the LDS reads of a block of straight code between its matrix instructions, evenly.
+template <int READS, int PRODUCTS>
+__device__ __forceinline__ void interleave() {
+    constexpr int kEach = PRODUCTS / READS > 0 ? PRODUCTS / READS : 1;
+#pragma unroll
+    for (int i = 0; i < READS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);       // one LDS read
+        __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);   // matrix instructions
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS, 0);
+}
 
 enum class Does { kForward, kSlope, kDx, kDw };
 
@@ -487,24 +500,43 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 ? 2 : 1) void produ
 #pragma unroll
         for (int j = 0; j < S::QB; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
 
-    if (stages != 0) fetch(0);
-    for (unsigned s = 0; s < stages; ++s) {
+    // A stage is multiplied in two halves.  While a half's products run, the next half is read from LDS; between
+    // the halves everyone has read the stage, and its buffer takes the stage after the next.
+    using Frag = typename Fragment<T>::type;
+    Frag a[2][S::PB], b[2][S::QB];
+    const auto read = [&](auto half, unsigned stage) {
+        constexpr int kHalf = decltype(half)::value;
+#pragma unroll
+        for (int i = 0; i < S::PB; ++i) a[kHalf][i] = out_p.read(i, kHalf, stage);
+#pragma unroll
+        for (int j = 0; j < S::QB; ++j) b[kHalf][j] = out_q.read(j, kHalf, stage);
+    };
+    const auto product = [&](auto half) {
+        constexpr int kHalf = decltype(half)::value;
+#pragma unroll
+        for (int j = 0; j < S::QB; ++j)
+#pragma unroll
+            for (int i = 0; i < S::PB; ++i) acc[i][j] = multiply(a[kHalf][i], b[kHalf][j], acc[i][j]);
+        interleave<Reader<T, kP, S::PT, S::PB, kFold>::kReads + Reader<T, kQ, S::QT, S::QB, false>::kReads,
+                   S::PB * S::QB * (W == 4 ? 4 : 1)>();
+    };
+    constexpr std::integral_constant<int, 0> kFirst{};
+    constexpr std::integral_constant<int, 1> kSecond{};
+    if (stages != 0) {
+        fetch(0);
         wait_loads<0>();
-        group_barrier();                     // stage s is there, and everyone has read stage s - 1
-        if (s + 1 < stages) fetch(s + 1);
-        const unsigned stage = (s & 1) * S::kStage;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            typename Fragment<T>::type a[S::PB], b[S::QB];
-#pragma unroll
-            for (int i = 0; i < S::PB; ++i) a[i] = out_p.read(i, half, stage);
-#pragma unroll
-            for (int j = 0; j < S::QB; ++j) b[j] = out_q.read(j, half, stage);
-#pragma unroll
-            for (int j = 0; j < S::QB; ++j)
-#pragma unroll
-                for (int i = 0; i < S::PB; ++i) acc[i][j] = multiply(a[i], b[j], acc[i][j]);
-        }
+        group_barrier();
+        if (stages > 1) fetch(1);
+        read(kFirst, 0);
+    }
+    for (unsigned s = 0; s < stages; ++s) {
+        read(kSecond, (s & 1) * S::kStage);
+        product(kFirst);
+        wait_loads<0>();
+        group_barrier();                     // stage s + 1 is there, and everyone has read stage s
+        if (s + 2 < stages) fetch(s + 2);
+        read(kFirst, (~s & 1) * S::kStage);  // (behind the last stage: what the buffer held, for nothing)
+        product(kSecond);
     }
 
     const int r = lane & 15, quarter = lane >> 4;
