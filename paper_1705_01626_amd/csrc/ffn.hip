@@ -154,22 +154,46 @@ struct ActValue {
     float value, slope;
 };
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + __expf(-x)); }
+// 1 / (1 + exp(-x)), to a few units in the last place of 32 bits.
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
 
 // act(g) and its derivative.  relu: a NaN is not <= 0 and stays.
-__device__ __forceinline__ ActValue activate(int act, float g) {
-    if (act == ZVC_RELU) return {g <= 0.f ? 0.f : g, g <= 0.f ? 0.f : 1.f};
-    if (act == ZVC_SILU) {
-        const float s = sigmoid(g);
-        return {g * s, s + g * s * (1.f - s)};
+template <int ACT, typename T>
+__device__ __forceinline__ ActValue activate(float g) {
+    if constexpr (ACT == ZVC_RELU) {
+        return {g <= 0.f ? 0.f : g, g <= 0.f ? 0.f : 1.f};
+    } else if constexpr (ACT == ZVC_SILU) {
+        const float s = sigmoid(g), a = g * s;
+        return {a, s + a * (1.f - s)};
+    } else if constexpr (ACT == ZVC_GELU) {
+        const float density = __expf(-0.5f * g * g);
+        float cdf;
+        if constexpr (sizeof(T) == 4) {
+            cdf = 0.5f * erfcf(-0.70710678f * g);
+        } else {
+            // erfc by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26: within 1.5e-7, where a 16-bit
+            // result is rounded by 2^-9 or 2^-12 of itself (a fifth of erfcf's instructions, 64 times per lane and tile)
+            const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * 0.70710678f * fabsf(g));
+            const float tail = 0.5f * density * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+            cdf = g <= 0.f ? tail : 1.f - tail;
+        }
+        return {g * cdf, cdf + g * 0.39894228f * density};
+    } else {
+        // (1 + tanh(z)) / 2 = sigmoid(2 z)
+        const float s = sigmoid(1.5957691f * (g + 0.044715f * g * g * g)), a = g * s;
+        return {a, s + a * (1.f - s) * 1.5957691f * (1.f + 0.134145f * g * g)};
     }
-    if (act == ZVC_GELU) {
-        const float cdf = 0.5f * erfcf(-0.70710678f * g);
-        return {g * cdf, cdf + g * 0.39894228f * __expf(-0.5f * g * g)};
+}
+
+// f(constant) for the activation.
+template <typename F>
+__device__ __forceinline__ void with_activation(int act, F f) {
+    switch (act) {
+        case ZVC_RELU: f(std::integral_constant<int, ZVC_RELU>{}); break;
+        case ZVC_SILU: f(std::integral_constant<int, ZVC_SILU>{}); break;
+        case ZVC_GELU: f(std::integral_constant<int, ZVC_GELU>{}); break;
+        default: f(std::integral_constant<int, ZVC_GELU_TANH>{});
     }
-    // (1 + tanh(z)) / 2 = sigmoid(2 z)
-    const float s = sigmoid(1.5957691f * (g + 0.044715f * g * g * g));
-    return {g * s, s + g * s * (1.f - s) * 1.5957691f * (1.f + 0.134145f * g * g)};
 }
 
 // ------------------------------------------------------------------ products on the matrix cores
@@ -244,6 +268,7 @@ struct Shape {
     static constexpr int kWavesAll = WP * WQ, kThreads = 64 * kWavesAll;
     static constexpr int PT = WP * PB * 16, QT = WQ * QB * 16;
     static constexpr int kStage = (PT + QT) * kStageBytes;
+    static constexpr int kPerUnit = 4 * kStage > 160 << 10 ? 1 : 2;     // workgroups that a compute unit's LDS holds
 };
 
 // How one operand's tile of SIDE rows (kAlong) or columns (kAcross) is staged and read.  FOLD: the projections' P, in
@@ -298,16 +323,19 @@ struct Operand {
         const int row = (first + i) * kRowsPerLoad + lane_row;
         return LIES == Lies::kAlong ? logical(row) / W < left : row < left;
     }
-    // Stage: `left` of the reduction remain at `base`.
-    __device__ __forceinline__ void fetch(uint64_t base, int64_t left, unsigned lds) const {
-        const int4v buffer = buffer_at(base);
+    // Stage: `left` of the reduction remain at `base` (FOLD: at `base` for Wg's rows, at `other` for Wu's).
+    __device__ __forceinline__ void fetch(uint64_t base, uint64_t other, int64_t left, unsigned lds) const {
+        constexpr int kRun = 32 / kRowsPerLoad;             // loads that bring 32 rows
+        const bool odd = FOLD && kLoads == kRun && (first / kRun & 1);
+        const int4v buffers[] = {buffer_at(odd ? other : base), buffer_at(other)};
+        const auto from = [&](int i) { return buffers[FOLD && kRun > 0 && i >= kRun]; };
         if (left >= kSteps) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) load_to_lds(buffer, offset[i], lds + (first + i) * 1024);
+            for (int i = 0; i < kLoads; ++i) load_to_lds(from(i), offset[i], lds + (first + i) * 1024);
         } else {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
-                load_to_lds(buffer, within(i, static_cast<int>(left)) ? offset[i] : kNowhere, lds + (first + i) * 1024);
+                load_to_lds(from(i), within(i, static_cast<int>(left)) ? offset[i] : kNowhere, lds + (first + i) * 1024);
         }
     }
 };
@@ -375,135 +403,193 @@ struct GluArgs {
     T *out, *out2;                      // dx; dwg and dwu
     size_t ldx, ldw, lddh, ldh, ldp, ldd, ldo, m, n, k;
     int act;
+    float* sums;                        // parts > 1: each part's sums, to be joined
+    size_t lds;                         // their row stride
+    unsigned parts;                     // of the reduction
     Drop d;
     bool wide;                          // the outputs' and dh's rows take 16-byte (dx, dw: four-element) accesses
 };
 
-// What becomes of eight neighbouring columns' projections, col a multiple of eight.
+// Eight neighbouring columns' projections g and u, col a multiple of eight: dg and du in their place ...
+template <int ACT, typename T>
+__device__ __forceinline__ void slope8(const GluArgs<T>& p, unsigned keep, const Eight& dh, Eight& g, Eight& u) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const ActValue a = activate<ACT, T>(g.v[j]);
+        const float d = (keep >> j & 1u) ? dh.v[j] * p.d.scale : 0.f;
+        g.v[j] = ACT == ZVC_RELU ? (g.v[j] <= 0.f ? 0.f : d * u.v[j]) : d * u.v[j] * a.slope;
+        u.v[j] = d * a.value;
+    }
+}
+// ... or h, and what is kept of them in their place.
+template <int ACT, typename T>
+__device__ __forceinline__ void forward8(const GluArgs<T>& p, unsigned keep, Eight& h, Eight& g, Eight& u) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float a = activate<ACT, T>(g.v[j]).value;
+        const bool stays = keep >> j & 1u;
+        h.v[j] = stays ? a * u.v[j] * p.d.scale : 0.f;
+        if (!stays || (ACT == ZVC_RELU && g.v[j] <= 0.f)) g.v[j] = u.v[j] = 0.f;
+    }
+}
+
+// The first `there` of eight elements, wherever they lie; `wide`: a multiple of 16 bytes.
+template <typename T>
+__device__ __forceinline__ Eight load_some(const T* at, int there, bool wide) {
+    Eight e = {};
+    if (wide && there >= 8) return load8(at);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < there) e.v[j] = static_cast<float>(at[j]);
+    return e;
+}
+template <typename T>
+__device__ __forceinline__ void store_some(T* at, const Eight& e, int there, bool wide) {
+    if (wide && there >= 8) return store8(at, e);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < there) at[j] = static_cast<T>(e.v[j]);
+}
+
+// What becomes of them in their row: `there` of them (none: dg's and du's filling) are columns.  dh: for the slope.
 template <typename T, Does DOES>
-__device__ __forceinline__ void finish8(const GluArgs<T>& p, uint64_t offset, size_t row, size_t col, const Eight& g, const Eight& u) {
-    const uint64_t i = static_cast<uint64_t>(row) * p.n + col;
-    const unsigned keep = p.d.active ? keep_span(p.d, offset, i) : 0xFFu;
-    const bool relu = p.act == ZVC_RELU;
-    const int there = static_cast<int>(p.n - col < 8 ? p.n - col : 8);
-    const bool wide = p.wide && there == 8;
+__device__ __forceinline__ void finish8(const GluArgs<T>& p, unsigned keep, size_t row, size_t col, int there, const Eight& dh, Eight& g, Eight& u) {
     if constexpr (DOES == Does::kSlope) {
-        Eight dh, dg, du;
-        if (wide) {
-            dh = load8(p.dh + row * p.lddh + col);
-        } else {
+        with_activation(p.act, [&](auto act) { slope8<decltype(act)::value>(p, keep, dh, g, u); });
 #pragma unroll
-            for (int j = 0; j < 8; ++j) dh.v[j] = j < there ? static_cast<float>(p.dh[row * p.lddh + col + j]) : 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const ActValue a = activate(p.act, g.v[j]);
-            const float d = (keep >> j & 1u) ? dh.v[j] * p.d.scale : 0.f;
-            dg.v[j] = relu && g.v[j] <= 0.f ? 0.f : d * u.v[j] * a.slope;
-            du.v[j] = d * a.value;
-            if (j >= there) dg.v[j] = du.v[j] = 0.f;
-        }
-        store8(p.dg + row * p.ldd + col, dg);
-        store8(p.du + row * p.ldd + col, du);
+        for (int j = 0; j < 8; ++j)
+            if (j >= there) g.v[j] = u.v[j] = 0.f;
+        store8(p.dg + row * p.ldd + col, g);
+        store8(p.du + row * p.ldd + col, u);
     } else {
-        Eight h, gate, up;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const ActValue a = activate(p.act, g.v[j]);
-            const bool stays = keep >> j & 1u;
-            h.v[j] = stays ? a.value * u.v[j] * p.d.scale : 0.f;
-            gate.v[j] = !stays ? 0.f : relu ? a.value : g.v[j];
-            up.v[j] = !stays || (relu && g.v[j] <= 0.f) ? 0.f : u.v[j];
-        }
-        T* const out[] = {p.h + row * p.ldh + col, p.gate == nullptr ? nullptr : p.gate + row * p.ldp + col,
-                          p.gate == nullptr ? nullptr : p.up + row * p.ldp + col};
-        const Eight* const from[] = {&h, &gate, &up};
-#pragma unroll
-        for (int o = 0; o < 3; ++o) {
-            if (out[o] == nullptr) continue;
-            if (wide) {
-                store8(out[o], *from[o]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j < there) out[o][j] = static_cast<T>(from[o]->v[j]);
-            }
+        Eight h;
+        with_activation(p.act, [&](auto act) { forward8<decltype(act)::value>(p, keep, h, g, u); });
+        store_some(p.h + row * p.ldh + col, h, there, p.wide);
+        if (p.gate != nullptr) {
+            store_some(p.gate + row * p.ldp + col, g, there, p.wide);
+            store_some(p.up + row * p.ldp + col, u, there, p.wide);
         }
     }
 }
 
-// The tile of workgroup `id` of tp x tq: workgroups go to the eight XCDs in turn, so each takes a contiguous run of the
-// order in which eight rows of tiles are walked together (what 32 workgroups of an XCD read at a time then fits its L2).
-__device__ __forceinline__ void tile_of(unsigned id, unsigned tp, unsigned tq, unsigned* p, unsigned* q) {
-    const unsigned count = tp * tq, xcd = id % 8, per = count / 8, more = count % 8;
-    const unsigned at = xcd * per + (xcd < more ? xcd : more) + id / 8;
-    const unsigned band = at / (8 * tp), in_band = at % (8 * tp);
-    const unsigned height = tq - band * 8 < 8 ? tq - band * 8 : 8;
-    *q = band * 8 + in_band % height;
-    *p = in_band / height;
+// How many of eight columns from `col` on there are.
+__device__ __forceinline__ int columns_left(size_t n, size_t col) { return col + 8 <= n ? 8 : col < n ? static_cast<int>(n - col) : 0; }
+
+// What becomes of a lane's strip of a tile, eight columns of QB rows 16 apart: straight code, row after row (the fences keep the
+// compiler from working on all rows at once, out of registers).
+template <typename T, Does DOES, class S>
+__device__ __forceinline__ void finish_tile(const GluArgs<T>& p, size_t row, size_t col, float4v (&acc)[S::PB][S::QB]) {
+    static_assert(S::QB <= 8, "a bit for each of a lane's elements");
+    if (col >= (DOES == Does::kSlope ? p.ldd : p.n)) return;     // (dg and du are written up to their rows' ends)
+    const int there = columns_left(p.n, col);
+    uint64_t keep = ~uint64_t{0};
+    if (p.d.active) {
+        const uint64_t offset = effective_offset(p.d);
+        keep = 0;
+#pragma unroll 1
+        for (int j = 0; j < S::QB; ++j)
+            keep |= static_cast<uint64_t>(keep_span(p.d, offset, static_cast<uint64_t>(row + j * 16) * p.n + col)) << (8 * j);
+    }
+    const auto load = [&](int j) {
+        return DOES == Does::kSlope && j < S::QB && row + j * 16 < p.m ? load_some(p.dh + (row + j * 16) * p.lddh + col, there, p.wide) : Eight{};
+    };
+    Eight dh = load(0);
+#pragma unroll
+    for (int j = 0; j < S::QB; ++j) {
+        const Eight next = load(j + 1);
+        if (row + j * 16 < p.m) {
+            Eight g, u;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g.v[e] = acc[e / 4][j][e % 4], u.v[e] = acc[2 + e / 4][j][e % 4];
+            finish8<T, DOES>(p, static_cast<unsigned>(keep >> (8 * j)), row + j * 16, col, there, dh, g, u);
+        }
+        dh = next;
+        __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
+// The place of work item `id` of `count` in the order that they are walked in: workgroups go to the eight XCDs in turn, so
+// that each XCD takes a contiguous run of it.
+__device__ __forceinline__ unsigned place_of(unsigned id, unsigned count) {
+    const unsigned xcd = id % 8, per = count / 8, more = count % 8;
+    return xcd * per + (xcd < more ? xcd : more) + id / 8;
+}
+
+// One workgroup's view of a tile: where its operands and its part of the reduction lie.
 template <typename T, Does DOES, class S>
-__global__ __launch_bounds__(S::kThreads, S::kThreads == 256 ? 2 : 1) void product_kernel(GluArgs<T> p, unsigned tp, unsigned tq) {
-    constexpr bool kFold = DOES == Does::kForward || DOES == Does::kSlope;
-    constexpr Lies kP = kFold ? Lies::kAlong : Lies::kAcross, kQ = DOES == Does::kDw ? Lies::kAcross : Lies::kAlong;
-    constexpr int W = sizeof(T), kSteps = kStageBytes / W;
+struct Tile {
+    static constexpr bool kFold = DOES == Does::kForward || DOES == Does::kSlope;
+    static constexpr Lies kP = kFold ? Lies::kAlong : Lies::kAcross, kQ = DOES == Does::kDw ? Lies::kAcross : Lies::kAlong;
+    static constexpr int W = sizeof(T), kSteps = kStageBytes / W;
+    static constexpr int kCols = kFold ? S::PT / 2 : S::PT;
+    using InP = Operand<T, kP, S::PT, S::kWavesAll, kFold>;
+    using InQ = Operand<T, kQ, S::QT, S::kWavesAll, false>;
+    static_assert(!kFold || InP::kLoads * InP::kRowsPerLoad == 32 || InP::kLoads * InP::kRowsPerLoad == 64, "whole runs of one weight's rows");
+    static_assert(!kFold || S::PB == 4, "a wave's strip is 32 rows of each weight");
+
+    size_t col0, row0;
+    bool second;                                    // dW: of dWu
+    unsigned part, begin, end, once;                // stages; dx: the first `once` are Wg's
+    InP in_p;
+    InQ in_q;
+    uint64_t p0, p1, q0, q1;
+
+    // Tiles are walked in bands of eight rows: what 32 workgroups of an XCD read at a time then fits its L2.
+    __device__ __forceinline__ void init(const GluArgs<T>& p, unsigned at, unsigned tp, unsigned tq, int wave, int lane) {
+        const unsigned tiles = tp * tq;
+        part = at / tiles;
+        at -= part * tiles;
+        const unsigned band = at / (8 * tp), in_band = at % (8 * tp), height = tq - band * 8 < 8 ? tq - band * 8 : 8;
+        const unsigned tile_q = band * 8 + in_band % height, halves = tq / 2;
+        col0 = static_cast<size_t>(in_band / height) * kCols;
+        second = DOES == Does::kDw && tile_q >= halves;
+        row0 = static_cast<size_t>(second ? tile_q - halves : tile_q) * S::QT;
+        const size_t rows = DOES == Does::kDw ? p.n : p.m, cols = kFold ? p.n : p.k;
+        once = static_cast<unsigned>((length(p) + kSteps - 1) / kSteps);
+        const uint64_t stages = DOES == Does::kDx ? 2 * once : once;
+        begin = static_cast<unsigned>(stages * part / p.parts);
+        end = static_cast<unsigned>(stages * (part + 1) / p.parts);
+        in_p.init(wave, lane, static_cast<unsigned>(kFold || DOES == Does::kDx ? p.ldw : p.ldx), static_cast<unsigned>(cols - col0 < S::PT ? cols - col0 : S::PT));
+        in_q.init(wave, lane, static_cast<unsigned>(kFold ? p.ldx : p.ldd), static_cast<unsigned>(rows - row0 < S::QT ? rows - row0 : S::QT));
+        p0 = reinterpret_cast<uint64_t>(kFold ? p.wg + col0 * p.ldw : DOES == Does::kDx ? p.wg + col0 : p.x + col0);
+        p1 = reinterpret_cast<uint64_t>(kFold ? p.wu + col0 * p.ldw : p.wu + col0);
+        q0 = reinterpret_cast<uint64_t>(kFold ? p.x + row0 * p.ldx : DOES == Does::kDx ? p.dg + row0 * p.ldd : (second ? p.du : p.dg) + row0);
+        q1 = reinterpret_cast<uint64_t>(p.du + row0 * p.ldd);
+    }
+    static __device__ __forceinline__ size_t length(const GluArgs<T>& p) { return kFold ? p.k : DOES == Does::kDx ? p.n : p.m; }
+
+    __device__ __forceinline__ void fetch(const GluArgs<T>& p, unsigned s, unsigned lds) const {
+        const uint64_t step_p = kFold ? kStageBytes : kSteps * W * (DOES == Does::kDx ? p.ldw : p.ldx);
+        const uint64_t step_q = DOES == Does::kDw ? kSteps * W * p.ldd : kStageBytes;
+        const bool late = DOES == Does::kDx && s >= once;
+        const unsigned t = late ? s - once : s;
+        const int64_t left = static_cast<int64_t>(length(p)) - static_cast<int64_t>(t) * kSteps;
+        in_p.fetch((late ? p1 : p0) + t * step_p, p1 + t * step_p, left, lds);
+        // (dx: the columns of dg and du behind the last are zeros, up to a whole stage)
+        in_q.fetch((late ? q1 : q0) + t * step_q, 0, DOES == Does::kDx ? kSteps : left, lds + S::PT * kStageBytes);
+    }
+};
+
+// Workgroups take tiles until there are none left; the next tile's first stages are on their way while a tile is finished.
+template <typename T, Does DOES, class S>
+__global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluArgs<T> p, unsigned tp, unsigned tq) {
+    using Where = Tile<T, DOES, S>;
+    constexpr bool kFold = Where::kFold;
     __shared__ alignas(1024) unsigned char lds[2 * S::kStage];
     const unsigned base = static_cast<unsigned>(reinterpret_cast<uintptr_t>((LdsByte*)lds));
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wp = wave % S::WP, wq = wave / S::WP;
-    unsigned tile_p, tile_q;
-    tile_of(blockIdx.x, tp, tq, &tile_p, &tile_q);
+    const int wp = wave % S::WP, wq = wave / S::WP, r = lane & 15, quarter = lane >> 4;
+    const unsigned items = tp * tq * p.parts;
 
-    // The tile's place, the operands' bases and the stages of the reduction.
-    constexpr int kCols = kFold ? S::PT / 2 : S::PT;
-    const size_t col0 = static_cast<size_t>(tile_p) * kCols;
-    const unsigned halves = DOES == Does::kDw ? tq / 2 : 0;              // dW: tiles of dWg, then of dWu
-    const bool second = DOES == Does::kDw && tile_q >= halves;
-    const size_t row0 = static_cast<size_t>(second ? tile_q - halves : tile_q) * S::QT;
-    const size_t rows = DOES == Does::kDw ? p.n : p.m, cols = kFold ? p.n : p.k;
-    const size_t length = kFold ? p.k : DOES == Does::kDx ? p.n : p.m;   // dx: twice
-    const unsigned once = static_cast<unsigned>((length + kSteps - 1) / kSteps), stages = DOES == Does::kDx ? 2 * once : once;
-
-    Operand<T, kP, S::PT, S::kWavesAll, kFold> in_p;
-    Operand<T, kQ, S::QT, S::kWavesAll, false> in_q;
-    in_p.init(wave, lane, static_cast<unsigned>(kFold || DOES == Does::kDx ? p.ldw : p.ldx), static_cast<unsigned>(cols - col0 < S::PT ? cols - col0 : S::PT));
-    in_q.init(wave, lane, static_cast<unsigned>(kFold ? p.ldx : p.ldd), static_cast<unsigned>(rows - row0 < S::QT ? rows - row0 : S::QT));
-    const T* const dd = second ? p.du : p.dg;
-    const uint64_t p0 = reinterpret_cast<uint64_t>(kFold ? ((wave & 1) ? p.wu : p.wg) + col0 * p.ldw : DOES == Does::kDx ? p.wg + col0 : p.x + col0);
-    const uint64_t p1 = reinterpret_cast<uint64_t>(p.wu + col0);
-    const uint64_t q0 = reinterpret_cast<uint64_t>(kFold ? p.x + row0 * p.ldx : DOES == Does::kDx ? p.dg + row0 * p.ldd : dd + row0);
-    const uint64_t q1 = reinterpret_cast<uint64_t>(p.du + row0 * p.ldd);
-    const uint64_t step_p = kFold ? kStageBytes : kSteps * W * (DOES == Does::kDx ? p.ldw : p.ldx);
-    const uint64_t step_q = DOES == Does::kDw ? kSteps * W * p.ldd : kStageBytes;
-    static_assert(!kFold || Operand<T, kP, S::PT, S::kWavesAll, kFold>::kLoads == 4, "a wave fetches 32 rows of one weight");
-    static_assert(!kFold || S::PB == 4, "a wave's strip is 32 rows of each weight");
-
-    const auto fetch = [&](unsigned s) {
-        const unsigned lds_at = base + (s & 1) * S::kStage;
-        const bool late = DOES == Does::kDx && s >= once;
-        const unsigned t = late ? s - once : s;
-        const int64_t left = static_cast<int64_t>(length) - static_cast<int64_t>(t) * kSteps;
-        in_p.fetch((late ? p1 : p0) + t * step_p, left, lds_at);
-        // (dx: the columns of dg and du behind the last are zeros, up to a whole stage)
-        in_q.fetch((late ? q1 : q0) + t * step_q, DOES == Does::kDx ? kSteps : left, lds_at + S::PT * kStageBytes);
-    };
-
-    Reader<T, kP, S::PT, S::PB, kFold> out_p;
-    Reader<T, kQ, S::QT, S::QB, false> out_q;
+    using ReadP = Reader<T, Where::kP, S::PT, S::PB, kFold>;
+    using ReadQ = Reader<T, Where::kQ, S::QT, S::QB, false>;
+    ReadP out_p;
+    ReadQ out_q;
     out_p.init(base, wp, lane);
     out_q.init(base + S::PT * kStageBytes, wq, lane);
-
-    float4v acc[S::PB][S::QB];
-#pragma unroll
-    for (int i = 0; i < S::PB; ++i)
-#pragma unroll
-        for (int j = 0; j < S::QB; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
-
-    // A stage is multiplied in two halves.  While a half's products run, the next half is read from LDS; between
-    // the halves everyone has read the stage, and its buffer takes the stage after the next.
     using Frag = typename Fragment<T>::type;
     Frag a[2][S::PB], b[2][S::QB];
+    float4v acc[S::PB][S::QB];
     const auto read = [&](auto half, unsigned stage) {
         constexpr int kHalf = decltype(half)::value;
 #pragma unroll
@@ -517,95 +603,146 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 ? 2 : 1) void produ
         for (int j = 0; j < S::QB; ++j)
 #pragma unroll
             for (int i = 0; i < S::PB; ++i) acc[i][j] = multiply(a[kHalf][i], b[kHalf][j], acc[i][j]);
-        interleave<Reader<T, kP, S::PT, S::PB, kFold>::kReads + Reader<T, kQ, S::QT, S::QB, false>::kReads,
-                   S::PB * S::QB * (W == 4 ? 4 : 1)>();
+        interleave<ReadP::kReads + ReadQ::kReads, S::PB * S::QB * (sizeof(T) == 4 ? 4 : 1)>();
     };
     constexpr std::integral_constant<int, 0> kFirst{};
     constexpr std::integral_constant<int, 1> kSecond{};
-    if (stages != 0) {
-        fetch(0);
+
+    Where tile;
+    const auto begin = [&](unsigned item) {
+        tile.init(p, place_of(item, items), tp, tq, wave, lane);
+        if (tile.begin < tile.end) tile.fetch(p, tile.begin, base);
+        if (tile.begin + 1 < tile.end) tile.fetch(p, tile.begin + 1, base + S::kStage);
+    };
+    begin(blockIdx.x);
+    for (unsigned item = blockIdx.x; item < items;) {
+#pragma unroll
+        for (int i = 0; i < S::PB; ++i)
+#pragma unroll
+            for (int j = 0; j < S::QB; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
+        // A stage is multiplied in two halves.  While a half's products run, the next half is read from LDS; between
+        // the halves everyone has read the stage, and its buffer takes the stage after the next.
         wait_loads<0>();
         group_barrier();
-        if (stages > 1) fetch(1);
         read(kFirst, 0);
-    }
-    for (unsigned s = 0; s < stages; ++s) {
-        read(kSecond, (s & 1) * S::kStage);
-        product(kFirst);
-        wait_loads<0>();
-        group_barrier();                     // stage s + 1 is there, and everyone has read stage s
-        if (s + 2 < stages) fetch(s + 2);
-        read(kFirst, (~s & 1) * S::kStage);  // (behind the last stage: what the buffer held, for nothing)
-        product(kSecond);
-    }
-
-    const int r = lane & 15, quarter = lane >> 4;
-    if constexpr (kFold) {
-        const uint64_t offset = effective_offset(p.d);
-        const size_t end = DOES == Does::kSlope ? p.ldd : p.n;      // dg and du are written up to their rows' ends
-        // One copy of the code for all blocks: each turn takes the first ones, and the others move up.
-#pragma unroll 1
-        for (int j = 0; j < S::QB; ++j) {
-            const size_t row = row0 + (wq * S::QB + j) * 16 + r, col = col0 + wp * 32 + quarter * 8;
-            Eight g, u;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) g.v[e] = acc[e / 4][0][e % 4], u.v[e] = acc[2 + e / 4][0][e % 4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int next = 1; next < S::QB; ++next) acc[i][next - 1] = acc[i][next];
-            if (row >= p.m || col >= end) continue;
-            if (col < p.n) {
-                finish8<T, DOES>(p, offset, row, col, g, u);
-            } else if constexpr (DOES == Does::kSlope) {
-                const Eight zero = {};
-                store8(p.dg + row * p.ldd + col, zero), store8(p.du + row * p.ldd + col, zero);
-            }
+        for (unsigned s = tile.begin; s < tile.end; ++s) {
+            const unsigned even = ((s - tile.begin) & 1) * S::kStage;
+            read(kSecond, even);
+            product(kFirst);
+            wait_loads<0>();
+            group_barrier();                     // stage s + 1 is there, and everyone has read stage s
+            if (s + 2 < tile.end) tile.fetch(p, s + 2, base + even);
+            read(kFirst, S::kStage - even);      // (behind the last stage: what the buffer held, for nothing)
+            product(kSecond);
         }
-    } else {
-        T* const out = second ? p.out2 : p.out;
+        const size_t col0 = tile.col0, row0 = tile.row0;
+        const unsigned part = tile.part;
+        const bool second = tile.second;
+        item += gridDim.x;
+        if (item < items) {
+            group_barrier();                     // (the reads for nothing are done)
+            begin(item);
+        }
+
+        const size_t row_first = row0 + wq * S::QB * 16 + r;
+        if constexpr (kFold) {
+            const size_t col = col0 + wp * 32 + quarter * 8;
+            if (p.parts > 1) {
 #pragma unroll
-        for (int j = 0; j < S::QB; ++j) {
-            const size_t row = row0 + (wq * S::QB + j) * 16 + r;
-            if (row >= rows) continue;
+                for (int j = 0; j < S::QB; ++j) {
+                    const size_t row = row_first + j * 16;
+                    if (row >= p.m || col >= p.lds) continue;
 #pragma unroll
-            for (int i = 0; i < S::PB; ++i) {
-                const size_t col = col0 + (wp * S::PB + i) * 16 + quarter * 4;
-                T* const at = out + row * p.ldo + col;
-                if (p.wide && col + 4 <= cols) {
-                    struct alignas(4 * W) { T v[4]; } four;
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<float4v*>(p.sums + ((part * 2 + i / 2) * p.m + row) * p.lds + col + i % 2 * 4) = acc[i][j];
+                }
+                continue;
+            }
+            finish_tile<T, DOES, S>(p, row_first, col, acc);
+        } else {
+            const size_t rows = DOES == Does::kDw ? p.n : p.m;
+            constexpr int kMatrices = DOES == Does::kDw ? 2 : 1;
+            T* const out = second ? p.out2 : p.out;
+            float* const sums = p.sums + (part * kMatrices + (second ? 1 : 0)) * rows * p.lds;
+#pragma unroll
+            for (int j = 0; j < S::QB; ++j) {
+                const size_t row = row_first + j * 16;
+                if (row >= rows) continue;
+#pragma unroll
+                for (int i = 0; i < S::PB; ++i) {
+                    const size_t col = col0 + (wp * S::PB + i) * 16 + quarter * 4;
+                    if (p.parts > 1) {
+                        if (col < p.lds) *reinterpret_cast<float4v*>(sums + row * p.lds + col) = acc[i][j];
+                        continue;
+                    }
+                    T* const at = out + row * p.ldo + col;
+                    struct alignas(4 * sizeof(T)) Four { T v[4]; } four;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) four.v[e] = static_cast<T>(acc[i][j][e]);
-                    __builtin_memcpy(__builtin_assume_aligned(at, 4 * W), &four, sizeof four);
-                } else {
+                    if (p.wide && col + 4 <= p.k) {
+                        *reinterpret_cast<Four*>(at) = four;
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (col + e < cols) at[e] = static_cast<T>(acc[i][j][e]);
+                        for (int e = 0; e < 4; ++e)
+                            if (col + e < p.k) at[e] = four.v[e];
+                    }
                 }
             }
         }
     }
 }
 
+// The same for one group of eight columns, outside a tile.
+template <typename T, Does DOES>
+__device__ __forceinline__ void finish_group(const GluArgs<T>& p, size_t row, size_t col, Eight& g, Eight& u) {
+    const int there = columns_left(p.n, col);
+    const unsigned keep = p.d.active && there > 0 ? keep_span(p.d, effective_offset(p.d), static_cast<uint64_t>(row) * p.n + col) : 0xFFu;
+    const Eight dh = DOES == Does::kSlope ? load_some(p.dh + row * p.lddh + col, there, p.wide) : Eight{};
+    finish8<T, DOES>(p, keep, row, col, there, dh, g, u);
+}
+
+// The parts' sums joined, in the order of the parts.  A lane takes eight neighbouring columns.
+template <typename T, Does DOES>
+__global__ __launch_bounds__(256) void join_kernel(GluArgs<T> p, uint64_t total) {
+    constexpr bool kFold = DOES == Does::kForward || DOES == Does::kSlope;
+    constexpr int kMatrices = DOES == Does::kDx ? 1 : 2;
+    const uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= total) return;
+    const size_t rows = DOES == Does::kDw ? p.n : p.m, cols = kFold ? p.n : p.k;
+    const size_t width = DOES == Does::kSlope ? p.ldd : p.lds;           // dg and du are written up to their rows' ends
+    const uint64_t groups = width / 8, line = i / groups;
+    const size_t col = (i - line * groups) * 8;
+    const bool second = DOES == Does::kDw && line >= rows;
+    const size_t row = second ? line - rows : line;
+    const auto sum = [&](int matrix) {
+        Eight e = {};
+        const float* at = p.sums + (matrix * rows + row) * p.lds + col;
+#pragma unroll 4
+        for (unsigned part = 0; part < p.parts; ++part, at += kMatrices * rows * p.lds) {
+            const Eight x = load8(at);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e.v[j] += x.v[j];
+        }
+        return e;
+    };
+    if constexpr (kFold) {
+        Eight g = {}, u = {};
+        if (col < p.n) g = sum(0), u = sum(1);
+        finish_group<T, DOES>(p, row, col, g, u);
+    } else {
+        store_some((second ? p.out2 : p.out) + row * p.ldo + col, sum(second ? 1 : 0), columns_left(cols, col), p.wide);
+    }
+}
+
 // dg and du from kept projections; their rows are filled with zeros up to ldd.
 template <typename T>
 __global__ __launch_bounds__(256) void slope_kernel(GluArgs<T> p) {
-    const uint64_t offset = effective_offset(p.d);
     const uint64_t groups = p.ldd / 8, total = groups * p.m, step = static_cast<uint64_t>(gridDim.x) * 256;
     for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += step) {
         const size_t row = i / groups, col = (i - row * groups) * 8;
-        Eight g = {}, u = {};
-        if (col >= p.n) {
-            store8(p.dg + row * p.ldd + col, g), store8(p.du + row * p.ldd + col, u);
-            continue;
-        }
-        const T *gate = p.gate_in + row * p.ldp + col, *up = p.up_in + row * p.ldp + col;
-        if (p.wide && col + 8 <= p.n) {
-            g = load8(gate), u = load8(up);
-        } else {
-            for (int j = 0; j < 8 && col + j < p.n; ++j) g.v[j] = static_cast<float>(gate[j]), u.v[j] = static_cast<float>(up[j]);
-        }
-        finish8<T, Does::kSlope>(p, offset, row, col, g, u);
+        const int there = columns_left(p.n, col);
+        Eight g = load_some(p.gate_in + row * p.ldp + col, there, p.wide), u = load_some(p.up_in + row * p.ldp + col, there, p.wide);
+        finish_group<T, Does::kSlope>(p, row, col, g, u);
     }
 }
 
@@ -674,11 +811,103 @@ zvc_status dropout_as(const void* x, size_t ldx, const void* residual, size_t ld
                   static_cast<const T*>(x), ldx, static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy, cols, total, d);
 }
 
+bool sizes_ok(size_t m, size_t n, size_t k) {
+    return m <= ZVC_FFN_MAX_ROWS && n <= ZVC_FFN_MAX_COLUMNS && k <= ZVC_FFN_MAX_COLUMNS;
+}
+
+bool stride_ok(size_t ld, size_t cols) { return ld >= cols && ld <= ZVC_FFN_MAX_COLUMNS; }
+
+using Large = Shape<4, 2, 4, 8>;                // 256 x 256, eight waves
+using Small = Shape<2, 2, 4, 4>;                // 128 x 128, four waves
+using Thin = Shape<4, 1, 4, 2>;                 // 256 x 32, four waves: few tokens
+
+constexpr unsigned kUnits = 256;                // compute units
+
+// Tiles of a product of this shape, by columns and rows.
+template <Does DOES, class S>
+void tiles_of(size_t m, size_t n, size_t k, size_t* cols, size_t* rows) {
+    constexpr bool kFold = DOES == Does::kForward || DOES == Does::kSlope;
+    *cols = kFold ? div_up(n, S::PT / 2) : div_up(k, S::PT);
+    *rows = DOES == Does::kDw ? 2 * div_up(n, S::QT) : div_up(m, S::QT);
+}
+
+enum class Size { kLarge, kSmall, kThin };
+
+// How a product is cut: the tiles' shape, and how many parts of the reduction are summed apart and joined.
+struct Cut {
+    Size size;
+    unsigned parts;
+    size_t sums;                                // bytes of the parts' sums
+};
+
+template <Does DOES>
+Cut cut_of(size_t m, size_t n, size_t k, size_t w) {
+    size_t cols, rows;
+    Cut cut{};
+    tiles_of<DOES, Large>(m, n, k, &cols, &rows);
+    const size_t outer = DOES == Does::kDw ? n : m;
+    size_t slots = kUnits;
+    if (cols * rows >= 192) {
+        cut.size = Size::kLarge;
+    } else if (outer > 32) {
+        cut.size = Size::kSmall, slots = 2 * kUnits;
+        tiles_of<DOES, Small>(m, n, k, &cols, &rows);
+    } else {
+        cut.size = Size::kThin, slots = 2 * kUnits;
+        tiles_of<DOES, Thin>(m, n, k, &cols, &rows);
+    }
+    // Parts of at least four stages, as many as fill the card once.
+    const size_t stages = div_up(DOES == Does::kDw ? m : DOES == Does::kDx ? 2 * n : k, kStageBytes / w);
+    const size_t tiles = cols * rows > 0 ? cols * rows : 1;
+    size_t parts = cut.size == Size::kLarge ? 1 : slots / tiles;
+    if (parts > stages / 4) parts = stages / 4;
+    cut.parts = static_cast<unsigned>(parts < 2 ? 1 : parts);
+    if (cut.parts > 1)
+        cut.sums = cut.parts * (DOES == Does::kDx ? 1 : 2) * outer * round_up(DOES == Does::kDw || DOES == Does::kDx ? k : n, 8) * 4;
+    return cut;
+}
+
+template <typename T, Does DOES, class S>
+zvc_status product_of(const GluArgs<T>& p, hipStream_t stream) {
+    size_t cols, rows;
+    tiles_of<DOES, S>(p.m, p.n, p.k, &cols, &rows);
+    if (cols * rows * p.parts > 0x7FFFFFFF) return ZVC_E_ARG;
+    const size_t items = cols * rows * p.parts, room = kUnits * S::kPerUnit;
+    return launch(product_kernel<T, DOES, S>, dim3(items < room ? items : room), S::kThreads, stream, p, static_cast<unsigned>(cols),
+                  static_cast<unsigned>(rows));
+}
+
+template <typename T, Does DOES>
+zvc_status product(GluArgs<T> p, float* sums, hipStream_t stream) {
+    const Cut cut = cut_of<DOES>(p.m, p.n, p.k, sizeof(T));
+    p.parts = cut.parts;
+    p.sums = sums;
+    p.lds = round_up(DOES == Does::kDw || DOES == Does::kDx ? p.k : p.n, 8);
+    const zvc_status st = cut.size == Size::kLarge ? product_of<T, DOES, Large>(p, stream)
+                        : cut.size == Size::kSmall ? product_of<T, DOES, Small>(p, stream) : product_of<T, DOES, Thin>(p, stream);
+    if (st != ZVC_OK || p.parts == 1) return st;
+    if constexpr (DOES == Does::kDx || DOES == Does::kDw) {
+        const auto takes = [&](const T* at) { return at == nullptr || (aligned_to(at, 16) && p.ldo * sizeof(T) % 16 == 0); };
+        p.wide = takes(p.out) && takes(p.out2);
+    }
+    const uint64_t total = (DOES == Does::kDw ? 2 * p.n : p.m) * ((DOES == Does::kSlope ? p.ldd : p.lds) / 8);
+    return launch(join_kernel<T, DOES>, dim3(div_up(total, 256)), 256, stream, p, total);
+}
+
+// Bytes for the sums of whichever of a call's products is cut into parts.
+size_t sums_bytes(size_t m, size_t n, size_t k, size_t w, bool backward) {
+    if (!backward) return cut_of<Does::kForward>(m, n, k, w).sums;
+    size_t most = cut_of<Does::kSlope>(m, n, k, w).sums;
+    const size_t dx = cut_of<Does::kDx>(m, n, k, w).sums, dw = cut_of<Does::kDw>(m, n, k, w).sums;
+    if (dx > most) most = dx;
+    return dw > most ? dw : most;
+}
+
 constexpr size_t kColumnsUp = 64;               // dg's and du's rows are filled up to a multiple of this
 
 // Where the parts of a workspace begin.
 struct Layout {
-    size_t dg, du, x, wg, wu, bytes;
+    size_t dg, du, x, wg, wu, sums, bytes;
     size_t ldd, aligned_k;              // row strides of dg and du, and of the copies of x, Wg and Wu
 };
 
@@ -694,35 +923,9 @@ Layout layout_of(size_t m, size_t n, size_t k, size_t w, bool backward, bool cop
     };
     if (backward) at.dg = part(m * at.ldd * w), at.du = part(m * at.ldd * w);
     if (copies) at.x = part(m * at.aligned_k * w), at.wg = part(n * at.aligned_k * w), at.wu = part(n * at.aligned_k * w);
+    at.sums = part(sums_bytes(m, n, k, w, backward));
     at.bytes += 256;
     return at;
-}
-
-bool sizes_ok(size_t m, size_t n, size_t k) {
-    return m <= ZVC_FFN_MAX_ROWS && n <= ZVC_FFN_MAX_COLUMNS && k <= ZVC_FFN_MAX_COLUMNS;
-}
-
-bool stride_ok(size_t ld, size_t cols) { return ld >= cols && ld <= ZVC_FFN_MAX_COLUMNS; }
-
-using Large = Shape<4, 2, 4, 8>;                // 256 x 256, eight waves
-using Small = Shape<2, 2, 4, 4>;                // 128 x 128, four waves
-
-template <typename T, Does DOES, class S>
-zvc_status product_of(const GluArgs<T>& p, hipStream_t stream) {
-    constexpr bool kFold = DOES == Does::kForward || DOES == Does::kSlope;
-    const size_t cols = kFold ? div_up(p.n, S::PT / 2) : div_up(p.k, S::PT);
-    const size_t rows = DOES == Does::kDw ? 2 * div_up(p.n, S::QT) : div_up(p.m, S::QT);
-    if (cols * rows > 0x7FFFFFFF) return ZVC_E_ARG;
-    return launch(product_kernel<T, DOES, S>, dim3(cols * rows), S::kThreads, stream, p, static_cast<unsigned>(cols),
-                  static_cast<unsigned>(rows));
-}
-
-template <typename T, Does DOES>
-zvc_status product(const GluArgs<T>& p, hipStream_t stream) {
-    constexpr bool kFold = DOES == Does::kForward || DOES == Does::kSlope;
-    const size_t tiles = (kFold ? div_up(p.n, Large::PT / 2) : div_up(p.k, Large::PT)) *
-                         (DOES == Does::kDw ? 2 * div_up(p.n, Large::QT) : div_up(p.m, Large::QT));
-    return tiles >= 192 ? product_of<T, DOES, Large>(p, stream) : product_of<T, DOES, Small>(p, stream);
 }
 
 // Copies of x and the weights where they do not take 16-byte accesses as they lie.
@@ -757,18 +960,19 @@ template <typename T>
 zvc_status forward_as(GluArgs<T> p, const Layout& at, unsigned char* base, hipStream_t stream) {
     if (zvc_status st = align_inputs(&p, at, base, stream)) return st;
     p.wide = takes(p.h, p.ldh, 16) && (p.gate == nullptr || (takes(p.gate, p.ldp, 16) && takes(p.up, p.ldp, 16)));
-    return product<T, Does::kForward>(p, stream);
+    return product<T, Does::kForward>(p, reinterpret_cast<float*>(base + at.sums), stream);
 }
 
 template <typename T>
 zvc_status backward_as(GluArgs<T> p, T* dx, size_t lddx, T* dwg, T* dwu, size_t lddw, const Layout& at, unsigned char* base,
                        hipStream_t stream) {
     if (zvc_status st = align_inputs(&p, at, base, stream)) return st;
+    float* const sums = reinterpret_cast<float*>(base + at.sums);
     if (p.m != 0 && p.n != 0) {
         zvc_status st;
         p.wide = takes(p.dh, p.lddh, 16);
         if (p.gate_in == nullptr) {
-            st = product<T, Does::kSlope>(p, stream);
+            st = product<T, Does::kSlope>(p, sums, stream);
         } else {
             p.wide = p.wide && takes(p.gate_in, p.ldp, 16) && takes(p.up_in, p.ldp, 16);
             const size_t blocks = div_up(p.m * (p.ldd / 8), 256);
@@ -778,11 +982,11 @@ zvc_status backward_as(GluArgs<T> p, T* dx, size_t lddx, T* dwg, T* dwu, size_t 
     }
     if (dx != nullptr && p.m != 0) {
         p.out = dx, p.ldo = lddx, p.wide = takes(dx, lddx, 4 * sizeof(T));
-        if (zvc_status st = product<T, Does::kDx>(p, stream)) return st;
+        if (zvc_status st = product<T, Does::kDx>(p, sums, stream)) return st;
     }
     if (dwg == nullptr || p.n == 0) return ZVC_OK;
     p.out = dwg, p.out2 = dwu, p.ldo = lddw, p.wide = takes(dwg, lddw, 4 * sizeof(T)) && takes(dwu, lddw, 4 * sizeof(T));
-    return product<T, Does::kDw>(p, stream);
+    return product<T, Does::kDw>(p, sums, stream);
 }
 
 }  // namespace
