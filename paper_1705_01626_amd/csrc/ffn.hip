@@ -87,18 +87,20 @@ struct Eight {
     float v[8];
 };
 
+// 16 bytes at any element: the instruction takes them wherever they lie.
 template <typename T>
-struct alignas(16) Pack {
+struct Pack {
     T v[16 / sizeof(T)];
 };
 
 template <typename T>
-__device__ __forceinline__ Eight load8(const T* at) {          // 16-byte aligned
+__device__ __forceinline__ Eight load8(const T* at) {
     Eight out;
     constexpr int kPer = 16 / sizeof(T);
 #pragma unroll
     for (int h = 0; h < 8 / kPer; ++h) {
-        const Pack<T> p = reinterpret_cast<const Pack<T>*>(at)[h];
+        Pack<T> p;
+        __builtin_memcpy(&p, at + h * kPer, 16);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) out.v[h * kPer + j] = static_cast<float>(p.v[j]);
     }
@@ -106,22 +108,40 @@ __device__ __forceinline__ Eight load8(const T* at) {          // 16-byte aligne
 }
 
 template <typename T>
-__device__ __forceinline__ void store8(T* at, const Eight& e) {   // 16-byte aligned
+__device__ __forceinline__ void store8(T* at, const Eight& e) {
     constexpr int kPer = 16 / sizeof(T);
 #pragma unroll
     for (int h = 0; h < 8 / kPer; ++h) {
         Pack<T> p;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) p.v[j] = static_cast<T>(e.v[h * kPer + j]);
-        reinterpret_cast<Pack<T>*>(at)[h] = p;
+        __builtin_memcpy(at + h * kPer, &p, 16);
     }
+}
+
+// The first `there` of eight elements.
+template <typename T>
+__device__ __forceinline__ Eight load_some(const T* at, int there) {
+    if (there >= 8) return load8(at);
+    Eight e = {};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < there) e.v[j] = static_cast<float>(at[j]);
+    return e;
+}
+template <typename T>
+__device__ __forceinline__ void store_some(T* at, const Eight& e, int there) {
+    if (there >= 8) return store8(at, e);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < there) at[j] = static_cast<T>(e.v[j]);
 }
 
 constexpr int kDropThreads = 256;
 
-// y = drop(x) [+ residual].  A lane owns eight consecutive elements, one counter of the generator.  VECTOR: every
-// row's groups of eight lie at multiples of 16 bytes, and no group straddles two rows.
-template <typename T, bool VECTOR>
+// y = drop(x) [+ residual].  A lane owns eight consecutive elements, one counter of the generator.  WHOLE: no group of
+// eight straddles two rows.
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const T* x, size_t ldx, const T* residual, size_t ldr,
                                                                T* y, size_t ldy, size_t cols, uint64_t total, Drop d) {
     const uint64_t group = static_cast<uint64_t>(blockIdx.x) * kDropThreads + threadIdx.x;
@@ -129,16 +149,17 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const T* x, size_
     if (first >= total) return;
     const unsigned keep = d.active ? keep_group(d, effective_offset(d), group) : 0xFFu;
     uint64_t row = first / cols, col = first - row * cols;
-    if constexpr (VECTOR) {
-        Eight e = load8(x + row * ldx + col);
+    if constexpr (WHOLE) {
+        const int there = total - first < 8 ? static_cast<int>(total - first) : 8;
+        Eight e = load_some(x + row * ldx + col, there);
 #pragma unroll
         for (int j = 0; j < 8; ++j) e.v[j] = (keep >> j & 1u) ? e.v[j] * d.scale : 0.f;
         if (residual != nullptr) {
-            const Eight r = load8(residual + row * ldr + col);
+            const Eight r = load_some(residual + row * ldr + col, there);
 #pragma unroll
             for (int j = 0; j < 8; ++j) e.v[j] += r.v[j];
         }
-        store8(y + row * ldy + col, e);
+        store_some(y + row * ldy + col, e, there);
     } else {
         for (int j = 0; j < 8 && first + j < total; ++j) {
             float v = (keep >> j & 1u) ? static_cast<float>(x[row * ldx + col]) * d.scale : 0.f;
@@ -403,11 +424,9 @@ struct GluArgs {
     T *out, *out2;                      // dx; dwg and dwu
     size_t ldx, ldw, lddh, ldh, ldp, ldd, ldo, m, n, k;
     int act;
-    float* sums;                        // parts > 1: each part's sums, to be joined
-    size_t lds;                         // their row stride
-    unsigned parts;                     // of the reduction
+    float* sums;                        // parts' sums, to be joined: part by part, tile by tile as they lie in it
+    unsigned whole, parts;              // the tiles behind the first `whole` are summed in parts of the reduction
     Drop d;
-    bool wide;                          // the outputs' and dh's rows take 16-byte (dx, dw: four-element) accesses
 };
 
 // Eight neighbouring columns' projections g and u, col a multiple of eight: dg and du in their place ...
@@ -433,24 +452,6 @@ __device__ __forceinline__ void forward8(const GluArgs<T>& p, unsigned keep, Eig
     }
 }
 
-// The first `there` of eight elements, wherever they lie; `wide`: a multiple of 16 bytes.
-template <typename T>
-__device__ __forceinline__ Eight load_some(const T* at, int there, bool wide) {
-    Eight e = {};
-    if (wide && there >= 8) return load8(at);
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (j < there) e.v[j] = static_cast<float>(at[j]);
-    return e;
-}
-template <typename T>
-__device__ __forceinline__ void store_some(T* at, const Eight& e, int there, bool wide) {
-    if (wide && there >= 8) return store8(at, e);
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (j < there) at[j] = static_cast<T>(e.v[j]);
-}
-
 // What becomes of them in their row: `there` of them (none: dg's and du's filling) are columns.  dh: for the slope.
 template <typename T, Does DOES>
 __device__ __forceinline__ void finish8(const GluArgs<T>& p, unsigned keep, size_t row, size_t col, int there, const Eight& dh, Eight& g, Eight& u) {
@@ -464,10 +465,10 @@ __device__ __forceinline__ void finish8(const GluArgs<T>& p, unsigned keep, size
     } else {
         Eight h;
         with_activation(p.act, [&](auto act) { forward8<decltype(act)::value>(p, keep, h, g, u); });
-        store_some(p.h + row * p.ldh + col, h, there, p.wide);
+        store_some(p.h + row * p.ldh + col, h, there);
         if (p.gate != nullptr) {
-            store_some(p.gate + row * p.ldp + col, g, there, p.wide);
-            store_some(p.up + row * p.ldp + col, u, there, p.wide);
+            store_some(p.gate + row * p.ldp + col, g, there);
+            store_some(p.up + row * p.ldp + col, u, there);
         }
     }
 }
@@ -491,7 +492,7 @@ __device__ __forceinline__ void finish_tile(const GluArgs<T>& p, size_t row, siz
             keep |= static_cast<uint64_t>(keep_span(p.d, offset, static_cast<uint64_t>(row + j * 16) * p.n + col)) << (8 * j);
     }
     const auto load = [&](int j) {
-        return DOES == Does::kSlope && j < S::QB && row + j * 16 < p.m ? load_some(p.dh + (row + j * 16) * p.lddh + col, there, p.wide) : Eight{};
+        return DOES == Does::kSlope && j < S::QB && row + j * 16 < p.m ? load_some(p.dh + (row + j * 16) * p.lddh + col, there) : Eight{};
     };
     Eight dh = load(0);
 #pragma unroll
@@ -528,27 +529,39 @@ struct Tile {
     static_assert(!kFold || S::PB == 4, "a wave's strip is 32 rows of each weight");
 
     size_t col0, row0;
-    bool second;                                    // dW: of dWu
-    unsigned part, begin, end, once;                // stages; dx: the first `once` are Wg's
+    bool second, split;                             // dW: of dWu; summed in parts
+    unsigned number, part;                          // of the split tiles; of its reduction
+    unsigned begin, end, once;                      // stages; dx: the first `once` are Wg's
     InP in_p;
     InQ in_q;
     uint64_t p0, p1, q0, q1;
 
-    // Tiles are walked in bands of eight rows: what 32 workgroups of an XCD read at a time then fits its L2.
-    __device__ __forceinline__ void init(const GluArgs<T>& p, unsigned at, unsigned tp, unsigned tq, int wave, int lane) {
-        const unsigned tiles = tp * tq;
-        part = at / tiles;
-        at -= part * tiles;
+    // Where tile `at` lies.  Tiles are walked in bands of eight rows: what 32 workgroups of an XCD read at a time then fits its L2.
+    __device__ __forceinline__ void locate(unsigned at, unsigned tp, unsigned tq) {
         const unsigned band = at / (8 * tp), in_band = at % (8 * tp), height = tq - band * 8 < 8 ? tq - band * 8 : 8;
         const unsigned tile_q = band * 8 + in_band % height, halves = tq / 2;
         col0 = static_cast<size_t>(in_band / height) * kCols;
         second = DOES == Does::kDw && tile_q >= halves;
         row0 = static_cast<size_t>(second ? tile_q - halves : tile_q) * S::QT;
+    }
+    __device__ __forceinline__ void init(const GluArgs<T>& p, unsigned item, unsigned tp, unsigned tq, int wave, int lane) {
+        const unsigned rest = tp * tq - p.whole;
+        split = item >= p.whole;
+        part = 0;
+        if (split) {
+            const unsigned at = place_of(item - p.whole, rest * p.parts);
+            part = at / rest;
+            number = at - part * rest;
+            locate(p.whole + number, tp, tq);
+        } else {
+            locate(place_of(item, p.whole), tp, tq);
+        }
+        const unsigned parts = split ? p.parts : 1;
         const size_t rows = DOES == Does::kDw ? p.n : p.m, cols = kFold ? p.n : p.k;
         once = static_cast<unsigned>((length(p) + kSteps - 1) / kSteps);
         const uint64_t stages = DOES == Does::kDx ? 2 * once : once;
-        begin = static_cast<unsigned>(stages * part / p.parts);
-        end = static_cast<unsigned>(stages * (part + 1) / p.parts);
+        begin = static_cast<unsigned>(stages * part / parts);
+        end = static_cast<unsigned>(stages * (part + 1) / parts);
         in_p.init(wave, lane, static_cast<unsigned>(kFold || DOES == Does::kDx ? p.ldw : p.ldx), static_cast<unsigned>(cols - col0 < S::PT ? cols - col0 : S::PT));
         in_q.init(wave, lane, static_cast<unsigned>(kFold ? p.ldx : p.ldd), static_cast<unsigned>(rows - row0 < S::QT ? rows - row0 : S::QT));
         p0 = reinterpret_cast<uint64_t>(kFold ? p.wg + col0 * p.ldw : DOES == Does::kDx ? p.wg + col0 : p.x + col0);
@@ -579,7 +592,7 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
     const unsigned base = static_cast<unsigned>(reinterpret_cast<uintptr_t>((LdsByte*)lds));
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wp = wave % S::WP, wq = wave / S::WP, r = lane & 15, quarter = lane >> 4;
-    const unsigned items = tp * tq * p.parts;
+    const unsigned items = p.whole + (tp * tq - p.whole) * p.parts;
 
     using ReadP = Reader<T, Where::kP, S::PT, S::PB, kFold>;
     using ReadQ = Reader<T, Where::kQ, S::QT, S::QB, false>;
@@ -610,7 +623,7 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
 
     Where tile;
     const auto begin = [&](unsigned item) {
-        tile.init(p, place_of(item, items), tp, tq, wave, lane);
+        tile.init(p, item, tp, tq, wave, lane);
         if (tile.begin < tile.end) tile.fetch(p, tile.begin, base);
         if (tile.begin + 1 < tile.end) tile.fetch(p, tile.begin + 1, base + S::kStage);
     };
@@ -636,34 +649,30 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
             product(kSecond);
         }
         const size_t col0 = tile.col0, row0 = tile.row0;
-        const unsigned part = tile.part;
-        const bool second = tile.second;
+        const bool second = tile.second, split = tile.split;
+        float* const sums = p.sums + (static_cast<size_t>(tile.part) * (tp * tq - p.whole) + tile.number) * (S::PT * S::QT);
         item += gridDim.x;
         if (item < items) {
             group_barrier();                     // (the reads for nothing are done)
             begin(item);
         }
 
-        const size_t row_first = row0 + wq * S::QB * 16 + r;
-        if constexpr (kFold) {
-            const size_t col = col0 + wp * 32 + quarter * 8;
-            if (p.parts > 1) {
+        const int row_in = wq * S::QB * 16 + r;
+        const size_t row_first = row0 + row_in;
+        if (split) {                             // the sums as they lie in the tile: QT rows of the reduction's PT indexes
 #pragma unroll
-                for (int j = 0; j < S::QB; ++j) {
-                    const size_t row = row_first + j * 16;
-                    if (row >= p.m || col >= p.lds) continue;
+            for (int j = 0; j < S::QB; ++j)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        *reinterpret_cast<float4v*>(p.sums + ((part * 2 + i / 2) * p.m + row) * p.lds + col + i % 2 * 4) = acc[i][j];
+                for (int i = 0; i < S::PB; ++i) {
+                    // (folded: the strip's eight columns of g, then of u)
+                    const int at = kFold ? i / 2 * (S::PT / 2) + wp * 32 + quarter * 8 + i % 2 * 4 : (wp * S::PB + i) * 16 + quarter * 4;
+                    *reinterpret_cast<float4v*>(sums + (row_in + j * 16) * S::PT + at) = acc[i][j];
                 }
-                continue;
-            }
-            finish_tile<T, DOES, S>(p, row_first, col, acc);
+        } else if constexpr (kFold) {
+            finish_tile<T, DOES, S>(p, row_first, col0 + wp * 32 + quarter * 8, acc);
         } else {
             const size_t rows = DOES == Does::kDw ? p.n : p.m;
-            constexpr int kMatrices = DOES == Does::kDw ? 2 : 1;
             T* const out = second ? p.out2 : p.out;
-            float* const sums = p.sums + (part * kMatrices + (second ? 1 : 0)) * rows * p.lds;
 #pragma unroll
             for (int j = 0; j < S::QB; ++j) {
                 const size_t row = row_first + j * 16;
@@ -671,16 +680,12 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
 #pragma unroll
                 for (int i = 0; i < S::PB; ++i) {
                     const size_t col = col0 + (wp * S::PB + i) * 16 + quarter * 4;
-                    if (p.parts > 1) {
-                        if (col < p.lds) *reinterpret_cast<float4v*>(sums + row * p.lds + col) = acc[i][j];
-                        continue;
-                    }
                     T* const at = out + row * p.ldo + col;
-                    struct alignas(4 * sizeof(T)) Four { T v[4]; } four;
+                    struct { T v[4]; } four;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) four.v[e] = static_cast<T>(acc[i][j][e]);
-                    if (p.wide && col + 4 <= p.k) {
-                        *reinterpret_cast<Four*>(at) = four;
+                    if (col + 4 <= p.k) {
+                        __builtin_memcpy(at, &four, sizeof four);
                     } else {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
@@ -697,40 +702,40 @@ template <typename T, Does DOES>
 __device__ __forceinline__ void finish_group(const GluArgs<T>& p, size_t row, size_t col, Eight& g, Eight& u) {
     const int there = columns_left(p.n, col);
     const unsigned keep = p.d.active && there > 0 ? keep_span(p.d, effective_offset(p.d), static_cast<uint64_t>(row) * p.n + col) : 0xFFu;
-    const Eight dh = DOES == Does::kSlope ? load_some(p.dh + row * p.lddh + col, there, p.wide) : Eight{};
+    const Eight dh = DOES == Does::kSlope ? load_some(p.dh + row * p.lddh + col, there) : Eight{};
     finish8<T, DOES>(p, keep, row, col, there, dh, g, u);
 }
 
-// The parts' sums joined, in the order of the parts.  A lane takes eight neighbouring columns.
-template <typename T, Does DOES>
-__global__ __launch_bounds__(256) void join_kernel(GluArgs<T> p, uint64_t total) {
-    constexpr bool kFold = DOES == Does::kForward || DOES == Does::kSlope;
-    constexpr int kMatrices = DOES == Does::kDx ? 1 : 2;
-    const uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= total) return;
-    const size_t rows = DOES == Does::kDw ? p.n : p.m, cols = kFold ? p.n : p.k;
-    const size_t width = DOES == Does::kSlope ? p.ldd : p.lds;           // dg and du are written up to their rows' ends
-    const uint64_t groups = width / 8, line = i / groups;
-    const size_t col = (i - line * groups) * 8;
-    const bool second = DOES == Does::kDw && line >= rows;
-    const size_t row = second ? line - rows : line;
-    const auto sum = [&](int matrix) {
+// The parts' sums of the tiles that are summed in parts, joined in the order of the parts.  A lane takes eight neighbouring columns.
+template <typename T, Does DOES, class S>
+__global__ __launch_bounds__(256) void join_kernel(GluArgs<T> p, unsigned tp, unsigned tq) {
+    using Where = Tile<T, DOES, S>;
+    constexpr int kGroups = Where::kCols / 8, kPerTile = S::QT * kGroups;
+    const unsigned rest = tp * tq - p.whole, i = blockIdx.x * 256 + threadIdx.x, number = i / kPerTile;
+    if (number >= rest) return;
+    const int row_in = i % kPerTile / kGroups, col_in = i % kGroups * 8;
+    Where tile;
+    tile.locate(p.whole + number, tp, tq);
+    const size_t rows = DOES == Does::kDw ? p.n : p.m, cols = Where::kFold ? p.n : p.k;
+    const size_t row = tile.row0 + row_in, col = tile.col0 + col_in;
+    if (row >= rows || col >= (DOES == Does::kSlope ? p.ldd : cols)) return;
+    const auto sum = [&](int from) {
         Eight e = {};
-        const float* at = p.sums + (matrix * rows + row) * p.lds + col;
+        const float* at = p.sums + static_cast<size_t>(number) * (S::PT * S::QT) + row_in * S::PT + from + col_in;
+        const size_t step = static_cast<size_t>(rest) * (S::PT * S::QT);
 #pragma unroll 4
-        for (unsigned part = 0; part < p.parts; ++part, at += kMatrices * rows * p.lds) {
+        for (unsigned part = 0; part < p.parts; ++part, at += step) {
             const Eight x = load8(at);
 #pragma unroll
             for (int j = 0; j < 8; ++j) e.v[j] += x.v[j];
         }
         return e;
     };
-    if constexpr (kFold) {
-        Eight g = {}, u = {};
-        if (col < p.n) g = sum(0), u = sum(1);
+    if constexpr (Where::kFold) {
+        Eight g = sum(0), u = sum(S::PT / 2);
         finish_group<T, DOES>(p, row, col, g, u);
     } else {
-        store_some((second ? p.out2 : p.out) + row * p.ldo + col, sum(second ? 1 : 0), columns_left(cols, col), p.wide);
+        store_some((tile.second ? p.out2 : p.out) + row * p.ldo + col, sum(0), columns_left(cols, col));
     }
 }
 
@@ -741,7 +746,7 @@ __global__ __launch_bounds__(256) void slope_kernel(GluArgs<T> p) {
     for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += step) {
         const size_t row = i / groups, col = (i - row * groups) * 8;
         const int there = columns_left(p.n, col);
-        Eight g = load_some(p.gate_in + row * p.ldp + col, there, p.wide), u = load_some(p.up_in + row * p.ldp + col, there, p.wide);
+        Eight g = load_some(p.gate_in + row * p.ldp + col, there), u = load_some(p.up_in + row * p.ldp + col, there);
         finish_group<T, Does::kSlope>(p, row, col, g, u);
     }
 }
@@ -802,12 +807,10 @@ zvc_status dropout_as(const void* x, size_t ldx, const void* residual, size_t ld
                       size_t cols, const Drop& d, hipStream_t stream) {
     if (ldx == cols && ldy == cols && (residual == nullptr || ldr == cols)) cols *= rows, rows = 1, ldx = ldy = ldr = cols;
     const uint64_t total = static_cast<uint64_t>(rows) * cols;
-    const bool vector = cols % 8 == 0 && aligned_to(x, 16) && aligned_to(y, 16) && aligned_to(residual, 16) &&
-                        (rows == 1 || (ldx * sizeof(T) % 16 == 0 && ldy * sizeof(T) % 16 == 0 &&
-                                       (residual == nullptr || ldr * sizeof(T) % 16 == 0)));
+    const bool whole = rows == 1 || cols % 8 == 0;
     const size_t blocks = div_up(div_up(total, 8), kDropThreads);
     if (blocks > 0x7FFFFFFF) return ZVC_E_ARG;
-    return launch(vector ? dropout_kernel<T, true> : dropout_kernel<T, false>, dim3(blocks), kDropThreads, stream,
+    return launch(whole ? dropout_kernel<T, true> : dropout_kernel<T, false>, dim3(blocks), kDropThreads, stream,
                   static_cast<const T*>(x), ldx, static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy, cols, total, d);
 }
 
@@ -822,6 +825,9 @@ using Small = Shape<2, 2, 4, 4>;                // 128 x 128, four waves
 using Thin = Shape<4, 1, 4, 2>;                 // 256 x 32, four waves: few tokens
 
 constexpr unsigned kUnits = 256;                // compute units
+constexpr double kAlone = 0.6;
+constexpr double kFp32Stage = 3.5;              // an fp32 stage against a 16-bit one: half the steps at a sixteenth of the rate
+constexpr double kJoinUs = 3, kSumsPerUs = 3e6;
 
 // Tiles of a product of this shape, by columns and rows.
 template <Does DOES, class S>
@@ -833,65 +839,72 @@ void tiles_of(size_t m, size_t n, size_t k, size_t* cols, size_t* rows) {
 
 enum class Size { kLarge, kSmall, kThin };
 
-// How a product is cut: the tiles' shape, and how many parts of the reduction are summed apart and joined.
+// How a product is cut: the tiles' shape, how many tiles are summed whole, and in how many parts of the reduction the others are,
+// to be joined by a second kernel.
 struct Cut {
     Size size;
-    unsigned parts;
+    unsigned whole, parts;
     size_t sums;                                // bytes of the parts' sums
+    double cost;
 };
+
+// The cut that takes the least time by this account, in us: workgroups take items in rounds; an item costs its stages and
+// something to begin and finish; joining costs a launch and the sums' way to memory and back.
+template <Does DOES, class S>
+void try_cut(Size size, double stage_us, double item_us, size_t m, size_t n, size_t k, size_t w, Cut* best) {
+    size_t cols, rows;
+    tiles_of<DOES, S>(m, n, k, &cols, &rows);
+    const size_t tiles = cols * rows, slots = kUnits * S::kPerUnit;
+    const size_t stages = div_up(DOES == Does::kDw ? m : DOES == Does::kDx ? 2 * n : k, kStageBytes / w);
+    if (w == 4) stage_us *= kFp32Stage;
+    const auto rounds = [&](size_t items, size_t stages_each) {
+        const size_t last = items % slots;             // alone on its compute unit, an item of two takes less time
+        const double alone = last != 0 && last <= kUnits && slots > kUnits ? kAlone : 1;
+        return items / slots * (stages_each * stage_us + item_us) + (last != 0 ? stages_each * stage_us * alone + item_us : 0);
+    };
+    const auto consider = [&](size_t whole, size_t parts) {
+        const size_t rest = tiles - whole;
+        const double sums = parts > 1 ? 4.0 * S::PT * S::QT * rest * parts : 0;
+        const double cost = rounds(whole, stages) + rounds(rest * parts, div_up(stages, parts)) + (parts > 1 ? kJoinUs + sums / kSumsPerUs : 0);
+        if (cost < best->cost) *best = {size, static_cast<unsigned>(whole), static_cast<unsigned>(parts), static_cast<size_t>(sums), cost};
+    };
+    consider(tiles, 1);
+    const size_t full = tiles / slots * slots;
+    for (size_t parts = 2; parts <= 32 && parts * 2 <= stages; ++parts)
+        if (full != tiles) consider(full, parts);
+}
 
 template <Does DOES>
 Cut cut_of(size_t m, size_t n, size_t k, size_t w) {
-    size_t cols, rows;
-    Cut cut{};
-    tiles_of<DOES, Large>(m, n, k, &cols, &rows);
-    const size_t outer = DOES == Does::kDw ? n : m;
-    size_t slots = kUnits;
-    if (cols * rows >= 192) {
-        cut.size = Size::kLarge;
-    } else if (outer > 32) {
-        cut.size = Size::kSmall, slots = 2 * kUnits;
-        tiles_of<DOES, Small>(m, n, k, &cols, &rows);
-    } else {
-        cut.size = Size::kThin, slots = 2 * kUnits;
-        tiles_of<DOES, Thin>(m, n, k, &cols, &rows);
-    }
-    // Parts of at least four stages, as many as fill the card once.
-    const size_t stages = div_up(DOES == Does::kDw ? m : DOES == Does::kDx ? 2 * n : k, kStageBytes / w);
-    const size_t tiles = cols * rows > 0 ? cols * rows : 1;
-    size_t parts = cut.size == Size::kLarge ? 1 : slots / tiles;
-    if (parts > stages / 4) parts = stages / 4;
-    cut.parts = static_cast<unsigned>(parts < 2 ? 1 : parts);
-    if (cut.parts > 1)
-        cut.sums = cut.parts * (DOES == Does::kDx ? 1 : 2) * outer * round_up(DOES == Does::kDw || DOES == Does::kDx ? k : n, 8) * 4;
-    return cut;
+    Cut best{Size::kSmall, 0, 1, 0, 1e300};
+    constexpr int kWhich = DOES == Does::kDx ? 1 : DOES == Does::kDw ? 2 : 0;
+    constexpr double kLargeStage[] = {1.45, 1.55, 1.6}, kSmallStage[] = {0.85, 1.15, 1.1}, kThinStage[] = {0.9, 0.9, 0.9};
+    if (w == 2) try_cut<DOES, Large>(Size::kLarge, kLargeStage[kWhich], 8, m, n, k, w, &best);
+    try_cut<DOES, Small>(Size::kSmall, kSmallStage[kWhich], 5, m, n, k, w, &best);
+    try_cut<DOES, Thin>(Size::kThin, kThinStage[kWhich], 4, m, n, k, w, &best);
+    return best;
 }
 
 template <typename T, Does DOES, class S>
 zvc_status product_of(const GluArgs<T>& p, hipStream_t stream) {
     size_t cols, rows;
     tiles_of<DOES, S>(p.m, p.n, p.k, &cols, &rows);
-    if (cols * rows * p.parts > 0x7FFFFFFF) return ZVC_E_ARG;
-    const size_t items = cols * rows * p.parts, room = kUnits * S::kPerUnit;
-    return launch(product_kernel<T, DOES, S>, dim3(items < room ? items : room), S::kThreads, stream, p, static_cast<unsigned>(cols),
-                  static_cast<unsigned>(rows));
+    const size_t items = p.whole + (cols * rows - p.whole) * p.parts, room = kUnits * S::kPerUnit;
+    if (items > 0x7FFFFFFF) return ZVC_E_ARG;
+    const unsigned tp = static_cast<unsigned>(cols), tq = static_cast<unsigned>(rows);
+    const zvc_status st = launch(product_kernel<T, DOES, S>, dim3(items < room ? items : room), S::kThreads, stream, p, tp, tq);
+    if (st != ZVC_OK || p.parts == 1) return st;
+    const size_t groups = (cols * rows - p.whole) * (S::QT * Tile<T, DOES, S>::kCols / 8);
+    return launch(join_kernel<T, DOES, S>, dim3(div_up(groups, 256)), 256, stream, p, tp, tq);
 }
 
 template <typename T, Does DOES>
 zvc_status product(GluArgs<T> p, float* sums, hipStream_t stream) {
     const Cut cut = cut_of<DOES>(p.m, p.n, p.k, sizeof(T));
-    p.parts = cut.parts;
-    p.sums = sums;
-    p.lds = round_up(DOES == Does::kDw || DOES == Does::kDx ? p.k : p.n, 8);
-    const zvc_status st = cut.size == Size::kLarge ? product_of<T, DOES, Large>(p, stream)
-                        : cut.size == Size::kSmall ? product_of<T, DOES, Small>(p, stream) : product_of<T, DOES, Thin>(p, stream);
-    if (st != ZVC_OK || p.parts == 1) return st;
-    if constexpr (DOES == Does::kDx || DOES == Does::kDw) {
-        const auto takes = [&](const T* at) { return at == nullptr || (aligned_to(at, 16) && p.ldo * sizeof(T) % 16 == 0); };
-        p.wide = takes(p.out) && takes(p.out2);
-    }
-    const uint64_t total = (DOES == Does::kDw ? 2 * p.n : p.m) * ((DOES == Does::kSlope ? p.ldd : p.lds) / 8);
-    return launch(join_kernel<T, DOES>, dim3(div_up(total, 256)), 256, stream, p, total);
+    p.whole = cut.whole, p.parts = cut.parts, p.sums = sums;
+    if constexpr (sizeof(T) == 2)
+        if (cut.size == Size::kLarge) return product_of<T, DOES, Large>(p, stream);
+    return cut.size == Size::kSmall ? product_of<T, DOES, Small>(p, stream) : product_of<T, DOES, Thin>(p, stream);
 }
 
 // Bytes for the sums of whichever of a call's products is cut into parts.
@@ -952,14 +965,9 @@ zvc_status align_inputs(GluArgs<T>* p, const Layout& at, unsigned char* base, hi
     return ZVC_OK;
 }
 
-// Whether rows at this address and stride take accesses of `bytes`.
-template <typename T>
-bool takes(const T* at, size_t ld, size_t bytes) { return aligned_to(at, bytes) && ld * sizeof(T) % bytes == 0; }
-
 template <typename T>
 zvc_status forward_as(GluArgs<T> p, const Layout& at, unsigned char* base, hipStream_t stream) {
     if (zvc_status st = align_inputs(&p, at, base, stream)) return st;
-    p.wide = takes(p.h, p.ldh, 16) && (p.gate == nullptr || (takes(p.gate, p.ldp, 16) && takes(p.up, p.ldp, 16)));
     return product<T, Does::kForward>(p, reinterpret_cast<float*>(base + at.sums), stream);
 }
 
@@ -970,22 +978,20 @@ zvc_status backward_as(GluArgs<T> p, T* dx, size_t lddx, T* dwg, T* dwu, size_t 
     float* const sums = reinterpret_cast<float*>(base + at.sums);
     if (p.m != 0 && p.n != 0) {
         zvc_status st;
-        p.wide = takes(p.dh, p.lddh, 16);
         if (p.gate_in == nullptr) {
             st = product<T, Does::kSlope>(p, sums, stream);
         } else {
-            p.wide = p.wide && takes(p.gate_in, p.ldp, 16) && takes(p.up_in, p.ldp, 16);
             const size_t blocks = div_up(p.m * (p.ldd / 8), 256);
             st = launch(slope_kernel<T>, dim3(blocks < 65536 ? blocks : 65536), 256, stream, p);
         }
         if (st != ZVC_OK) return st;
     }
     if (dx != nullptr && p.m != 0) {
-        p.out = dx, p.ldo = lddx, p.wide = takes(dx, lddx, 4 * sizeof(T));
+        p.out = dx, p.ldo = lddx;
         if (zvc_status st = product<T, Does::kDx>(p, sums, stream)) return st;
     }
     if (dwg == nullptr || p.n == 0) return ZVC_OK;
-    p.out = dwg, p.out2 = dwu, p.ldo = lddw, p.wide = takes(dwg, lddw, 4 * sizeof(T)) && takes(dwu, lddw, 4 * sizeof(T));
+    p.out = dwg, p.out2 = dwu, p.ldo = lddw;
     return product<T, Does::kDw>(p, sums, stream);
 }
 
