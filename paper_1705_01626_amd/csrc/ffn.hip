@@ -119,10 +119,19 @@ __device__ __forceinline__ void store8(T* at, const Eight& e) {
     }
 }
 
-// The first `there` of eight elements.
+// Zero where the mask's bit is clear, whatever is there (without a branch: an element's chain of exp and reciprocal is long, and
+// only the chains of several elements side by side hide it).
+__device__ __forceinline__ void drop8(unsigned keep, Eight& x) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        x.v[j] = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, x.v[j]) & (0u - (keep >> j & 1u)));
+}
+
+// The first `there` of eight elements; `full`: eight, in all of a wave's lanes (a branch that the wave takes as one: with masks
+// for lanes that have fewer, a tile's stores cost 3 us more).
 template <typename T>
-__device__ __forceinline__ Eight load_some(const T* at, int there) {
-    if (there >= 8) return load8(at);
+__device__ __forceinline__ Eight load_some(const T* at, int there, bool full) {
+    if (full) return load8(at);
     Eight e = {};
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -130,8 +139,8 @@ __device__ __forceinline__ Eight load_some(const T* at, int there) {
     return e;
 }
 template <typename T>
-__device__ __forceinline__ void store_some(T* at, const Eight& e, int there) {
-    if (there >= 8) return store8(at, e);
+__device__ __forceinline__ void store_some(T* at, const Eight& e, int there, bool full) {
+    if (full) return store8(at, e);
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         if (j < there) at[j] = static_cast<T>(e.v[j]);
@@ -151,15 +160,17 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const T* x, size_
     uint64_t row = first / cols, col = first - row * cols;
     if constexpr (WHOLE) {
         const int there = total - first < 8 ? static_cast<int>(total - first) : 8;
-        Eight e = load_some(x + row * ldx + col, there);
+        const bool full = __all(there == 8);
+        Eight e = load_some(x + row * ldx + col, there, full);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e.v[j] = (keep >> j & 1u) ? e.v[j] * d.scale : 0.f;
+        for (int j = 0; j < 8; ++j) e.v[j] *= d.scale;
+        drop8(keep, e);
         if (residual != nullptr) {
-            const Eight r = load_some(residual + row * ldr + col, there);
+            const Eight r = load_some(residual + row * ldr + col, there, full);
 #pragma unroll
             for (int j = 0; j < 8; ++j) e.v[j] += r.v[j];
         }
-        store_some(y + row * ldy + col, e, there);
+        store_some(y + row * ldy + col, e, there, full);
     } else {
         for (int j = 0; j < 8 && first + j < total; ++j) {
             float v = (keep >> j & 1u) ? static_cast<float>(x[row * ldx + col]) * d.scale : 0.f;
@@ -429,46 +440,53 @@ struct GluArgs {
     Drop d;
 };
 
-// Eight neighbouring columns' projections g and u, col a multiple of eight: dg and du in their place ...
+// Eight neighbouring columns' projections g and u, col a multiple of eight: dg and du in their place, before what is dropped is ...
 template <int ACT, typename T>
-__device__ __forceinline__ void slope8(const GluArgs<T>& p, unsigned keep, const Eight& dh, Eight& g, Eight& u) {
+__device__ __forceinline__ void slope8(const GluArgs<T>& p, const Eight& dh, Eight& g, Eight& u) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const ActValue a = activate<ACT, T>(g.v[j]);
-        const float d = (keep >> j & 1u) ? dh.v[j] * p.d.scale : 0.f;
+        const float d = dh.v[j] * p.d.scale;
         g.v[j] = ACT == ZVC_RELU ? (g.v[j] <= 0.f ? 0.f : d * u.v[j]) : d * u.v[j] * a.slope;
         u.v[j] = d * a.value;
     }
 }
-// ... or h, and what is kept of them in their place.
+// ... or h.
 template <int ACT, typename T>
-__device__ __forceinline__ void forward8(const GluArgs<T>& p, unsigned keep, Eight& h, Eight& g, Eight& u) {
+__device__ __forceinline__ Eight forward8(const GluArgs<T>& p, const Eight& g, const Eight& u) {
+    Eight h;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float a = activate<ACT, T>(g.v[j]).value;
-        const bool stays = keep >> j & 1u;
-        h.v[j] = stays ? a * u.v[j] * p.d.scale : 0.f;
-        if (!stays || (ACT == ZVC_RELU && g.v[j] <= 0.f)) g.v[j] = u.v[j] = 0.f;
+    for (int j = 0; j < 8; ++j) h.v[j] = activate<ACT, T>(g.v[j]).value * u.v[j] * p.d.scale;
+    return h;
+}
+
+// What is kept of them, in their place.
+template <typename T>
+__device__ __forceinline__ void kept8(const GluArgs<T>& p, unsigned keep, Eight& g, Eight& u) {
+    if (p.act == ZVC_RELU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u.v[j] = g.v[j] <= 0.f ? 0.f : u.v[j], g.v[j] = g.v[j] <= 0.f ? 0.f : g.v[j];
     }
+    if (p.d.active) drop8(keep, g), drop8(keep, u);
 }
 
 // What becomes of them in their row: `there` of them (none: dg's and du's filling) are columns.  dh: for the slope.
 template <typename T, Does DOES>
-__device__ __forceinline__ void finish8(const GluArgs<T>& p, unsigned keep, size_t row, size_t col, int there, const Eight& dh, Eight& g, Eight& u) {
+__device__ __forceinline__ void finish8(const GluArgs<T>& p, unsigned keep, size_t row, size_t col, int there, bool full, const Eight& dh, Eight& g, Eight& u) {
     if constexpr (DOES == Does::kSlope) {
-        with_activation(p.act, [&](auto act) { slope8<decltype(act)::value>(p, keep, dh, g, u); });
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j >= there) g.v[j] = u.v[j] = 0.f;
+        with_activation(p.act, [&](auto act) { slope8<decltype(act)::value>(p, dh, g, u); });
+        drop8(keep & ((1u << there) - 1u), g), drop8(keep & ((1u << there) - 1u), u);
         store8(p.dg + row * p.ldd + col, g);
         store8(p.du + row * p.ldd + col, u);
     } else {
         Eight h;
-        with_activation(p.act, [&](auto act) { forward8<decltype(act)::value>(p, keep, h, g, u); });
-        store_some(p.h + row * p.ldh + col, h, there);
+        with_activation(p.act, [&](auto act) { h = forward8<decltype(act)::value>(p, g, u); });
+        drop8(keep, h);
+        store_some(p.h + row * p.ldh + col, h, there, full);
         if (p.gate != nullptr) {
-            store_some(p.gate + row * p.ldp + col, g, there);
-            store_some(p.up + row * p.ldp + col, u, there);
+            kept8(p, keep, g, u);
+            store_some(p.gate + row * p.ldp + col, g, there, full);
+            store_some(p.up + row * p.ldp + col, u, there, full);
         }
     }
 }
@@ -479,7 +497,7 @@ __device__ __forceinline__ int columns_left(size_t n, size_t col) { return col +
 // What becomes of a lane's strip of a tile, eight columns of QB rows 16 apart: straight code, row after row (the fences keep the
 // compiler from working on all rows at once, out of registers).
 template <typename T, Does DOES, class S>
-__device__ __forceinline__ void finish_tile(const GluArgs<T>& p, size_t row, size_t col, float4v (&acc)[S::PB][S::QB]) {
+__device__ __forceinline__ void finish_tile(const GluArgs<T>& p, size_t row, size_t col, bool full, float4v (&acc)[S::PB][S::QB]) {
     static_assert(S::QB <= 8, "a bit for each of a lane's elements");
     if (col >= (DOES == Does::kSlope ? p.ldd : p.n)) return;     // (dg and du are written up to their rows' ends)
     const int there = columns_left(p.n, col);
@@ -491,21 +509,68 @@ __device__ __forceinline__ void finish_tile(const GluArgs<T>& p, size_t row, siz
         for (int j = 0; j < S::QB; ++j)
             keep |= static_cast<uint64_t>(keep_span(p.d, offset, static_cast<uint64_t>(row + j * 16) * p.n + col)) << (8 * j);
     }
-    const auto load = [&](int j) {
-        return DOES == Does::kSlope && j < S::QB && row + j * 16 < p.m ? load_some(p.dh + (row + j * 16) * p.lddh + col, there) : Eight{};
+    const auto take = [&](int j, Eight& g, Eight& u) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g.v[e] = acc[e / 4][j][e % 4], u.v[e] = acc[2 + e / 4][j][e % 4];
     };
-    Eight dh = load(0);
+    const auto keeps = [&](int j) { return static_cast<unsigned>(keep >> (8 * j)) & 0xFFu; };
+    if (!full) {                                    // (only where the columns end inside a strip)
 #pragma unroll
-    for (int j = 0; j < S::QB; ++j) {
-        const Eight next = load(j + 1);
-        if (row + j * 16 < p.m) {
-            Eight g, u;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) g.v[e] = acc[e / 4][j][e % 4], u.v[e] = acc[2 + e / 4][j][e % 4];
-            finish8<T, DOES>(p, static_cast<unsigned>(keep >> (8 * j)), row + j * 16, col, there, dh, g, u);
+        for (int j = 0; j < S::QB; ++j) {
+            if (row + j * 16 < p.m) {
+                Eight g, u;
+                take(j, g, u);
+                const Eight dh = DOES == Does::kSlope ? load_some(p.dh + (row + j * 16) * p.lddh + col, there, false) : Eight{};
+                finish8<T, DOES>(p, keeps(j), row + j * 16, col, there, false, dh, g, u);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        dh = next;
-        __builtin_amdgcn_sched_barrier(0);
+        return;
+    }
+    if constexpr (DOES == Does::kSlope) {
+        const auto load = [&](int j) { return j < S::QB && row + j * 16 < p.m ? load8(p.dh + (row + j * 16) * p.lddh + col) : Eight{}; };
+        with_activation(p.act, [&](auto act) {
+            Eight dh = load(0);
+#pragma unroll
+            for (int j = 0; j < S::QB; ++j) {
+                const Eight next = load(j + 1);
+                Eight g, u;
+                take(j, g, u);
+                slope8<decltype(act)::value>(p, dh, g, u);
+                if (p.d.active) drop8(keeps(j), g), drop8(keeps(j), u);
+                if (row + j * 16 < p.m) {
+                    store8(p.dg + (row + j * 16) * p.ldd + col, g);
+                    store8(p.du + (row + j * 16) * p.ldd + col, u);
+                }
+                dh = next;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        });
+    } else {
+        if (p.gate != nullptr) {
+#pragma unroll
+            for (int j = 0; j < S::QB; ++j) {
+                Eight g, u;
+                take(j, g, u);
+                kept8(p, keeps(j), g, u);
+                if (row + j * 16 < p.m) {
+                    store8(p.gate + (row + j * 16) * p.ldp + col, g);
+                    store8(p.up + (row + j * 16) * p.ldp + col, u);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        with_activation(p.act, [&](auto act) {
+#pragma unroll
+            for (int j = 0; j < S::QB; ++j) {
+                Eight g, u;
+                take(j, g, u);
+                Eight h = forward8<decltype(act)::value>(p, g, u);
+                if (p.d.active) drop8(keeps(j), h);
+                if (row + j * 16 < p.m) store8(p.h + (row + j * 16) * p.ldh + col, h);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        });
     }
 }
 
@@ -559,9 +624,10 @@ struct Tile {
         const unsigned parts = split ? p.parts : 1;
         const size_t rows = DOES == Does::kDw ? p.n : p.m, cols = kFold ? p.n : p.k;
         once = static_cast<unsigned>((length(p) + kSteps - 1) / kSteps);
-        const uint64_t stages = DOES == Does::kDx ? 2 * once : once;
-        begin = static_cast<unsigned>(stages * part / parts);
-        end = static_cast<unsigned>(stages * (part + 1) / parts);
+        // (parts differ by a stage at most)
+        const unsigned stages = DOES == Does::kDx ? 2 * once : once, each = split ? stages / p.parts : stages, longer = stages - each * parts;
+        begin = part * each + (part < longer ? part : longer);
+        end = begin + each + (part < longer ? 1 : 0);
         in_p.init(wave, lane, static_cast<unsigned>(kFold || DOES == Does::kDx ? p.ldw : p.ldx), static_cast<unsigned>(cols - col0 < S::PT ? cols - col0 : S::PT));
         in_q.init(wave, lane, static_cast<unsigned>(kFold ? p.ldx : p.ldd), static_cast<unsigned>(rows - row0 < S::QT ? rows - row0 : S::QT));
         p0 = reinterpret_cast<uint64_t>(kFold ? p.wg + col0 * p.ldw : DOES == Does::kDx ? p.wg + col0 : p.x + col0);
@@ -669,10 +735,11 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
                     *reinterpret_cast<float4v*>(sums + (row_in + j * 16) * S::PT + at) = acc[i][j];
                 }
         } else if constexpr (kFold) {
-            finish_tile<T, DOES, S>(p, row_first, col0 + wp * 32 + quarter * 8, acc);
+            finish_tile<T, DOES, S>(p, row_first, col0 + wp * 32 + quarter * 8, col0 + wp * 32 + 32 <= p.n, acc);
         } else {
             const size_t rows = DOES == Does::kDw ? p.n : p.m;
             T* const out = second ? p.out2 : p.out;
+            const bool full = col0 + (wp + 1) * S::PB * 16 <= p.k;
 #pragma unroll
             for (int j = 0; j < S::QB; ++j) {
                 const size_t row = row_first + j * 16;
@@ -684,7 +751,7 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
                     struct { T v[4]; } four;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) four.v[e] = static_cast<T>(acc[i][j][e]);
-                    if (col + 4 <= p.k) {
+                    if (full) {
                         __builtin_memcpy(at, &four, sizeof four);
                     } else {
 #pragma unroll
@@ -702,8 +769,9 @@ template <typename T, Does DOES>
 __device__ __forceinline__ void finish_group(const GluArgs<T>& p, size_t row, size_t col, Eight& g, Eight& u) {
     const int there = columns_left(p.n, col);
     const unsigned keep = p.d.active && there > 0 ? keep_span(p.d, effective_offset(p.d), static_cast<uint64_t>(row) * p.n + col) : 0xFFu;
-    const Eight dh = DOES == Does::kSlope ? load_some(p.dh + row * p.lddh + col, there) : Eight{};
-    finish8<T, DOES>(p, keep, row, col, there, dh, g, u);
+    const bool full = __all(there == 8);
+    const Eight dh = DOES == Does::kSlope ? load_some(p.dh + row * p.lddh + col, there, full) : Eight{};
+    finish8<T, DOES>(p, keep, row, col, there, full, dh, g, u);
 }
 
 // The parts' sums of the tiles that are summed in parts, joined in the order of the parts.  A lane takes eight neighbouring columns.
@@ -735,7 +803,8 @@ __global__ __launch_bounds__(256) void join_kernel(GluArgs<T> p, unsigned tp, un
         Eight g = sum(0), u = sum(S::PT / 2);
         finish_group<T, DOES>(p, row, col, g, u);
     } else {
-        store_some((tile.second ? p.out2 : p.out) + row * p.ldo + col, sum(0), columns_left(cols, col));
+        const int there = columns_left(cols, col);
+        store_some((tile.second ? p.out2 : p.out) + row * p.ldo + col, sum(0), there, __all(there == 8));
     }
 }
 
@@ -746,7 +815,8 @@ __global__ __launch_bounds__(256) void slope_kernel(GluArgs<T> p) {
     for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += step) {
         const size_t row = i / groups, col = (i - row * groups) * 8;
         const int there = columns_left(p.n, col);
-        Eight g = load_some(p.gate_in + row * p.ldp + col, there), u = load_some(p.up_in + row * p.ldp + col, there);
+        const bool full = __all(there == 8);
+        Eight g = load_some(p.gate_in + row * p.ldp + col, there, full), u = load_some(p.up_in + row * p.ldp + col, there, full);
         finish_group<T, Does::kSlope>(p, row, col, g, u);
     }
 }
