@@ -740,23 +740,37 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
             const size_t rows = DOES == Does::kDw ? p.n : p.m;
             T* const out = second ? p.out2 : p.out;
             const bool full = col0 + (wp + 1) * S::PB * 16 <= p.k;
+            const size_t col = col0 + wp * S::PB * 16 + quarter * 4;
+            struct Four { T v[4]; };
+            const auto four = [&](int i, int j) {
+                Four f;
 #pragma unroll
-            for (int j = 0; j < S::QB; ++j) {
-                const size_t row = row_first + j * 16;
-                if (row >= rows) continue;
+                for (int e = 0; e < 4; ++e) f.v[e] = static_cast<T>(acc[i][j][e]);
+                return f;
+            };
+            if (full) {
 #pragma unroll
-                for (int i = 0; i < S::PB; ++i) {
-                    const size_t col = col0 + (wp * S::PB + i) * 16 + quarter * 4;
-                    T* const at = out + row * p.ldo + col;
-                    struct { T v[4]; } four;
+                for (int j = 0; j < S::QB; ++j) {
+                    T* const at = out + (row_first + j * 16) * p.ldo + col;
+                    if (row_first + j * 16 < rows) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) four.v[e] = static_cast<T>(acc[i][j][e]);
-                    if (full) {
-                        __builtin_memcpy(at, &four, sizeof four);
-                    } else {
+                        for (int i = 0; i < S::PB; ++i) {
+                            const Four f = four(i, j);
+                            __builtin_memcpy(at + i * 16, &f, sizeof f);
+                        }
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < S::QB; ++j) {
+                    T* const at = out + (row_first + j * 16) * p.ldo + col;
+                    if (row_first + j * 16 >= rows) continue;
+#pragma unroll
+                    for (int i = 0; i < S::PB; ++i) {
+                        const Four f = four(i, j);
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (col + e < p.k) at[e] = four.v[e];
+                            if (col + i * 16 + e < p.k) at[i * 16 + e] = f.v[e];
                     }
                 }
             }
