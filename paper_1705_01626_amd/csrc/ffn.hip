@@ -119,6 +119,9 @@ __device__ __forceinline__ void store8(T* at, const Eight& e) {
     }
 }
 
+template <typename T>
+__device__ __forceinline__ T* cell(T* at, unsigned row, unsigned ld, unsigned col) { return at + (static_cast<uint64_t>(row) * ld + col); }
+
 // Zero where the mask's bit is clear, whatever is there (without a branch: an element's chain of exp and reciprocal is long, and
 // only the chains of several elements side by side hide it).
 __device__ __forceinline__ void drop8(unsigned keep, Eight& x) {
@@ -356,7 +359,7 @@ struct Operand {
         return LIES == Lies::kAlong ? logical(row) / W < left : row < left;
     }
     // Stage: `left` of the reduction remain at `base` (FOLD: at `base` for Wg's rows, at `other` for Wu's).
-    __device__ __forceinline__ void fetch(uint64_t base, uint64_t other, int64_t left, unsigned lds) const {
+    __device__ __forceinline__ void fetch(uint64_t base, uint64_t other, int left, unsigned lds) const {
         constexpr int kRun = 32 / kRowsPerLoad;             // loads that bring 32 rows
         const bool odd = FOLD && kLoads == kRun && (first / kRun & 1);
         const int4v buffers[] = {buffer_at(odd ? other : base), buffer_at(other)};
@@ -367,7 +370,7 @@ struct Operand {
         } else {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
-                load_to_lds(from(i), within(i, static_cast<int>(left)) ? offset[i] : kNowhere, lds + (first + i) * 1024);
+                load_to_lds(from(i), within(i, left) ? offset[i] : kNowhere, lds + (first + i) * 1024);
         }
     }
 };
@@ -433,7 +436,7 @@ struct GluArgs {
     const T *gate_in, *up_in;
     T *h, *gate, *up, *dg, *du;
     T *out, *out2;                      // dx; dwg and dwu
-    size_t ldx, ldw, lddh, ldh, ldp, ldd, ldo, m, n, k;
+    unsigned ldx, ldw, lddh, ldh, ldp, ldd, ldo, m, n, k;   // (32 bits hold them: scalar registers are short)
     int act;
     float* sums;                        // parts' sums, to be joined: part by part, tile by tile as they lie in it
     unsigned whole, parts;              // the tiles behind the first `whole` are summed in parts of the reduction
@@ -472,32 +475,32 @@ __device__ __forceinline__ void kept8(const GluArgs<T>& p, unsigned keep, Eight&
 
 // What becomes of them in their row: `there` of them (none: dg's and du's filling) are columns.  dh: for the slope.
 template <typename T, Does DOES>
-__device__ __forceinline__ void finish8(const GluArgs<T>& p, unsigned keep, size_t row, size_t col, int there, bool full, const Eight& dh, Eight& g, Eight& u) {
+__device__ __forceinline__ void finish8(const GluArgs<T>& p, unsigned keep, unsigned row, unsigned col, int there, bool full, const Eight& dh, Eight& g, Eight& u) {
     if constexpr (DOES == Does::kSlope) {
         with_activation(p.act, [&](auto act) { slope8<decltype(act)::value>(p, dh, g, u); });
         drop8(keep & ((1u << there) - 1u), g), drop8(keep & ((1u << there) - 1u), u);
-        store8(p.dg + row * p.ldd + col, g);
-        store8(p.du + row * p.ldd + col, u);
+        store8(cell(p.dg, row, p.ldd, col), g);
+        store8(cell(p.du, row, p.ldd, col), u);
     } else {
         Eight h;
         with_activation(p.act, [&](auto act) { h = forward8<decltype(act)::value>(p, g, u); });
         drop8(keep, h);
-        store_some(p.h + row * p.ldh + col, h, there, full);
+        store_some(cell(p.h, row, p.ldh, col), h, there, full);
         if (p.gate != nullptr) {
             kept8(p, keep, g, u);
-            store_some(p.gate + row * p.ldp + col, g, there, full);
-            store_some(p.up + row * p.ldp + col, u, there, full);
+            store_some(cell(p.gate, row, p.ldp, col), g, there, full);
+            store_some(cell(p.up, row, p.ldp, col), u, there, full);
         }
     }
 }
 
 // How many of eight columns from `col` on there are.
-__device__ __forceinline__ int columns_left(size_t n, size_t col) { return col + 8 <= n ? 8 : col < n ? static_cast<int>(n - col) : 0; }
+__device__ __forceinline__ int columns_left(unsigned n, unsigned col) { return col + 8 <= n ? 8 : col < n ? static_cast<int>(n - col) : 0; }
 
 // What becomes of a lane's strip of a tile, eight columns of QB rows 16 apart: straight code, row after row (the fences keep the
 // compiler from working on all rows at once, out of registers).
 template <typename T, Does DOES, class S>
-__device__ __forceinline__ void finish_tile(const GluArgs<T>& p, size_t row, size_t col, bool full, float4v (&acc)[S::PB][S::QB]) {
+__device__ __forceinline__ void finish_tile(const GluArgs<T>& p, unsigned row, unsigned col, bool full, float4v (&acc)[S::PB][S::QB]) {
     static_assert(S::QB <= 8, "a bit for each of a lane's elements");
     if (col >= (DOES == Does::kSlope ? p.ldd : p.n)) return;     // (dg and du are written up to their rows' ends)
     const int there = columns_left(p.n, col);
@@ -520,7 +523,7 @@ __device__ __forceinline__ void finish_tile(const GluArgs<T>& p, size_t row, siz
             if (row + j * 16 < p.m) {
                 Eight g, u;
                 take(j, g, u);
-                const Eight dh = DOES == Does::kSlope ? load_some(p.dh + (row + j * 16) * p.lddh + col, there, false) : Eight{};
+                const Eight dh = DOES == Does::kSlope ? load_some(cell(p.dh, row + j * 16, p.lddh, col), there, false) : Eight{};
                 finish8<T, DOES>(p, keeps(j), row + j * 16, col, there, false, dh, g, u);
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -528,7 +531,7 @@ __device__ __forceinline__ void finish_tile(const GluArgs<T>& p, size_t row, siz
         return;
     }
     if constexpr (DOES == Does::kSlope) {
-        const auto load = [&](int j) { return j < S::QB && row + j * 16 < p.m ? load8(p.dh + (row + j * 16) * p.lddh + col) : Eight{}; };
+        const auto load = [&](int j) { return j < S::QB && row + j * 16 < p.m ? load8(cell(p.dh, row + j * 16, p.lddh, col)) : Eight{}; };
         with_activation(p.act, [&](auto act) {
             Eight dh = load(0);
 #pragma unroll
@@ -539,8 +542,8 @@ __device__ __forceinline__ void finish_tile(const GluArgs<T>& p, size_t row, siz
                 slope8<decltype(act)::value>(p, dh, g, u);
                 if (p.d.active) drop8(keeps(j), g), drop8(keeps(j), u);
                 if (row + j * 16 < p.m) {
-                    store8(p.dg + (row + j * 16) * p.ldd + col, g);
-                    store8(p.du + (row + j * 16) * p.ldd + col, u);
+                    store8(cell(p.dg, row + j * 16, p.ldd, col), g);
+                    store8(cell(p.du, row + j * 16, p.ldd, col), u);
                 }
                 dh = next;
                 __builtin_amdgcn_sched_barrier(0);
@@ -554,8 +557,8 @@ __device__ __forceinline__ void finish_tile(const GluArgs<T>& p, size_t row, siz
                 take(j, g, u);
                 kept8(p, keeps(j), g, u);
                 if (row + j * 16 < p.m) {
-                    store8(p.gate + (row + j * 16) * p.ldp + col, g);
-                    store8(p.up + (row + j * 16) * p.ldp + col, u);
+                    store8(cell(p.gate, row + j * 16, p.ldp, col), g);
+                    store8(cell(p.up, row + j * 16, p.ldp, col), u);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -567,7 +570,7 @@ __device__ __forceinline__ void finish_tile(const GluArgs<T>& p, size_t row, siz
                 take(j, g, u);
                 Eight h = forward8<decltype(act)::value>(p, g, u);
                 if (p.d.active) drop8(keeps(j), h);
-                if (row + j * 16 < p.m) store8(p.h + (row + j * 16) * p.ldh + col, h);
+                if (row + j * 16 < p.m) store8(cell(p.h, row + j * 16, p.ldh, col), h);
                 __builtin_amdgcn_sched_barrier(0);
             }
         });
@@ -593,7 +596,7 @@ struct Tile {
     static_assert(!kFold || InP::kLoads * InP::kRowsPerLoad == 32 || InP::kLoads * InP::kRowsPerLoad == 64, "whole runs of one weight's rows");
     static_assert(!kFold || S::PB == 4, "a wave's strip is 32 rows of each weight");
 
-    size_t col0, row0;
+    unsigned col0, row0;
     bool second, split;                             // dW: of dWu; summed in parts
     unsigned number, part;                          // of the split tiles; of its reduction
     unsigned begin, end, once;                      // stages; dx: the first `once` are Wg's
@@ -605,9 +608,9 @@ struct Tile {
     __device__ __forceinline__ void locate(unsigned at, unsigned tp, unsigned tq) {
         const unsigned band = at / (8 * tp), in_band = at % (8 * tp), height = tq - band * 8 < 8 ? tq - band * 8 : 8;
         const unsigned tile_q = band * 8 + in_band % height, halves = tq / 2;
-        col0 = static_cast<size_t>(in_band / height) * kCols;
+        col0 = in_band / height * kCols;
         second = DOES == Does::kDw && tile_q >= halves;
-        row0 = static_cast<size_t>(second ? tile_q - halves : tile_q) * S::QT;
+        row0 = (second ? tile_q - halves : tile_q) * S::QT;
     }
     __device__ __forceinline__ void init(const GluArgs<T>& p, unsigned item, unsigned tp, unsigned tq, int wave, int lane) {
         const unsigned rest = tp * tq - p.whole;
@@ -622,30 +625,30 @@ struct Tile {
             locate(place_of(item, p.whole), tp, tq);
         }
         const unsigned parts = split ? p.parts : 1;
-        const size_t rows = DOES == Does::kDw ? p.n : p.m, cols = kFold ? p.n : p.k;
-        once = static_cast<unsigned>((length(p) + kSteps - 1) / kSteps);
+        const unsigned rows = DOES == Does::kDw ? p.n : p.m, cols = kFold ? p.n : p.k;
+        once = (length(p) + kSteps - 1) / kSteps;
         // (parts differ by a stage at most)
         const unsigned stages = DOES == Does::kDx ? 2 * once : once, each = split ? stages / p.parts : stages, longer = stages - each * parts;
         begin = part * each + (part < longer ? part : longer);
         end = begin + each + (part < longer ? 1 : 0);
-        in_p.init(wave, lane, static_cast<unsigned>(kFold || DOES == Does::kDx ? p.ldw : p.ldx), static_cast<unsigned>(cols - col0 < S::PT ? cols - col0 : S::PT));
-        in_q.init(wave, lane, static_cast<unsigned>(kFold ? p.ldx : p.ldd), static_cast<unsigned>(rows - row0 < S::QT ? rows - row0 : S::QT));
-        p0 = reinterpret_cast<uint64_t>(kFold ? p.wg + col0 * p.ldw : DOES == Does::kDx ? p.wg + col0 : p.x + col0);
-        p1 = reinterpret_cast<uint64_t>(kFold ? p.wu + col0 * p.ldw : p.wu + col0);
-        q0 = reinterpret_cast<uint64_t>(kFold ? p.x + row0 * p.ldx : DOES == Does::kDx ? p.dg + row0 * p.ldd : (second ? p.du : p.dg) + row0);
-        q1 = reinterpret_cast<uint64_t>(p.du + row0 * p.ldd);
+        in_p.init(wave, lane, kFold || DOES == Does::kDx ? p.ldw : p.ldx, cols - col0 < S::PT ? cols - col0 : S::PT);
+        in_q.init(wave, lane, kFold ? p.ldx : p.ldd, rows - row0 < S::QT ? rows - row0 : S::QT);
+        p0 = reinterpret_cast<uint64_t>(kFold ? cell(p.wg, col0, p.ldw, 0) : DOES == Does::kDx ? p.wg + col0 : p.x + col0);
+        p1 = reinterpret_cast<uint64_t>(kFold ? cell(p.wu, col0, p.ldw, 0) : p.wu + col0);
+        q0 = reinterpret_cast<uint64_t>(kFold ? cell(p.x, row0, p.ldx, 0) : DOES == Does::kDx ? cell(p.dg, row0, p.ldd, 0) : (second ? p.du : p.dg) + row0);
+        q1 = reinterpret_cast<uint64_t>(cell(p.du, row0, p.ldd, 0));
     }
-    static __device__ __forceinline__ size_t length(const GluArgs<T>& p) { return kFold ? p.k : DOES == Does::kDx ? p.n : p.m; }
+    static __device__ __forceinline__ unsigned length(const GluArgs<T>& p) { return kFold ? p.k : DOES == Does::kDx ? p.n : p.m; }
 
     __device__ __forceinline__ void fetch(const GluArgs<T>& p, unsigned s, unsigned lds) const {
-        const uint64_t step_p = kFold ? kStageBytes : kSteps * W * (DOES == Does::kDx ? p.ldw : p.ldx);
-        const uint64_t step_q = DOES == Does::kDw ? kSteps * W * p.ldd : kStageBytes;
+        const unsigned step_p = kFold ? kStageBytes : kSteps * W * (DOES == Does::kDx ? p.ldw : p.ldx);
+        const unsigned step_q = DOES == Does::kDw ? kSteps * W * p.ldd : kStageBytes;
         const bool late = DOES == Does::kDx && s >= once;
         const unsigned t = late ? s - once : s;
-        const int64_t left = static_cast<int64_t>(length(p)) - static_cast<int64_t>(t) * kSteps;
-        in_p.fetch((late ? p1 : p0) + t * step_p, p1 + t * step_p, left, lds);
+        const int left = static_cast<int>(length(p) - t * kSteps);
+        in_p.fetch((late ? p1 : p0) + static_cast<uint64_t>(t) * step_p, p1 + static_cast<uint64_t>(t) * step_p, left, lds);
         // (dx: the columns of dg and du behind the last are zeros, up to a whole stage)
-        in_q.fetch((late ? q1 : q0) + t * step_q, 0, DOES == Does::kDx ? kSteps : left, lds + S::PT * kStageBytes);
+        in_q.fetch((late ? q1 : q0) + static_cast<uint64_t>(t) * step_q, 0, DOES == Does::kDx ? kSteps : left, lds + S::PT * kStageBytes);
     }
 };
 
@@ -714,7 +717,7 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
             read(kFirst, S::kStage - even);      // (behind the last stage: what the buffer held, for nothing)
             product(kSecond);
         }
-        const size_t col0 = tile.col0, row0 = tile.row0;
+        const unsigned col0 = tile.col0, row0 = tile.row0;
         const bool second = tile.second, split = tile.split;
         float* const sums = p.sums + (static_cast<size_t>(tile.part) * (tp * tq - p.whole) + tile.number) * (S::PT * S::QT);
         item += gridDim.x;
@@ -724,7 +727,7 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
         }
 
         const int row_in = wq * S::QB * 16 + r;
-        const size_t row_first = row0 + row_in;
+        const unsigned row_first = row0 + row_in;
         if (split) {                             // the sums as they lie in the tile: QT rows of the reduction's PT indexes
 #pragma unroll
             for (int j = 0; j < S::QB; ++j)
@@ -737,10 +740,10 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
         } else if constexpr (kFold) {
             finish_tile<T, DOES, S>(p, row_first, col0 + wp * 32 + quarter * 8, col0 + wp * 32 + 32 <= p.n, acc);
         } else {
-            const size_t rows = DOES == Does::kDw ? p.n : p.m;
+            const unsigned rows = DOES == Does::kDw ? p.n : p.m;
             T* const out = second ? p.out2 : p.out;
             const bool full = col0 + (wp + 1) * S::PB * 16 <= p.k;
-            const size_t col = col0 + wp * S::PB * 16 + quarter * 4;
+            const unsigned col = col0 + wp * S::PB * 16 + quarter * 4;
             struct Four { T v[4]; };
             const auto four = [&](int i, int j) {
                 Four f;
@@ -751,7 +754,7 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
             if (full) {
 #pragma unroll
                 for (int j = 0; j < S::QB; ++j) {
-                    T* const at = out + (row_first + j * 16) * p.ldo + col;
+                    T* const at = cell(out, row_first + j * 16, p.ldo, col);
                     if (row_first + j * 16 < rows) {
 #pragma unroll
                         for (int i = 0; i < S::PB; ++i) {
@@ -763,7 +766,7 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
             } else {
 #pragma unroll
                 for (int j = 0; j < S::QB; ++j) {
-                    T* const at = out + (row_first + j * 16) * p.ldo + col;
+                    T* const at = cell(out, row_first + j * 16, p.ldo, col);
                     if (row_first + j * 16 >= rows) continue;
 #pragma unroll
                     for (int i = 0; i < S::PB; ++i) {
@@ -780,11 +783,11 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
 
 // The same for one group of eight columns, outside a tile.
 template <typename T, Does DOES>
-__device__ __forceinline__ void finish_group(const GluArgs<T>& p, size_t row, size_t col, Eight& g, Eight& u) {
+__device__ __forceinline__ void finish_group(const GluArgs<T>& p, unsigned row, unsigned col, Eight& g, Eight& u) {
     const int there = columns_left(p.n, col);
     const unsigned keep = p.d.active && there > 0 ? keep_span(p.d, effective_offset(p.d), static_cast<uint64_t>(row) * p.n + col) : 0xFFu;
     const bool full = __all(there == 8);
-    const Eight dh = DOES == Does::kSlope ? load_some(p.dh + row * p.lddh + col, there, full) : Eight{};
+    const Eight dh = DOES == Does::kSlope ? load_some(cell(p.dh, row, p.lddh, col), there, full) : Eight{};
     finish8<T, DOES>(p, keep, row, col, there, full, dh, g, u);
 }
 
@@ -798,8 +801,8 @@ __global__ __launch_bounds__(256) void join_kernel(GluArgs<T> p, unsigned tp, un
     const int row_in = i % kPerTile / kGroups, col_in = i % kGroups * 8;
     Where tile;
     tile.locate(p.whole + number, tp, tq);
-    const size_t rows = DOES == Does::kDw ? p.n : p.m, cols = Where::kFold ? p.n : p.k;
-    const size_t row = tile.row0 + row_in, col = tile.col0 + col_in;
+    const unsigned rows = DOES == Does::kDw ? p.n : p.m, cols = Where::kFold ? p.n : p.k;
+    const unsigned row = tile.row0 + row_in, col = tile.col0 + col_in;
     if (row >= rows || col >= (DOES == Does::kSlope ? p.ldd : cols)) return;
     const auto sum = [&](int from) {
         Eight e = {};
@@ -818,19 +821,20 @@ __global__ __launch_bounds__(256) void join_kernel(GluArgs<T> p, unsigned tp, un
         finish_group<T, DOES>(p, row, col, g, u);
     } else {
         const int there = columns_left(cols, col);
-        store_some((tile.second ? p.out2 : p.out) + row * p.ldo + col, sum(0), there, __all(there == 8));
+        store_some(cell(tile.second ? p.out2 : p.out, row, p.ldo, col), sum(0), there, __all(there == 8));
     }
 }
 
 // dg and du from kept projections; their rows are filled with zeros up to ldd.
 template <typename T>
 __global__ __launch_bounds__(256) void slope_kernel(GluArgs<T> p) {
-    const uint64_t groups = p.ldd / 8, total = groups * p.m, step = static_cast<uint64_t>(gridDim.x) * 256;
+    const unsigned groups = p.ldd / 8;
+    const uint64_t total = static_cast<uint64_t>(groups) * p.m, step = static_cast<uint64_t>(gridDim.x) * 256;
     for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += step) {
-        const size_t row = i / groups, col = (i - row * groups) * 8;
+        const unsigned row = static_cast<unsigned>(i / groups), col = static_cast<unsigned>(i - static_cast<uint64_t>(row) * groups) * 8;
         const int there = columns_left(p.n, col);
         const bool full = __all(there == 8);
-        Eight g = load_some(p.gate_in + row * p.ldp + col, there, full), u = load_some(p.up_in + row * p.ldp + col, there, full);
+        Eight g = load_some(cell(p.gate_in, row, p.ldp, col), there, full), u = load_some(cell(p.up_in, row, p.ldp, col), there, full);
         finish_group<T, Does::kSlope>(p, row, col, g, u);
     }
 }
@@ -900,6 +904,13 @@ zvc_status dropout_as(const void* x, size_t ldx, const void* residual, size_t ld
 
 bool sizes_ok(size_t m, size_t n, size_t k) {
     return m <= ZVC_FFN_MAX_ROWS && n <= ZVC_FFN_MAX_COLUMNS && k <= ZVC_FFN_MAX_COLUMNS;
+}
+
+template <typename T>
+void set_sizes(GluArgs<T>* p, size_t ldx, size_t ldw, size_t ldp, size_t m, size_t n, size_t k, int activation, const Drop& d) {
+    p->ldx = static_cast<unsigned>(ldx), p->ldw = static_cast<unsigned>(ldw), p->ldp = static_cast<unsigned>(ldp);
+    p->m = static_cast<unsigned>(m), p->n = static_cast<unsigned>(n), p->k = static_cast<unsigned>(k);
+    p->act = activation, p->d = d;
 }
 
 bool stride_ok(size_t ld, size_t cols) { return ld >= cols && ld <= ZVC_FFN_MAX_COLUMNS; }
@@ -1028,21 +1039,21 @@ Layout layout_of(size_t m, size_t n, size_t k, size_t w, bool backward, bool cop
 // Copies of x and the weights where they do not take 16-byte accesses as they lie.
 template <typename T>
 zvc_status align_inputs(GluArgs<T>* p, const Layout& at, unsigned char* base, hipStream_t stream) {
-    const auto copy = [&](const T** from, size_t* ld, size_t rows, size_t to) {
+    const auto copy = [&](const T** from, unsigned* ld, size_t rows, size_t to) {
         if (rows == 0 || p->k == 0) return ZVC_OK;
         T* const out = reinterpret_cast<T*>(base + to);
         const size_t blocks = div_up(rows * at.aligned_k * sizeof(T) / 16, 256);
-        const zvc_status st = launch(align_kernel<T>, dim3(blocks < 65536 ? blocks : 65536), 256, stream, *from, *ld, out,
-                                     at.aligned_k, rows, p->k);
+        const zvc_status st = launch(align_kernel<T>, dim3(blocks < 65536 ? blocks : 65536), 256, stream, *from, size_t{*ld}, out,
+                                     at.aligned_k, rows, size_t{p->k});
         *from = out;
-        *ld = at.aligned_k;
+        *ld = static_cast<unsigned>(at.aligned_k);
         return st;
     };
     const bool odd = p->k * sizeof(T) % 16 != 0;
     if (odd || !aligned_to(p->x, 16) || p->ldx * sizeof(T) % 16 != 0)
         if (zvc_status st = copy(&p->x, &p->ldx, p->m, at.x)) return st;
     if (odd || !aligned_to(p->wg, 16) || !aligned_to(p->wu, 16) || p->ldw * sizeof(T) % 16 != 0) {
-        size_t ld = p->ldw;
+        unsigned ld = p->ldw;
         if (zvc_status st = copy(&p->wg, &ld, p->n, at.wg)) return st;
         return copy(&p->wu, &p->ldw, p->n, at.wu);
     }
@@ -1065,17 +1076,17 @@ zvc_status backward_as(GluArgs<T> p, T* dx, size_t lddx, T* dwg, T* dwu, size_t 
         if (p.gate_in == nullptr) {
             st = product<T, Does::kSlope>(p, sums, stream);
         } else {
-            const size_t blocks = div_up(p.m * (p.ldd / 8), 256);
+            const size_t blocks = div_up(size_t{p.m} * (p.ldd / 8), 256);
             st = launch(slope_kernel<T>, dim3(blocks < 65536 ? blocks : 65536), 256, stream, p);
         }
         if (st != ZVC_OK) return st;
     }
     if (dx != nullptr && p.m != 0) {
-        p.out = dx, p.ldo = lddx;
+        p.out = dx, p.ldo = static_cast<unsigned>(lddx);
         if (zvc_status st = product<T, Does::kDx>(p, sums, stream)) return st;
     }
     if (dwg == nullptr || p.n == 0) return ZVC_OK;
-    p.out = dwg, p.out2 = dwu, p.ldo = lddw;
+    p.out = dwg, p.out2 = dwu, p.ldo = static_cast<unsigned>(lddw);
     return product<T, Does::kDw>(p, sums, stream);
 }
 
@@ -1151,7 +1162,8 @@ zvc_status zvc_glu_forward(const void* d_x, size_t ldx, const void* d_wg, const 
         GluArgs<T> p{};
         p.x = static_cast<const T*>(d_x), p.wg = static_cast<const T*>(d_wg), p.wu = static_cast<const T*>(d_wu);
         p.h = static_cast<T*>(d_h), p.gate = static_cast<T*>(d_gate), p.up = static_cast<T*>(d_up);
-        p.ldx = ldx, p.ldw = ldw, p.ldh = ldh, p.ldp = ldp, p.m = m, p.n = n, p.k = k, p.act = activation, p.d = d;
+        set_sizes(&p, ldx, ldw, ldp, m, n, k, activation, d);
+        p.ldh = static_cast<unsigned>(ldh);
         return forward_as(p, at, static_cast<unsigned char*>(d_ws), stream);
     };
     return type == ZVC_FP32 ? as(0.f) : type == ZVC_FP16 ? as(fp16{}) : as(bf16{});
@@ -1196,7 +1208,8 @@ zvc_status zvc_glu_backward(const void* d_dh, size_t lddh, const void* d_x, size
         p.x = static_cast<const T*>(d_x), p.wg = static_cast<const T*>(d_wg), p.wu = static_cast<const T*>(d_wu);
         p.dh = static_cast<const T*>(d_dh), p.gate_in = static_cast<const T*>(d_gate), p.up_in = static_cast<const T*>(d_up);
         p.dg = reinterpret_cast<T*>(base + at.dg), p.du = reinterpret_cast<T*>(base + at.du);
-        p.ldx = ldx, p.ldw = ldw, p.lddh = lddh, p.ldp = ldp, p.ldd = at.ldd, p.m = m, p.n = n, p.k = k, p.act = activation, p.d = d;
+        set_sizes(&p, ldx, ldw, ldp, m, n, k, activation, d);
+        p.lddh = static_cast<unsigned>(lddh), p.ldd = static_cast<unsigned>(at.ldd);
         return backward_as(p, static_cast<T*>(d_dx), lddx, static_cast<T*>(d_dwg), static_cast<T*>(d_dwu), lddw, at, base, stream);
     };
     return type == ZVC_FP32 ? as(0.f) : type == ZVC_FP16 ? as(fp16{}) : as(bf16{});
