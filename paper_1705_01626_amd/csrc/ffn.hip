@@ -791,6 +791,91 @@ __device__ __forceinline__ void finish_group(const GluArgs<T>& p, unsigned row, 
     finish8<T, DOES>(p, keep, row, col, there, full, dh, g, u);
 }
 
+// ------------------------------------------------------------------ few tokens
+// The projections of up to 16 TB tokens.  Every weight is read once and used for all of them, so this is a matter of reading the
+// weights: straight into registers, 128 neighbouring bytes of 32 rows at a time and wave.  A workgroup takes 16 columns of both
+// weights, its WAVES waves take turns along k and their sums meet in LDS.  Workgroups begin at different places along k:
+// rows lie a power of two apart, and the same place in all of them is in few of the memory's channels.
+template <typename T, Does DOES, int TB, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void token_kernel(GluArgs<T> p) {
+    constexpr int W = sizeof(T), kChunk = 16 / W, kSpan = 128 / W;       // elements of 16 and of 128 bytes
+    constexpr int kBatch = TB == 1 ? 4 : 2;                              // spans on their way together
+    constexpr int kCols = 16, kFrom = 2 + TB;
+    using Frag = typename Fragment<T>::type;
+    __shared__ float4v sums[WAVES][2][TB * 16][kCols / 4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, quarter = lane >> 4;
+    const unsigned col0 = blockIdx.x * kCols;
+    // (rows and tokens that are not there: the last one again, and what comes of it is left out)
+    const unsigned row = col0 + r < p.n ? col0 + r : p.n - 1;
+    const T* from[kFrom] = {cell(p.wg, row, p.ldw, quarter * kChunk), cell(p.wu, row, p.ldw, quarter * kChunk)};
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+        const unsigned at = t * 16 + r, token = at < p.m ? at : p.m - 1;
+        from[2 + t] = cell(p.x, token, p.ldx, quarter * kChunk);
+    }
+    float4v acc[2][TB];
+#pragma unroll
+    for (int t = 0; t < TB; ++t) acc[0][t] = acc[1][t] = float4v{0.f, 0.f, 0.f, 0.f};
+    const auto take = [&](const Frag (&f)[kFrom]) {
+#pragma unroll
+        for (int t = 0; t < TB; ++t)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) acc[c][t] = multiply(f[c], f[2 + t], acc[c][t]);
+    };
+    const unsigned spans = p.k / kSpan, start = spans != 0 ? blockIdx.x * 29 % spans : 0;
+    const auto turn = [&](unsigned span) { return span + start < spans ? span + start : span + start - spans; };
+    unsigned span = wave;
+    for (; span + (kBatch - 1) * WAVES < spans; span += kBatch * WAVES) {
+        Frag f[kBatch][2][kFrom];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+            for (int o = 0; o < kFrom; ++o)
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+                    f[i][half][o] = *reinterpret_cast<const Frag*>(from[o] + turn(span + i * WAVES) * kSpan + half * (kSpan / 2));
+        __builtin_amdgcn_sched_barrier(0);                               // (all of them before the first is used)
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) take(f[i][0]), take(f[i][1]);
+    }
+    for (; span * kSpan < p.k; span += WAVES) {                          // (k is whole chunks)
+        const unsigned first = (span < spans ? turn(span) : span) * kSpan;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            Frag f[kFrom];
+            const unsigned at = first + half * (kSpan / 2);
+#pragma unroll
+            for (int o = 0; o < kFrom; ++o) {
+                f[o] = Frag{};
+                if (at + quarter * kChunk < p.k) f[o] = *reinterpret_cast<const Frag*>(from[o] + at);
+            }
+            take(f);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) sums[wave][c][t * 16 + r][quarter] = acc[c][t];
+    __syncthreads();
+    float4v* const flat = &sums[0][0][0][0];
+    constexpr int kFlat = 2 * TB * 16 * kCols / 4;
+    for (int i = threadIdx.x; i < kFlat; i += 64 * WAVES) {
+        float4v sum = flat[i];
+#pragma unroll
+        for (int other = 1; other < WAVES; ++other) sum += flat[other * kFlat + i];
+        flat[i] = sum;
+    }
+    __syncthreads();
+    constexpr int kGroups = kCols / 8;
+    static_assert(TB * 16 * kGroups <= 64 * WAVES, "a lane for each group of eight columns");
+    const unsigned token = threadIdx.x / kGroups, group = threadIdx.x % kGroups, col = col0 + group * 8;
+    if (token >= p.m || token >= TB * 16 || col >= (DOES == Does::kSlope ? p.ldd : p.n)) return;
+    Eight g, u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) g.v[e] = sums[0][0][token][group * 2 + e / 4][e % 4], u.v[e] = sums[0][1][token][group * 2 + e / 4][e % 4];
+    finish_group<T, DOES>(p, token, col, g, u);
+}
+
 // The parts' sums of the tiles that are summed in parts, joined in the order of the parts.  A lane takes eight neighbouring columns.
 template <typename T, Does DOES, class S>
 __global__ __launch_bounds__(256) void join_kernel(GluArgs<T> p, unsigned tp, unsigned tq) {
@@ -993,8 +1078,26 @@ zvc_status product_of(const GluArgs<T>& p, hipStream_t stream) {
     return launch(join_kernel<T, DOES, S>, dim3(div_up(groups, 256)), 256, stream, p, tp, tq);
 }
 
+template <typename T, Does DOES, int TB, int WAVES>
+zvc_status tokens_of(const GluArgs<T>& p, hipStream_t stream) {
+    const size_t cols = DOES == Does::kSlope ? p.ldd : p.n;
+    return launch(token_kernel<T, DOES, TB, WAVES>, dim3(div_up(cols, 16)), 64 * WAVES, stream, p);
+}
+
+// The most tokens that take the kernel for few of them.  us (weights from memory), tiles | that kernel: bf16 n = k = 4096, 1 token
+// 22.6 | 14.2, 16 tokens 22.9 | 15.0, 32 23.1 | 18.7, 64 27.0 | 25.8; n = 11264, 1 token 45.6 | 32.8, 64 tokens 64 | 68;
+// fp32 n = k = 4096, 1 token 40.6 | 26.0, 32 40.9 | 38.8, and from there on the products bound it, 40 at n = 11264 121 | 156.
+constexpr size_t few_tokens(size_t w) { return w == 4 ? 32 : 64; }
+
 template <typename T, Does DOES>
 zvc_status product(GluArgs<T> p, float* sums, hipStream_t stream) {
+    if constexpr (DOES == Does::kForward || DOES == Does::kSlope) {
+        if (p.m <= few_tokens(sizeof(T)) && p.k != 0) {
+            if (p.m <= 16) return tokens_of<T, DOES, 1, 8>(p, stream);
+            if (p.m <= 32) return tokens_of<T, DOES, 2, 8>(p, stream);
+            if constexpr (sizeof(T) == 2) return tokens_of<T, DOES, 4, 4>(p, stream);
+        }
+    }
     const Cut cut = cut_of<DOES>(p.m, p.n, p.k, sizeof(T));
     p.whole = cut.whole, p.parts = cut.parts, p.sums = sums;
     if constexpr (sizeof(T) == 2)
