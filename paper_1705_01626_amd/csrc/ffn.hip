@@ -31,6 +31,9 @@ struct Words {
     unsigned w[4];
 };
 
+// a ^ b ^ c, one instruction.
+__device__ __forceinline__ unsigned xor3(unsigned a, unsigned b, unsigned c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
+
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw 2011): a block cipher's rounds of two 32 x 32 bit products each.
 __device__ __forceinline__ Words philox(uint64_t index, uint64_t offset, uint64_t seed) {
     unsigned c0 = static_cast<unsigned>(index), c1 = static_cast<unsigned>(index >> 32);
@@ -39,9 +42,9 @@ __device__ __forceinline__ Words philox(uint64_t index, uint64_t offset, uint64_
 #pragma unroll
     for (int round = 0; round < 10; ++round) {
         const uint64_t a = static_cast<uint64_t>(0xD2511F53u) * c0, b = static_cast<uint64_t>(0xCD9E8D57u) * c2;
-        c0 = static_cast<unsigned>(b >> 32) ^ c1 ^ k0;
+        c0 = xor3(static_cast<unsigned>(b >> 32), c1, k0);
         c1 = static_cast<unsigned>(b);
-        c2 = static_cast<unsigned>(a >> 32) ^ c3 ^ k1;
+        c2 = xor3(static_cast<unsigned>(a >> 32), c3, k1);
         c3 = static_cast<unsigned>(a);
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
@@ -51,22 +54,34 @@ __device__ __forceinline__ Words philox(uint64_t index, uint64_t offset, uint64_
 
 __device__ __forceinline__ unsigned half_of(const Words& r, int j) { return (r.w[j / 2] >> (16 * (j % 2))) & 0xFFFFu; }
 
-// Bit j: element 8 * group + j stays.  16 bits decide, but for one in 65536 elements, where 16 more do.
-__device__ __forceinline__ unsigned keep_group(const Drop& d, uint64_t offset, uint64_t group) {
-    const Words r = philox(group, offset, d.seed);
-    unsigned keep = 0, tie = 0;
+// Whether 16 bits are enough for all eight: none of them equals the fraction's upper half (or that has no lower one).
+__device__ __forceinline__ bool decided(const Drop& d, const Words& r) {
+    if (d.low == 0) return true;
+    unsigned equal = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        keep |= static_cast<unsigned>(half_of(r, j) >= d.high) << j;
-        tie |= static_cast<unsigned>(half_of(r, j) == d.high) << j;
+    for (int i = 0; i < 4; ++i) {
+        const unsigned x = r.w[i] ^ (d.high * 0x10001u);             // a half of zeros where equal
+        equal |= (x - 0x10001u) & ~x & 0x80008000u;
     }
-    if (d.low != 0 && tie != 0) {
+    return equal == 0;
+}
+
+// Bit j: element 8 * group + j stays.  `r`: the group's words.
+__device__ __forceinline__ unsigned keep_bits(const Drop& d, uint64_t offset, uint64_t group, const Words& r) {
+    unsigned keep = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) keep |= static_cast<unsigned>(half_of(r, j) >= d.high) << j;
+    if (!decided(d, r)) {                                            // one element in 65536: 16 bits more
         const Words more = philox(group | (uint64_t{1} << 63), offset, d.seed);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if ((tie >> j & 1u) != 0 && half_of(more, j) < d.low) keep &= ~(1u << j);
+            if (half_of(r, j) == d.high && half_of(more, j) < d.low) keep &= ~(1u << j);
     }
     return keep;
+}
+
+__device__ __forceinline__ unsigned keep_group(const Drop& d, uint64_t offset, uint64_t group) {
+    return keep_bits(d, offset, group, philox(group, offset, d.seed));
 }
 
 // Bits for elements first .. first + 7, wherever they begin.
@@ -151,35 +166,72 @@ __device__ __forceinline__ void store_some(T* at, const Eight& e, int there, boo
 
 constexpr int kDropThreads = 256;
 
-// y = drop(x) [+ residual].  A lane owns eight consecutive elements, one counter of the generator.  WHOLE: no group of
-// eight straddles two rows.
-template <typename T, bool WHOLE>
+// Zeros in the place of a group's dropped elements.  Where 16 bits decide all of them each is compared where it lies: the
+// generator and these comparisons are what a 16-bit tensor's call spends beside its traffic.
+__device__ __forceinline__ void drop_group(const Drop& d, uint64_t offset, uint64_t group, const Words& words, Eight& e) {
+    if (!decided(d, words)) {
+        drop8(keep_bits(d, offset, group, words), e);
+    } else if (d.high != 0) {
+        const unsigned below = (d.high << 16) - 1;                   // (p = 1: nothing is above)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e.v[j] = (j % 2 ? words.w[j / 2] : words.w[j / 2] << 16) > below ? e.v[j] : 0.f;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void drop_some(const T* x, const T* residual, T* y, int count, unsigned keep, float scale) {
+    for (int j = 0; j < count; ++j) {
+        float v = (keep >> j & 1u) != 0 ? static_cast<float>(x[j]) * scale : 0.f;
+        if (residual != nullptr) v += static_cast<float>(residual[j]);
+        y[j] = static_cast<T>(v);
+    }
+}
+
+// y = drop(x) [+ residual].  A lane owns GROUPS times eight consecutive elements, each one counter of the generator.  Memory bounds
+// it, and with 16-bit elements nearly the generator too (20 multiplications for 16 bytes).  33.5 M elements, us and TB/s: bf16
+// 27.3, 4.9 (25.4 without the generator); fp32 49, 5.5; bf16 with a residual at 67 M elements 74.4, 5.4.  GROUPS = 1 | 2 | 4:
+// bf16 28.8 | 27.3 | 30.4, fp32 with a residual 68.3 | 71.1 | 71.9.
+template <typename T, int GROUPS>
 __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const T* x, size_t ldx, const T* residual, size_t ldr,
                                                                T* y, size_t ldy, size_t cols, uint64_t total, Drop d) {
-    const uint64_t group = static_cast<uint64_t>(blockIdx.x) * kDropThreads + threadIdx.x;
-    const uint64_t first = group * 8;
-    if (first >= total) return;
-    const unsigned keep = d.active ? keep_group(d, effective_offset(d), group) : 0xFFu;
-    uint64_t row = first / cols, col = first - row * cols;
-    if constexpr (WHOLE) {
-        const int there = total - first < 8 ? static_cast<int>(total - first) : 8;
-        const bool full = __all(there == 8);
-        Eight e = load_some(x + row * ldx + col, there, full);
+    const uint64_t offset = d.active ? effective_offset(d) : 0;
+    const uint64_t group0 = static_cast<uint64_t>(blockIdx.x) * (kDropThreads * GROUPS) + threadIdx.x;
+    Eight e[GROUPS], r[GROUPS];
+    uint64_t row[GROUPS], col[GROUPS];
+    bool inside[GROUPS];                                           // eight elements of one row
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e.v[j] *= d.scale;
-        drop8(keep, e);
-        if (residual != nullptr) {
-            const Eight r = load_some(residual + row * ldr + col, there, full);
+    for (int g = 0; g < GROUPS; ++g) {
+        const uint64_t first = (group0 + g * kDropThreads) * 8;
+        row[g] = cols >= total ? 0 : first / cols;
+        col[g] = first - row[g] * cols;
+        inside[g] = first + 8 <= total && col[g] + 8 <= cols;
+        if (!inside[g]) continue;
+        e[g] = load8(x + row[g] * ldx + col[g]);
+        if (residual != nullptr) r[g] = load8(residual + row[g] * ldr + col[g]);
+    }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e.v[j] += r.v[j];
-        }
-        store_some(y + row * ldy + col, e, there, full);
-    } else {
-        for (int j = 0; j < 8 && first + j < total; ++j) {
-            float v = (keep >> j & 1u) ? static_cast<float>(x[row * ldx + col]) * d.scale : 0.f;
-            if (residual != nullptr) v += static_cast<float>(residual[row * ldr + col]);
-            y[row * ldy + col] = static_cast<T>(v);
-            if (++col == cols) col = 0, ++row;
+    for (int g = 0; g < GROUPS; ++g) {
+        const uint64_t group = group0 + g * kDropThreads, first = group * 8;
+        if (first >= total) continue;
+        const Words words = d.active ? philox(group, offset, d.seed) : Words{};
+        if (inside[g]) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[g].v[j] *= d.scale;
+            if (d.active) drop_group(d, offset, group, words, e[g]);
+            if (residual != nullptr) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) e[g].v[j] += r[g].v[j];
+            }
+            store8(y + row[g] * ldy + col[g], e[g]);
+        } else {
+            const unsigned keep = d.active ? keep_bits(d, offset, group, words) : 0xFFu;
+            uint64_t line = row[g], at = col[g];
+            for (int j = 0; j < 8 && first + j < total; ++j) {
+                float v = (keep >> j & 1u) != 0 ? static_cast<float>(x[line * ldx + at]) * d.scale : 0.f;
+                if (residual != nullptr) v += static_cast<float>(residual[line * ldr + at]);
+                y[line * ldy + at] = static_cast<T>(v);
+                if (++at == cols) at = 0, ++line;
+            }
         }
     }
 }
@@ -980,11 +1032,11 @@ zvc_status dropout_as(const void* x, size_t ldx, const void* residual, size_t ld
                       size_t cols, const Drop& d, hipStream_t stream) {
     if (ldx == cols && ldy == cols && (residual == nullptr || ldr == cols)) cols *= rows, rows = 1, ldx = ldy = ldr = cols;
     const uint64_t total = static_cast<uint64_t>(rows) * cols;
-    const bool whole = rows == 1 || cols % 8 == 0;
-    const size_t blocks = div_up(div_up(total, 8), kDropThreads);
+    constexpr int kGroups = sizeof(T) == 2 ? 2 : 1;
+    const size_t blocks = div_up(div_up(total, 8), static_cast<size_t>(kDropThreads) * kGroups);
     if (blocks > 0x7FFFFFFF) return ZVC_E_ARG;
-    return launch(whole ? dropout_kernel<T, true> : dropout_kernel<T, false>, dim3(blocks), kDropThreads, stream,
-                  static_cast<const T*>(x), ldx, static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy, cols, total, d);
+    return launch(dropout_kernel<T, kGroups>, dim3(blocks), kDropThreads, stream, static_cast<const T*>(x), ldx,
+                  static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy, cols, total, d);
 }
 
 bool sizes_ok(size_t m, size_t n, size_t k) {
