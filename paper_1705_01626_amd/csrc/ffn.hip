@@ -1058,7 +1058,6 @@ using Thin = Shape<4, 1, 4, 2>;                 // 256 x 32, four waves: few tok
 
 constexpr unsigned kUnits = 256;                // compute units
 constexpr double kAlone = 0.6;
-constexpr double kFp32Stage = 3.5;              // an fp32 stage against a 16-bit one: half the steps at a sixteenth of the rate
 constexpr double kJoinUs = 3, kSumsPerUs = 3e6;
 
 // Tiles of a product of this shape, by columns and rows.
@@ -1088,7 +1087,6 @@ void try_cut(Size size, double stage_us, double item_us, size_t m, size_t n, siz
     tiles_of<DOES, S>(m, n, k, &cols, &rows);
     const size_t tiles = cols * rows, slots = kUnits * S::kPerUnit;
     const size_t stages = div_up(DOES == Does::kDw ? m : DOES == Does::kDx ? 2 * n : k, kStageBytes / w);
-    if (w == 4) stage_us *= kFp32Stage;
     const auto rounds = [&](size_t items, size_t stages_each) {
         const size_t last = items % slots;             // alone on its compute unit, an item of two takes less time
         const double alone = last != 0 && last <= kUnits && slots > kUnits ? kAlone : 1;
@@ -1109,11 +1107,16 @@ void try_cut(Size size, double stage_us, double item_us, size_t m, size_t n, siz
 template <Does DOES>
 Cut cut_of(size_t m, size_t n, size_t k, size_t w) {
     Cut best{Size::kSmall, 0, 1, 0, 1e300};
+    if (w == 4) {                                // the products bound it, whatever the tile; a stage is 32 steps
+        try_cut<DOES, Small>(Size::kSmall, 3.8, 5, m, n, k, w, &best);
+        try_cut<DOES, Thin>(Size::kThin, 1.95, 4, m, n, k, w, &best);
+        return best;
+    }
     constexpr int kWhich = DOES == Does::kDx ? 1 : DOES == Does::kDw ? 2 : 0;
-    constexpr double kLargeStage[] = {1.45, 1.55, 1.6}, kSmallStage[] = {0.85, 1.15, 1.1}, kThinStage[] = {0.9, 0.9, 0.9};
-    if (w == 2) try_cut<DOES, Large>(Size::kLarge, kLargeStage[kWhich], 8, m, n, k, w, &best);
+    constexpr double kLargeStage[] = {1.45, 1.55, 1.6}, kSmallStage[] = {0.85, 1.15, 1.1};
+    try_cut<DOES, Large>(Size::kLarge, kLargeStage[kWhich], 8, m, n, k, w, &best);
     try_cut<DOES, Small>(Size::kSmall, kSmallStage[kWhich], 5, m, n, k, w, &best);
-    try_cut<DOES, Thin>(Size::kThin, kThinStage[kWhich], 4, m, n, k, w, &best);
+    try_cut<DOES, Thin>(Size::kThin, 0.9, 4, m, n, k, w, &best);
     return best;
 }
 
