@@ -60,8 +60,9 @@ typedef enum zvc_activation { ZVC_RELU = 0, ZVC_SILU = 1, ZVC_GELU = 2, ZVC_GELU
 
 /* The largest n, k and row stride. */
 #define ZVC_FFN_MAX_COLUMNS ((size_t)1 << 21)
-/* The largest m. */
+/* The largest m, m n and m k. */
 #define ZVC_FFN_MAX_ROWS ((size_t)1 << 28)
+#define ZVC_FFN_MAX_ELEMENTS ((size_t)1 << 40)
 
 /* p as the calls take it: the nearest multiple of 2^-32, in 2^-32.  p outside [0, 1] or NaN: more than 2^32, which the calls refuse. */
 uint64_t zvc_dropout_fraction(double p);

@@ -7,7 +7,9 @@
 
 #include <cmath>
 #include <cstdint>
+#include <tuple>
 #include <type_traits>
+#include <utility>
 
 namespace {
 
@@ -656,10 +658,12 @@ struct Tile {
     InQ in_q;
     uint64_t p0, p1, q0, q1;
 
-    // Where tile `at` lies.  Tiles are walked in bands of eight rows: what 32 workgroups of an XCD read at a time then fits its L2.
+    // Where tile `at` lies.  Tiles are walked in bands of some rows: what 32 workgroups of an XCD read at a time then fits its L2.
+    // (4 | 8 | 16 rows: long prompt 2235 | 2205 | 2288 us, largest backward 3478 | 3515 | 3598.)
     __device__ __forceinline__ void locate(unsigned at, unsigned tp, unsigned tq) {
-        const unsigned band = at / (8 * tp), in_band = at % (8 * tp), height = tq - band * 8 < 8 ? tq - band * 8 : 8;
-        const unsigned tile_q = band * 8 + in_band % height, halves = tq / 2;
+        constexpr unsigned kBand = kFold ? 8 : 4;
+        const unsigned band = at / (kBand * tp), in_band = at % (kBand * tp), height = tq - band * kBand < kBand ? tq - band * kBand : kBand;
+        const unsigned tile_q = band * kBand + in_band % height, halves = tq / 2;
         col0 = in_band / height * kCols;
         second = DOES == Does::kDw && tile_q >= halves;
         row0 = (second ? tile_q - halves : tile_q) * S::QT;
@@ -991,11 +995,18 @@ __global__ __launch_bounds__(256) void align_kernel(const T* from, size_t ld, T*
 }
 
 // ------------------------------------------------------------------ host side
-template <typename K, typename... A>
-zvc_status launch(K kernel, dim3 grid, unsigned threads, hipStream_t stream, A... args) {
-    (void)hipGetLastError();
-    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, args...);
-    return hipGetLastError() == hipSuccess ? ZVC_OK : ZVC_E_HIP;
+// A launch that reports its own status (hipGetLastError would also report, and clear, an earlier error of the calling thread).
+template <typename... Params, size_t... I>
+zvc_status launch_as(void (*kernel)(Params...), dim3 grid, unsigned threads, hipStream_t stream, std::tuple<Params...>& values,
+                     std::index_sequence<I...>) {
+    void* pointers[] = {static_cast<void*>(&std::get<I>(values))...};
+    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), pointers, 0, stream) == hipSuccess ? ZVC_OK : ZVC_E_HIP;
+}
+template <typename... Params, typename... Args>
+zvc_status launch(void (*kernel)(Params...), dim3 grid, unsigned threads, hipStream_t stream, Args... args) {
+    static_assert(sizeof...(Params) == sizeof...(Args), "one argument per kernel parameter");
+    std::tuple<Params...> values(static_cast<Params>(args)...);
+    return launch_as(kernel, grid, threads, stream, values, std::index_sequence_for<Params...>{});
 }
 
 inline size_t type_bytes(int type) { return type == ZVC_FP32 ? 4 : type == ZVC_FP16 || type == ZVC_BF16 ? 2 : 0; }
@@ -1040,7 +1051,8 @@ zvc_status dropout_as(const void* x, size_t ldx, const void* residual, size_t ld
 }
 
 bool sizes_ok(size_t m, size_t n, size_t k) {
-    return m <= ZVC_FFN_MAX_ROWS && n <= ZVC_FFN_MAX_COLUMNS && k <= ZVC_FFN_MAX_COLUMNS;
+    return m <= ZVC_FFN_MAX_ROWS && n <= ZVC_FFN_MAX_COLUMNS && k <= ZVC_FFN_MAX_COLUMNS && m * n <= ZVC_FFN_MAX_ELEMENTS &&
+           m * k <= ZVC_FFN_MAX_ELEMENTS;
 }
 
 template <typename T>
@@ -1125,7 +1137,6 @@ zvc_status product_of(const GluArgs<T>& p, hipStream_t stream) {
     size_t cols, rows;
     tiles_of<DOES, S>(p.m, p.n, p.k, &cols, &rows);
     const size_t items = p.whole + (cols * rows - p.whole) * p.parts, room = kUnits * S::kPerUnit;
-    if (items > 0x7FFFFFFF) return ZVC_E_ARG;
     const unsigned tp = static_cast<unsigned>(cols), tq = static_cast<unsigned>(rows);
     const zvc_status st = launch(product_kernel<T, DOES, S>, dim3(items < room ? items : room), S::kThreads, stream, p, tp, tq);
     if (st != ZVC_OK || p.parts == 1) return st;
