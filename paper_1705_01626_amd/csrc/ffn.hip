@@ -124,15 +124,23 @@ __device__ __forceinline__ Eight load8(const T* at) {
     return out;
 }
 
-template <typename T>
+// STREAM: past the caches' replacement, for an output that they cannot hold.
+template <bool STREAM = false, typename T>
 __device__ __forceinline__ void store8(T* at, const Eight& e) {
     constexpr int kPer = 16 / sizeof(T);
+    using Quad = unsigned __attribute__((ext_vector_type(4), aligned(sizeof(T))));
 #pragma unroll
     for (int h = 0; h < 8 / kPer; ++h) {
         Pack<T> p;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) p.v[j] = static_cast<T>(e.v[h * kPer + j]);
-        __builtin_memcpy(at + h * kPer, &p, 16);
+        if constexpr (STREAM) {
+            Quad q;
+            __builtin_memcpy(&q, &p, 16);
+            __builtin_nontemporal_store(q, reinterpret_cast<Quad*>(at + h * kPer));
+        } else {
+            __builtin_memcpy(at + h * kPer, &p, 16);
+        }
     }
 }
 
@@ -193,7 +201,7 @@ __device__ __forceinline__ void drop_some(const T* x, const T* residual, T* y, i
 // it, and with 16-bit elements nearly the generator too (20 multiplications for 16 bytes).  33.5 M elements, us and TB/s: bf16
 // 27.3, 4.9 (25.4 without the generator); fp32 49, 5.5; bf16 with a residual at 67 M elements 74.4, 5.4.  GROUPS = 1 | 2 | 4:
 // bf16 28.8 | 27.3 | 30.4, fp32 with a residual 68.3 | 71.1 | 71.9.
-template <typename T, int GROUPS>
+template <typename T, int GROUPS, bool STREAM>
 __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const T* x, size_t ldx, const T* residual, size_t ldr,
                                                                T* y, size_t ldy, size_t cols, uint64_t total, Drop d) {
     const uint64_t offset = d.active ? effective_offset(d) : 0;
@@ -224,7 +232,7 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const T* x, size_
 #pragma unroll
                 for (int j = 0; j < 8; ++j) e[g].v[j] += r[g].v[j];
             }
-            store8(y + row[g] * ldy + col[g], e[g]);
+            store8<STREAM>(y + row[g] * ldy + col[g], e[g]);
         } else {
             const unsigned keep = d.active ? keep_bits(d, offset, group, words) : 0xFFu;
             uint64_t line = row[g], at = col[g];
@@ -552,10 +560,14 @@ __device__ __forceinline__ void finish8(const GluArgs<T>& p, unsigned keep, unsi
 __device__ __forceinline__ int columns_left(unsigned n, unsigned col) { return col + 8 <= n ? 8 : col < n ? static_cast<int>(n - col) : 0; }
 
 // What becomes of a lane's strip of a tile, eight columns of QB rows 16 apart: straight code, row after row (the fences keep the
-// compiler from working on all rows at once, out of registers).
+// compiler from working on all rows at once, out of registers), and what is rare in another place (a tile's code that the
+// instruction cache has to fetch anew costs 3 us).  The large tiles' outputs go past the caches, which would
+// not keep them, and leave the operands there (long prompt 2295 | 2253 us, 8192 tokens kept 375 | 361); dg and du, which
+// are read next, do not (largest backward 3557 | 3605).
 template <typename T, Does DOES, class S>
 __device__ __forceinline__ void finish_tile(const GluArgs<T>& p, unsigned row, unsigned col, bool full, float4v (&acc)[S::PB][S::QB]) {
     static_assert(S::QB <= 8, "a bit for each of a lane's elements");
+    constexpr bool kStream = S::QT >= 256;
     if (col >= (DOES == Does::kSlope ? p.ldd : p.n)) return;     // (dg and du are written up to their rows' ends)
     const int there = columns_left(p.n, col);
     uint64_t keep = ~uint64_t{0};
@@ -611,8 +623,8 @@ __device__ __forceinline__ void finish_tile(const GluArgs<T>& p, unsigned row, u
                 take(j, g, u);
                 kept8(p, keeps(j), g, u);
                 if (row + j * 16 < p.m) {
-                    store8(cell(p.gate, row + j * 16, p.ldp, col), g);
-                    store8(cell(p.up, row + j * 16, p.ldp, col), u);
+                    store8<kStream>(cell(p.gate, row + j * 16, p.ldp, col), g);
+                    store8<kStream>(cell(p.up, row + j * 16, p.ldp, col), u);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -624,7 +636,7 @@ __device__ __forceinline__ void finish_tile(const GluArgs<T>& p, unsigned row, u
                 take(j, g, u);
                 Eight h = forward8<decltype(act)::value>(p, g, u);
                 if (p.d.active) drop8(keeps(j), h);
-                if (row + j * 16 < p.m) store8(cell(p.h, row + j * 16, p.ldh, col), h);
+                if (row + j * 16 < p.m) store8<kStream>(cell(p.h, row + j * 16, p.ldh, col), h);
                 __builtin_amdgcn_sched_barrier(0);
             }
         });
@@ -1038,6 +1050,8 @@ zvc_status make_drop(uint64_t drop, uint64_t seed, uint64_t offset, const uint64
     return ZVC_OK;
 }
 
+constexpr size_t kCacheBytes = size_t{32} << 20;   // of the eight XCDs' L2 together
+
 template <typename T>
 zvc_status dropout_as(const void* x, size_t ldx, const void* residual, size_t ldr, void* y, size_t ldy, size_t rows,
                       size_t cols, const Drop& d, hipStream_t stream) {
@@ -1046,8 +1060,10 @@ zvc_status dropout_as(const void* x, size_t ldx, const void* residual, size_t ld
     constexpr int kGroups = sizeof(T) == 2 ? 2 : 1;
     const size_t blocks = div_up(div_up(total, 8), static_cast<size_t>(kDropThreads) * kGroups);
     if (blocks > 0x7FFFFFFF) return ZVC_E_ARG;
-    return launch(dropout_kernel<T, kGroups>, dim3(blocks), kDropThreads, stream, static_cast<const T*>(x), ldx,
-                  static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy, cols, total, d);
+    // us, as it is | STREAM: bf16 of 67 MB 27.9 | 25.9, 134 MB and a residual 74.6 | 72.0; fp32 of 134 MB 49.4 | 52.4
+    const bool stream_out = sizeof(T) == 2 && total * sizeof(T) > kCacheBytes;
+    return launch(stream_out ? dropout_kernel<T, kGroups, true> : dropout_kernel<T, kGroups, false>, dim3(blocks), kDropThreads, stream,
+                  static_cast<const T*>(x), ldx, static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy, cols, total, d);
 }
 
 bool sizes_ok(size_t m, size_t n, size_t k) {
