@@ -401,3 +401,32 @@ def test_rows_beyond_32_bit_offsets():
     ffn.zvc_glu_forward(x, wg, wu, h, ffn.new_glu_workspace(x, wg, wu), "silu")
     check(h[-300:], ffn_ref.forward(tail, wg, wu, "silu")[0], "h")
     assert not bool(h[:1024].any())
+
+
+def test_gradients_of_rows_beyond_32_bit_offsets():
+    """x, dh, dg and du of more than 4 GB each; only the last rows of dh are not zero, so the gradients are theirs alone."""
+    m, n, k, rows = (1 << 22) + 5, 520, 520, 300
+    gen = generator("far back")
+    make = lambda *shape: torch.randn(*shape, generator=gen, device=DEV)
+    x = make(1, k).to(torch.bfloat16).expand(m, k).contiguous()
+    x[-rows:] = make(rows, k).to(x.dtype)
+    dh = torch.zeros(m, n, dtype=x.dtype, device=DEV)
+    dh[-rows:] = make(rows, n).to(x.dtype)
+    wg, wu = ((make(n, k) * k ** -0.5).to(x.dtype) for _ in range(2))
+    dx, dwg, dwu = torch.empty_like(x), torch.empty_like(wg), torch.empty_like(wu)
+    ffn.zvc_glu_backward(dh, x, wg, wu, dx, dwg, dwu, ffn.new_glu_workspace(x, wg, wu, backward=True), "silu")
+    want = ffn_ref.backward(dh[-rows:], x[-rows:], wg, wu, "silu")
+    check(dx[-rows:], want[0], "dx")
+    assert not bool(dx[:1 << 20].any()) and not bool(dx[-rows - (1 << 20):-rows].any())
+    for got, expected, label in zip((dwg, dwu), want[1:], ("dwg", "dwu")):
+        check(got, expected, label)                       # (adding zeros rounds nothing)
+
+
+@pytest.mark.parametrize("m,n,k", [(33, 48, 64), (129, 1032, 264), (600, 72, 2056)])
+def test_gradients_ignore_what_lies_behind_the_rows(m, n, k):
+    """Rows with gaps full of NaNs, odd tokens and columns in a stage, and a workspace full of NaNs: nothing of it gets in."""
+    x, wg, wu, dh = problem(m, n, k, torch.bfloat16, "relu")
+    want = backward(dh, x, wg, wu, "relu")
+    got = backward(strided(dh, 8), strided(x, 16), strided(wg, 8), strided(wu, 8), "relu")
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
