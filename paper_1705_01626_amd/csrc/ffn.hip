@@ -358,14 +358,15 @@ __device__ __forceinline__ void group_barrier() {
 
 enum class Lies { kAlong, kAcross };
 
-// The workgroup's tile: WP x WQ waves of PB x QB blocks of 16 x 16.
-template <int WP_, int WQ_, int PB_, int QB_>
+// The workgroup's tile: WP x WQ waves of PB x QB blocks of 16 x 16, and the stages that are in LDS at a time.
+template <int WP_, int WQ_, int PB_, int QB_, int RING>
 struct Shape {
+    static constexpr int kRing = RING;
     static constexpr int WP = WP_, WQ = WQ_, PB = PB_, QB = QB_;
     static constexpr int kWavesAll = WP * WQ, kThreads = 64 * kWavesAll;
     static constexpr int PT = WP * PB * 16, QT = WQ * QB * 16;
     static constexpr int kStage = (PT + QT) * kStageBytes;
-    static constexpr int kPerUnit = 4 * kStage > 160 << 10 ? 1 : 2;     // workgroups that a compute unit's LDS holds
+    static constexpr int kPerUnit = 2 * kRing * kStage > 160 << 10 ? 1 : 2;     // workgroups that a compute unit's LDS holds
 };
 
 // How one operand's tile of SIDE rows (kAlong) or columns (kAcross) is staged and read.  FOLD: the projections' P, in
@@ -423,7 +424,7 @@ struct Operand {
     // Stage: `left` of the reduction remain at `base` (FOLD: at `base` for Wg's rows, at `other` for Wu's).
     __device__ __forceinline__ void fetch(uint64_t base, uint64_t other, int left, unsigned lds) const {
         constexpr int kRun = 32 / kRowsPerLoad;             // loads that bring 32 rows
-        const bool odd = FOLD && kLoads == kRun && (first / kRun & 1);
+        const bool odd = FOLD && kLoads <= kRun && (first / kRun & 1);
         const int4v buffers[] = {buffer_at(odd ? other : base), buffer_at(other)};
         const auto from = [&](int i) { return buffers[FOLD && kRun > 0 && i >= kRun]; };
         if (left >= kSteps) {
@@ -659,7 +660,7 @@ struct Tile {
     static constexpr int kCols = kFold ? S::PT / 2 : S::PT;
     using InP = Operand<T, kP, S::PT, S::kWavesAll, kFold>;
     using InQ = Operand<T, kQ, S::QT, S::kWavesAll, false>;
-    static_assert(!kFold || InP::kLoads * InP::kRowsPerLoad == 32 || InP::kLoads * InP::kRowsPerLoad == 64, "whole runs of one weight's rows");
+    static_assert(!kFold || 32 % (InP::kLoads * InP::kRowsPerLoad) == 0 || InP::kLoads * InP::kRowsPerLoad == 64, "a wave fetches one weight's rows, or a run of each");
     static_assert(!kFold || S::PB == 4, "a wave's strip is 32 rows of each weight");
 
     unsigned col0, row0;
@@ -725,7 +726,8 @@ template <typename T, Does DOES, class S>
 __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluArgs<T> p, unsigned tp, unsigned tq) {
     using Where = Tile<T, DOES, S>;
     constexpr bool kFold = Where::kFold;
-    __shared__ alignas(1024) unsigned char lds[2 * S::kStage];
+    constexpr int kRing = S::kRing;
+    __shared__ alignas(1024) unsigned char lds[kRing * S::kStage];
     const unsigned base = static_cast<unsigned>(reinterpret_cast<uintptr_t>((LdsByte*)lds));
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wp = wave % S::WP, wq = wave / S::WP, r = lane & 15, quarter = lane >> 4;
@@ -761,9 +763,19 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
     Where tile;
     const auto begin = [&](unsigned item) {
         tile.init(p, item, tp, tq, wave, lane);
-        if (tile.begin < tile.end) tile.fetch(p, tile.begin, base);
-        if (tile.begin + 1 < tile.end) tile.fetch(p, tile.begin + 1, base + S::kStage);
+#pragma unroll
+        for (int i = 0; i < kRing; ++i)
+            if (tile.begin + i < tile.end) tile.fetch(p, tile.begin + i, base + i * S::kStage);
     };
+    // Waits until the loads of `stages` stages at most are on their way, if as many as the ring holds were asked for.
+    constexpr int kLoads = Where::InP::kLoads + Where::InQ::kLoads;
+    const auto wait_stages = [&](auto stages, bool full) {
+        constexpr int kLeft = decltype(stages)::value * kLoads;
+        if (kLeft != 0 && full) wait_loads<kLeft>();
+        else wait_loads<0>();
+    };
+    const auto place = [&](unsigned s) { return ((s - tile.begin) & (kRing - 1)) * S::kStage; };
+    static_assert((kRing & (kRing - 1)) == 0, "stages take places in turn");
     begin(blockIdx.x);
     for (unsigned item = blockIdx.x; item < items;) {
 #pragma unroll
@@ -771,18 +783,17 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
 #pragma unroll
             for (int j = 0; j < S::QB; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
         // A stage is multiplied in two halves.  While a half's products run, the next half is read from LDS; between
-        // the halves everyone has read the stage, and its buffer takes the stage after the next.
-        wait_loads<0>();
+        // the halves everyone has read the stage, and its place takes the one after the ring's last.
+        wait_stages(std::integral_constant<int, kRing - 1>{}, tile.begin + kRing <= tile.end);
         group_barrier();
         read(kFirst, 0);
         for (unsigned s = tile.begin; s < tile.end; ++s) {
-            const unsigned even = ((s - tile.begin) & 1) * S::kStage;
-            read(kSecond, even);
+            read(kSecond, place(s));
             product(kFirst);
-            wait_loads<0>();
+            wait_stages(std::integral_constant<int, kRing - 2>{}, s + kRing <= tile.end);
             group_barrier();                     // stage s + 1 is there, and everyone has read stage s
-            if (s + 2 < tile.end) tile.fetch(p, s + 2, base + even);
-            read(kFirst, S::kStage - even);      // (behind the last stage: what the buffer held, for nothing)
+            if (s + kRing < tile.end) tile.fetch(p, s + kRing, base + place(s));
+            read(kFirst, place(s + 1));          // (behind the last stage: what the place held, for nothing)
             product(kSecond);
         }
         const unsigned col0 = tile.col0, row0 = tile.row0;
@@ -1080,9 +1091,9 @@ void set_sizes(GluArgs<T>* p, size_t ldx, size_t ldw, size_t ldp, size_t m, size
 
 bool stride_ok(size_t ld, size_t cols) { return ld >= cols && ld <= ZVC_FFN_MAX_COLUMNS; }
 
-using Large = Shape<4, 2, 4, 8>;                // 256 x 256, eight waves
-using Small = Shape<2, 2, 4, 4>;                // 128 x 128, four waves
-using Thin = Shape<4, 1, 4, 2>;                 // 256 x 32, four waves: few tokens
+using Large = Shape<4, 2, 4, 8, 2>;             // 256 x 256, eight waves
+using Small = Shape<2, 2, 4, 4, 2>;             // 128 x 128, four waves
+using Thin = Shape<4, 1, 4, 2, 2>;              // 256 x 32, four waves: few tokens
 
 constexpr unsigned kUnits = 256;                // compute units
 constexpr double kAlone = 0.6;
