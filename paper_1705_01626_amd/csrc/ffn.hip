@@ -1,5 +1,15 @@
 // Gated feed-forward block and dropout, forward and backward, for AMD gfx950 (wave64): kernels and C ABI
 // (include/zvc_ffn.h has the formulas).
+//
+//   * dropout_kernel: one pass over the data, the mask made on the way by the counter-based generator.
+//   * product_kernel: every large product (both projections with what becomes of them; dx; dWg and dWu), tiles on the matrix
+//     cores, staged from memory straight to LDS, with the activation, dropout and the kept projections, or their gradients,
+//     in the tile's epilogue.  Sums that are too long for the few tiles there are are cut into parts that join_kernel adds.
+//   * token_kernel: the projections of up to 64 tokens, bound by reading the weights once.
+//   * slope_kernel: dg and du from kept projections; align_kernel: copies of inputs that do not take 16-byte accesses.
+//
+// Times in the comments are us on one MI355X, where a large copy moves 5.0 TB/s and a large bf16 product of the vendor's library
+// reaches 1260 to 1460 TFLOP/s (fp32 155).
 
 #include "zvc_ffn.h"
 
@@ -722,6 +732,14 @@ struct Tile {
 };
 
 // Workgroups take tiles until there are none left; the next tile's first stages are on their way while a tile is finished.
+//
+// What bounds it, with the large tile: the card's power.  16384 x 11264 x 4096 (forward, bf16) takes 2220 to 2260, 1340 to 1360
+// TFLOP/s: 0.485 for each step of k, at which the matrix cores are busy for 87 % of the cycles of a clock that is held near
+// 1.7 GHz, and the rest to begin and finish 22 tiles.  LDS is next: a half stage's reads take 768 of its 1024 cycles.  Four waves
+// of 128 x 128 with sums in accumulation registers read a third less, 0.472 a step, and finish tiles so much slower that it
+// is 2700 in all; instructions of 32 x 32 2430; a ring of five half stages 2660; one wave at a raised priority 2360; without the
+// reads between the products 2540; with tiles that are not persistent and epilogues with a branch per element 2440.  Small tiles
+// are bound by LDS: 64 x 64 a wave, 0.85 a stage for the two of a compute unit.
 template <typename T, Does DOES, class S>
 __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluArgs<T> p, unsigned tp, unsigned tq) {
     using Where = Tile<T, DOES, S>;
@@ -872,9 +890,11 @@ __device__ __forceinline__ void finish_group(const GluArgs<T>& p, unsigned row, 
 
 // ------------------------------------------------------------------ few tokens
 // The projections of up to 16 TB tokens.  Every weight is read once and used for all of them, so this is a matter of reading the
-// weights: straight into registers, 128 neighbouring bytes of 32 rows at a time and wave.  A workgroup takes 16 columns of both
+// weights (11264 x 4096, bf16, one token: 32.8, 5.6 TB/s): straight into registers, 128 neighbouring bytes of 32 rows at a time and
+// wave, all of a batch before the first is used (without that 37.3).  A workgroup takes 16 columns of both
 // weights, its WAVES waves take turns along k and their sums meet in LDS.  Workgroups begin at different places along k:
-// rows lie a power of two apart, and the same place in all of them is in few of the memory's channels.
+// rows lie a power of two apart, and the same place in all of them is in few of the memory's channels (without that 35.8).
+// With 64 tokens x takes the longer way: every workgroup reads all of it.
 template <typename T, Does DOES, int TB, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void token_kernel(GluArgs<T> p) {
     constexpr int W = sizeof(T), kChunk = 16 / W, kSpan = 128 / W;       // elements of 16 and of 128 bytes
@@ -956,6 +976,7 @@ __global__ __launch_bounds__(64 * WAVES) void token_kernel(GluArgs<T> p) {
 }
 
 // The parts' sums of the tiles that are summed in parts, joined in the order of the parts.  A lane takes eight neighbouring columns.
+// (Sums joined by atomics would depend on who comes first.)  67 MB of sums: 15.
 template <typename T, Does DOES, class S>
 __global__ __launch_bounds__(256) void join_kernel(GluArgs<T> p, unsigned tp, unsigned tq) {
     using Where = Tile<T, DOES, S>;
@@ -989,7 +1010,7 @@ __global__ __launch_bounds__(256) void join_kernel(GluArgs<T> p, unsigned tp, un
     }
 }
 
-// dg and du from kept projections; their rows are filled with zeros up to ldd.
+// dg and du from kept projections; their rows are filled with zeros up to ldd.  Memory bounds it: 4096 x 5632 bf16 42, 5.5 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void slope_kernel(GluArgs<T> p) {
     const unsigned groups = p.ldd / 8;
@@ -1096,7 +1117,7 @@ using Small = Shape<2, 2, 4, 4, 2>;             // 128 x 128, four waves
 using Thin = Shape<4, 1, 4, 2, 2>;              // 256 x 32, four waves: few tokens
 
 constexpr unsigned kUnits = 256;                // compute units
-constexpr double kAlone = 0.6;
+constexpr double kAlone = 0.6;                  // a stage's time where one workgroup has a compute unit that takes two
 constexpr double kJoinUs = 3, kSumsPerUs = 3e6;
 
 // Tiles of a product of this shape, by columns and rows.
@@ -1119,7 +1140,12 @@ struct Cut {
 };
 
 // The cut that takes the least time by this account, in us: workgroups take items in rounds; an item costs its stages and
-// something to begin and finish; joining costs a launch and the sums' way to memory and back.
+// something to begin and finish; joining costs a launch and the sums' way to memory and back.  The stages' times are fitted to
+// calls with every cut forced in turn (L, S: large and small tiles, with parts): forward 4096 x 5632 x 2048 L 175, S 171, but
+// with outputs kept and other work around them 210 and 250; 2048 x 5632 x 2048 L 101, L in 2 parts behind the first round 98, S 93;
+// 512 x 4096 x 4096 S 44, L in 4 parts 50; dx of 4096 x 5632 x 2048 L in 2 parts 177, S 218; dx of 777 x 2730 x 1000 S in 8 parts 32,
+// 4 34, 1 71; dW of 4096 x 5632 x 2048 L 222, 2 parts behind the first round 190, S 219; fp32 2048 x 2816 x 1024 dx S in 4 parts 200,
+// S 377, thin tiles 233, dW thin in 4 parts 205, S 268.  The account's choice is within 15 % of the best of them.
 template <Does DOES, class S>
 void try_cut(Size size, double stage_us, double item_us, size_t m, size_t n, size_t k, size_t w, Cut* best) {
     size_t cols, rows;
