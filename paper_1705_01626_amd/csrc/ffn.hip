@@ -2,9 +2,9 @@
 // (include/zvc_ffn.h has the formulas).
 //
 //   * dropout_kernel: one pass over the data, the mask made on the way by the counter-based generator.
-//   * product_kernel: every large product (both projections with what becomes of them; dx; dWg and dWu), tiles on the matrix
-//     cores, staged from memory straight to LDS, with the activation, dropout and the kept projections, or their gradients,
-//     in the tile's epilogue.  Sums that are too long for the few tiles there are are cut into parts that join_kernel adds.
+//   * product_kernel, gradients_kernel: the large products (both projections with what becomes of them; dx with dWg and dWu),
+//     tiles on the matrix cores, staged from memory straight to LDS, with the activation, dropout and the kept projections, or
+//     their gradients, in the tile's epilogue.  Sums too long for the few tiles there are are cut into parts that a join adds.
 //   * token_kernel: the projections of up to 64 tokens, bound by reading the weights once.
 //   * slope_kernel: dg and du from kept projections; align_kernel: copies of inputs that do not take 16-byte accesses.
 //
@@ -508,11 +508,9 @@ struct GluArgs {
     const T *x, *wg, *wu, *dh;
     const T *gate_in, *up_in;
     T *h, *gate, *up, *dg, *du;
-    T *out, *out2;                      // dx; dwg and dwu
-    unsigned ldx, ldw, lddh, ldh, ldp, ldd, ldo, m, n, k;   // (32 bits hold them: scalar registers are short)
+    T *dx, *dwg, *dwu;
+    unsigned ldx, ldw, lddh, ldh, ldp, ldd, lddx, lddw, m, n, k;   // (32 bits hold them: scalar registers are short)
     int act;
-    float* sums;                        // parts' sums, to be joined: part by part, tile by tile as they lie in it
-    unsigned whole, parts;              // the tiles behind the first `whole` are summed in parts of the reduction
     Drop d;
 };
 
@@ -654,6 +652,14 @@ __device__ __forceinline__ void finish_tile(const GluArgs<T>& p, unsigned row, u
     }
 }
 
+// How one product is cut into work items: tp x tq tiles, of which the first `whole` are summed in one go and the others in `parts`
+// parts of the reduction each, whose sums lie part by part, tile by tile as they lie in it, and are joined.
+struct Plan {
+    float* sums;
+    unsigned tp, tq, whole, parts;
+    __host__ __device__ unsigned items() const { return whole + (tp * tq - whole) * parts; }
+};
+
 // The place of work item `id` of `count` in the order that they are walked in: workgroups go to the eight XCDs in turn, so
 // that each XCD takes a contiguous run of it.
 __device__ __forceinline__ unsigned place_of(unsigned id, unsigned count) {
@@ -691,23 +697,23 @@ struct Tile {
         second = DOES == Does::kDw && tile_q >= halves;
         row0 = (second ? tile_q - halves : tile_q) * S::QT;
     }
-    __device__ __forceinline__ void init(const GluArgs<T>& p, unsigned item, unsigned tp, unsigned tq, int wave, int lane) {
-        const unsigned rest = tp * tq - p.whole;
-        split = item >= p.whole;
+    __device__ __forceinline__ void init(const GluArgs<T>& p, const Plan& plan, unsigned item, int wave, int lane) {
+        const unsigned rest = plan.tp * plan.tq - plan.whole;
+        split = item >= plan.whole;
         part = 0;
         if (split) {
-            const unsigned at = place_of(item - p.whole, rest * p.parts);
+            const unsigned at = place_of(item - plan.whole, rest * plan.parts);
             part = at / rest;
             number = at - part * rest;
-            locate(p.whole + number, tp, tq);
+            locate(plan.whole + number, plan.tp, plan.tq);
         } else {
-            locate(place_of(item, p.whole), tp, tq);
+            locate(place_of(item, plan.whole), plan.tp, plan.tq);
         }
-        const unsigned parts = split ? p.parts : 1;
+        const unsigned parts = split ? plan.parts : 1;
         const unsigned rows = DOES == Does::kDw ? p.n : p.m, cols = kFold ? p.n : p.k;
         once = (length(p) + kSteps - 1) / kSteps;
         // (parts differ by a stage at most)
-        const unsigned stages = DOES == Does::kDx ? 2 * once : once, each = split ? stages / p.parts : stages, longer = stages - each * parts;
+        const unsigned stages = DOES == Does::kDx ? 2 * once : once, each = split ? stages / plan.parts : stages, longer = stages - each * parts;
         begin = part * each + (part < longer ? part : longer);
         end = begin + each + (part < longer ? 1 : 0);
         in_p.init(wave, lane, kFold || DOES == Does::kDx ? p.ldw : p.ldx, cols - col0 < S::PT ? cols - col0 : S::PT);
@@ -731,6 +737,8 @@ struct Tile {
     }
 };
 
+constexpr unsigned kNone = ~0u;                  // no work item
+
 // Workgroups take tiles until there are none left; the next tile's first stages are on their way while a tile is finished.
 //
 // What bounds it, with the large tile: the card's power.  16384 x 11264 x 4096 (forward, bf16) takes 2220 to 2260, 1340 to 1360
@@ -740,16 +748,15 @@ struct Tile {
 // is 2700 in all; instructions of 32 x 32 2430; a ring of five half stages 2660; one wave at a raised priority 2360; without the
 // reads between the products 2540; with tiles that are not persistent and epilogues with a branch per element 2440.  Small tiles
 // are bound by LDS: 64 x 64 a wave, 0.85 a stage for the two of a compute unit.
-template <typename T, Does DOES, class S>
-__global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluArgs<T> p, unsigned tp, unsigned tq) {
+//
+// `base`: the ring in LDS.  `next`: gives this workgroup's items, and kNone behind the last.
+template <typename T, Does DOES, class S, typename Next>
+__device__ __forceinline__ void work(const GluArgs<T>& p, const Plan& plan, unsigned base, int lane, Next next) {
     using Where = Tile<T, DOES, S>;
     constexpr bool kFold = Where::kFold;
     constexpr int kRing = S::kRing;
-    __shared__ alignas(1024) unsigned char lds[kRing * S::kStage];
-    const unsigned base = static_cast<unsigned>(reinterpret_cast<uintptr_t>((LdsByte*)lds));
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wp = wave % S::WP, wq = wave / S::WP, r = lane & 15, quarter = lane >> 4;
-    const unsigned items = p.whole + (tp * tq - p.whole) * p.parts;
 
     using ReadP = Reader<T, Where::kP, S::PT, S::PB, kFold>;
     using ReadQ = Reader<T, Where::kQ, S::QT, S::QB, false>;
@@ -780,7 +787,7 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
 
     Where tile;
     const auto begin = [&](unsigned item) {
-        tile.init(p, item, tp, tq, wave, lane);
+        tile.init(p, plan, item, wave, lane);
 #pragma unroll
         for (int i = 0; i < kRing; ++i)
             if (tile.begin + i < tile.end) tile.fetch(p, tile.begin + i, base + i * S::kStage);
@@ -794,8 +801,10 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
     };
     const auto place = [&](unsigned s) { return ((s - tile.begin) & (kRing - 1)) * S::kStage; };
     static_assert((kRing & (kRing - 1)) == 0, "stages take places in turn");
-    begin(blockIdx.x);
-    for (unsigned item = blockIdx.x; item < items;) {
+    unsigned item = next();
+    if (item == kNone) return;
+    begin(item);
+    while (item != kNone) {
 #pragma unroll
         for (int i = 0; i < S::PB; ++i)
 #pragma unroll
@@ -816,12 +825,10 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
         }
         const unsigned col0 = tile.col0, row0 = tile.row0;
         const bool second = tile.second, split = tile.split;
-        float* const sums = p.sums + (static_cast<size_t>(tile.part) * (tp * tq - p.whole) + tile.number) * (S::PT * S::QT);
-        item += gridDim.x;
-        if (item < items) {
-            group_barrier();                     // (the reads for nothing are done)
-            begin(item);
-        }
+        float* const sums = plan.sums + (static_cast<size_t>(tile.part) * (plan.tp * plan.tq - plan.whole) + tile.number) * (S::PT * S::QT);
+        item = next();
+        group_barrier();                         // (the reads for nothing are done)
+        if (item != kNone) begin(item);
 
         const int row_in = wq * S::QB * 16 + r;
         const unsigned row_first = row0 + row_in;
@@ -838,7 +845,8 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
             finish_tile<T, DOES, S>(p, row_first, col0 + wp * 32 + quarter * 8, col0 + wp * 32 + 32 <= p.n, acc);
         } else {
             const unsigned rows = DOES == Does::kDw ? p.n : p.m;
-            T* const out = second ? p.out2 : p.out;
+            T* const out = DOES == Does::kDx ? p.dx : second ? p.dwu : p.dwg;
+            const unsigned ldo = DOES == Does::kDx ? p.lddx : p.lddw;
             const bool full = col0 + (wp + 1) * S::PB * 16 <= p.k;
             const unsigned col = col0 + wp * S::PB * 16 + quarter * 4;
             struct Four { T v[4]; };
@@ -851,7 +859,7 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
             if (full) {
 #pragma unroll
                 for (int j = 0; j < S::QB; ++j) {
-                    T* const at = cell(out, row_first + j * 16, p.ldo, col);
+                    T* const at = cell(out, row_first + j * 16, ldo, col);
                     if (row_first + j * 16 < rows) {
 #pragma unroll
                         for (int i = 0; i < S::PB; ++i) {
@@ -863,7 +871,7 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
             } else {
 #pragma unroll
                 for (int j = 0; j < S::QB; ++j) {
-                    T* const at = cell(out, row_first + j * 16, p.ldo, col);
+                    T* const at = cell(out, row_first + j * 16, ldo, col);
                     if (row_first + j * 16 >= rows) continue;
 #pragma unroll
                     for (int i = 0; i < S::PB; ++i) {
@@ -876,6 +884,44 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluAr
             }
         }
     }
+}
+
+template <class S>
+__device__ __forceinline__ unsigned ring() {
+    __shared__ alignas(1024) unsigned char lds[S::kRing * S::kStage];
+    return static_cast<unsigned>(reinterpret_cast<uintptr_t>((LdsByte*)lds));
+}
+
+// Every gridDim.x-th item from `first` on.
+struct Turns {
+    unsigned at, items;
+    __device__ __forceinline__ unsigned operator()() {
+        const unsigned item = at;
+        at += gridDim.x;
+        return item < items ? item : kNone;
+    }
+};
+
+template <typename T, Does DOES, class S>
+__global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(GluArgs<T> p, Plan plan) {
+    work<T, DOES, S>(p, plan, ring<S>(), threadIdx.x & 63, Turns{blockIdx.x, plan.items()});
+}
+
+// dx, and behind it dWg and dWu, in one go: either alone leaves compute units idle in its last round.  The workgroups without a
+// dx item in its last round take `ahead` items of dW before the others take their first.
+template <typename T, class S>
+__global__ __launch_bounds__(S::kThreads, S::kPerUnit) void gradients_kernel(GluArgs<T> p, Plan dx, Plan dw, unsigned ahead) {
+    // (a lane's number that is had again at any time: no register holds the thread's through both)
+    const int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
+    const unsigned base = ring<S>(), first = dx.items() % gridDim.x, idle = gridDim.x - first;
+    work<T, Does::kDx, S>(p, dx, base, lane, Turns{blockIdx.x, dx.items()});
+    const unsigned items = dw.items(), mine = blockIdx.x >= first ? blockIdx.x - first : blockIdx.x + idle;
+    unsigned turn = mine < idle ? 0 : ahead;
+    work<T, Does::kDw, S>(p, dw, base, lane, [&]() {
+        const unsigned item = turn < ahead ? mine + turn * idle : ahead * idle + mine + (turn - ahead) * gridDim.x;
+        ++turn;
+        return item < items ? item : kNone;
+    });
 }
 
 // The same for one group of eight columns, outside a tile.
@@ -978,23 +1024,23 @@ __global__ __launch_bounds__(64 * WAVES) void token_kernel(GluArgs<T> p) {
 // The parts' sums of the tiles that are summed in parts, joined in the order of the parts.  A lane takes eight neighbouring columns.
 // (Sums joined by atomics would depend on who comes first.)  67 MB of sums: 15.
 template <typename T, Does DOES, class S>
-__global__ __launch_bounds__(256) void join_kernel(GluArgs<T> p, unsigned tp, unsigned tq) {
+__device__ __forceinline__ void join(const GluArgs<T>& p, const Plan& plan, unsigned i) {
     using Where = Tile<T, DOES, S>;
     constexpr int kGroups = Where::kCols / 8, kPerTile = S::QT * kGroups;
-    const unsigned rest = tp * tq - p.whole, i = blockIdx.x * 256 + threadIdx.x, number = i / kPerTile;
+    const unsigned rest = plan.tp * plan.tq - plan.whole, number = i / kPerTile;
     if (number >= rest) return;
     const int row_in = i % kPerTile / kGroups, col_in = i % kGroups * 8;
     Where tile;
-    tile.locate(p.whole + number, tp, tq);
+    tile.locate(plan.whole + number, plan.tp, plan.tq);
     const unsigned rows = DOES == Does::kDw ? p.n : p.m, cols = Where::kFold ? p.n : p.k;
     const unsigned row = tile.row0 + row_in, col = tile.col0 + col_in;
     if (row >= rows || col >= (DOES == Does::kSlope ? p.ldd : cols)) return;
     const auto sum = [&](int from) {
         Eight e = {};
-        const float* at = p.sums + static_cast<size_t>(number) * (S::PT * S::QT) + row_in * S::PT + from + col_in;
+        const float* at = plan.sums + static_cast<size_t>(number) * (S::PT * S::QT) + row_in * S::PT + from + col_in;
         const size_t step = static_cast<size_t>(rest) * (S::PT * S::QT);
 #pragma unroll 4
-        for (unsigned part = 0; part < p.parts; ++part, at += step) {
+        for (unsigned part = 0; part < plan.parts; ++part, at += step) {
             const Eight x = load8(at);
 #pragma unroll
             for (int j = 0; j < 8; ++j) e.v[j] += x.v[j];
@@ -1006,8 +1052,21 @@ __global__ __launch_bounds__(256) void join_kernel(GluArgs<T> p, unsigned tp, un
         finish_group<T, DOES>(p, row, col, g, u);
     } else {
         const int there = columns_left(cols, col);
-        store_some(cell(tile.second ? p.out2 : p.out, row, p.ldo, col), sum(0), there, __all(there == 8));
+        T* const out = DOES == Does::kDx ? p.dx : tile.second ? p.dwu : p.dwg;
+        store_some(cell(out, row, DOES == Does::kDx ? p.lddx : p.lddw, col), sum(0), there, __all(there == 8));
     }
+}
+
+template <typename T, Does DOES, class S>
+__global__ __launch_bounds__(256) void join_kernel(GluArgs<T> p, Plan plan) {
+    join<T, DOES, S>(p, plan, blockIdx.x * 256 + threadIdx.x);
+}
+
+// The first `blocks` workgroups: dx; the others: dWg and dWu.
+template <typename T, class S>
+__global__ __launch_bounds__(256) void join_gradients_kernel(GluArgs<T> p, Plan dx, Plan dw, unsigned blocks) {
+    if (blockIdx.x < blocks) join<T, Does::kDx, S>(p, dx, blockIdx.x * 256 + threadIdx.x);
+    else join<T, Does::kDw, S>(p, dw, (blockIdx.x - blocks) * 256 + threadIdx.x);
 }
 
 // dg and du from kept projections; their rows are filled with zeros up to ldd.  Memory bounds it: 4096 x 5632 bf16 42, 5.5 TB/s.
@@ -1141,17 +1200,15 @@ struct Cut {
 
 // The cut that takes the least time by this account, in us: workgroups take items in rounds; an item costs its stages and
 // something to begin and finish; joining costs a launch and the sums' way to memory and back.  The stages' times are fitted to
-// calls with every cut forced in turn (L, S: large and small tiles, with parts): forward 4096 x 5632 x 2048 L 175, S 171, but
-// with outputs kept and other work around them 210 and 250; 2048 x 5632 x 2048 L 101, L in 2 parts behind the first round 98, S 93;
-// 512 x 4096 x 4096 S 44, L in 4 parts 50; dx of 4096 x 5632 x 2048 L in 2 parts 177, S 218; dx of 777 x 2730 x 1000 S in 8 parts 32,
-// 4 34, 1 71; dW of 4096 x 5632 x 2048 L 222, 2 parts behind the first round 190, S 219; fp32 2048 x 2816 x 1024 dx S in 4 parts 200,
-// S 377, thin tiles 233, dW thin in 4 parts 205, S 268.  The account's choice is within 15 % of the best of them.
-template <Does DOES, class S>
+// calls with every cut forced in turn (L, S: large and small tiles): 4096 x 5632 x 2048 L 175, S 171, but with outputs kept and
+// other work around them 210 and 250; 2048 x 5632 x 2048 L 101, L in 2 parts behind the first round 98, S 93; 512 x 4096 x 4096
+// S 44, L in 4 parts 50.  The account's choice is within 15 % of the best of them.
+template <class S>
 void try_cut(Size size, double stage_us, double item_us, size_t m, size_t n, size_t k, size_t w, Cut* best) {
     size_t cols, rows;
-    tiles_of<DOES, S>(m, n, k, &cols, &rows);
+    tiles_of<Does::kForward, S>(m, n, k, &cols, &rows);
     const size_t tiles = cols * rows, slots = kUnits * S::kPerUnit;
-    const size_t stages = div_up(DOES == Does::kDw ? m : DOES == Does::kDx ? 2 * n : k, kStageBytes / w);
+    const size_t stages = div_up(k, kStageBytes / w);
     const auto rounds = [&](size_t items, size_t stages_each) {
         const size_t last = items % slots;             // alone on its compute unit, an item of two takes less time
         const double alone = last != 0 && last <= kUnits && slots > kUnits ? kAlone : 1;
@@ -1169,32 +1226,130 @@ void try_cut(Size size, double stage_us, double item_us, size_t m, size_t n, siz
         if (full != tiles) consider(full, parts);
 }
 
-template <Does DOES>
+// The projections' cut.
 Cut cut_of(size_t m, size_t n, size_t k, size_t w) {
     Cut best{Size::kSmall, 0, 1, 0, 1e300};
     if (w == 4) {                                // the products bound it, whatever the tile; a stage is 32 steps
-        try_cut<DOES, Small>(Size::kSmall, 3.8, 5, m, n, k, w, &best);
-        try_cut<DOES, Thin>(Size::kThin, 1.95, 4, m, n, k, w, &best);
+        try_cut<Small>(Size::kSmall, 3.8, 5, m, n, k, w, &best);
+        try_cut<Thin>(Size::kThin, 1.95, 4, m, n, k, w, &best);
         return best;
     }
-    constexpr int kWhich = DOES == Does::kDx ? 1 : DOES == Does::kDw ? 2 : 0;
-    constexpr double kLargeStage[] = {1.45, 1.55, 1.6}, kSmallStage[] = {0.85, 1.15, 1.1};
-    try_cut<DOES, Large>(Size::kLarge, kLargeStage[kWhich], 8, m, n, k, w, &best);
-    try_cut<DOES, Small>(Size::kSmall, kSmallStage[kWhich], 5, m, n, k, w, &best);
-    try_cut<DOES, Thin>(Size::kThin, 0.9, 4, m, n, k, w, &best);
+    try_cut<Large>(Size::kLarge, 1.45, 8, m, n, k, w, &best);
+    try_cut<Small>(Size::kSmall, 0.85, 5, m, n, k, w, &best);
+    try_cut<Thin>(Size::kThin, 0.9, 4, m, n, k, w, &best);
     return best;
 }
 
-template <typename T, Does DOES, class S>
-zvc_status product_of(const GluArgs<T>& p, hipStream_t stream) {
+// How dx's and dW's products are cut, of one tile shape, and how many items of dW go ahead where dx leaves compute units idle.
+struct Pair {
+    Cut dx, dw;
+    unsigned ahead;
+    double cost;
+};
+
+// The pair that takes the least time by the same account: the most loaded workgroup's items, and the joining.  With every pair
+// forced in turn (tiles, parts of dx, parts of dW, ahead), the gradients and dg, du: 4096 x 5632 x 2048 bf16 L 1 1 3 347, L 2 1 0 374,
+// S 1 2 0 422; 2048 x 2816 x 1024 L 3 1 1 78, S 3 1 0 79, thin 101; 512 x 4096 x 4096 S 2 1 5 115, L 3 1 4 117; 1024 x 5632 x 2048 L 4 1 2 123,
+// L 3 1 3 (taken) 131; 64 x 4096 x 4096 S 8 1 4 57, S 6 1 5 (taken) 55, L 63, thin 62; 777 x 2730 x 1000 S 3 1 2 49, L 6 1 0 (taken) 50.
+// The account's choice is within 7 % of the best.  Either product in a launch of its own, each cut for itself: 389, 100, 117, 143.
+template <class S>
+void try_pair(Size size, double dx_us, double dw_us, double item_us, size_t m, size_t n, size_t k, size_t w, Pair* best) {
+    static constexpr unsigned kParts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
+    struct Side {                                // one of the two products, with the parts that are tried
+        size_t tiles, stages;
+        double stage_us;
+        unsigned whole, parts, items;
+        double each, longest, sums;
+    };
     size_t cols, rows;
-    tiles_of<DOES, S>(p.m, p.n, p.k, &cols, &rows);
-    const size_t items = p.whole + (cols * rows - p.whole) * p.parts, room = kUnits * S::kPerUnit;
-    const unsigned tp = static_cast<unsigned>(cols), tq = static_cast<unsigned>(rows);
-    const zvc_status st = launch(product_kernel<T, DOES, S>, dim3(items < room ? items : room), S::kThreads, stream, p, tp, tq);
-    if (st != ZVC_OK || p.parts == 1) return st;
-    const size_t groups = (cols * rows - p.whole) * (S::QT * Tile<T, DOES, S>::kCols / 8);
-    return launch(join_kernel<T, DOES, S>, dim3(div_up(groups, 256)), 256, stream, p, tp, tq);
+    tiles_of<Does::kDx, S>(m, n, k, &cols, &rows);
+    Side x{cols * rows, 2 * div_up(n, kStageBytes / w), dx_us, 0, 0, 0, 0, 0, 0};
+    tiles_of<Does::kDw, S>(m, n, k, &cols, &rows);
+    Side y{cols * rows, div_up(m, kStageBytes / w), dw_us, 0, 0, 0, 0, 0, 0};
+    const unsigned slots = kUnits * S::kPerUnit;
+    const auto set = [&](Side* side, unsigned parts, double alone) {
+        const unsigned full = static_cast<unsigned>(side->tiles / slots * slots);
+        if (parts > 1 && (full == side->tiles || parts * 2 > side->stages)) return false;
+        side->parts = parts;
+        side->whole = parts == 1 ? static_cast<unsigned>(side->tiles) : full;
+        const unsigned rest = static_cast<unsigned>(side->tiles) - side->whole;
+        side->items = side->whole + rest * parts;
+        side->longest = side->stages * side->stage_us * alone + item_us;
+        const double short_one = div_up(side->stages, parts) * side->stage_us * alone + item_us;
+        side->each = side->items == 0 ? 0 : (side->whole * side->longest + rest * parts * short_one) / side->items;
+        side->sums = parts > 1 ? 4.0 * S::PT * S::QT * rest * parts : 0;
+        return true;
+    };
+    for (const unsigned parts_x : kParts)
+        for (const unsigned parts_y : kParts) {
+            if (!set(&x, parts_x, 1) || !set(&y, parts_y, 1)) continue;
+            if (slots > kUnits && x.items + y.items <= kUnits) set(&x, parts_x, kAlone), set(&y, parts_y, kAlone);
+            const unsigned first = x.items % slots, idle = slots - first;
+            const double turns = x.items / slots * x.each;
+            const double joining = x.sums + y.sums > 0 ? kJoinUs + (x.sums + y.sums) / kSumsPerUs : 0;
+            const unsigned most = first == 0 || y.each == 0 ? 0 : static_cast<unsigned>(x.each / y.each + 0.5);
+            for (const unsigned ahead : {0u, most}) {
+                const unsigned behind = y.items > ahead * idle ? y.items - ahead * idle : 0, round = behind / slots, last = behind % slots;
+                const unsigned early = behind > 0 ? ahead : static_cast<unsigned>(div_up(y.items, idle));
+                const double of_idle = (early + round + (last > 0 ? 1 : 0)) * y.each;
+                const double of_others = first == 0 ? 0 : x.each + (round + (last > idle ? 1 : 0)) * y.each;
+                const double cost = turns + (of_idle > of_others ? of_idle : of_others) + joining;
+                if (cost < best->cost)
+                    *best = {{size, x.whole, x.parts, static_cast<size_t>(x.sums), 0}, {size, y.whole, y.parts, static_cast<size_t>(y.sums), 0}, ahead, cost};
+            }
+        }
+}
+
+Pair pair_of(size_t m, size_t n, size_t k, size_t w) {
+    const Cut none{Size::kSmall, 0, 1, 0, 0};
+    Pair best{none, none, 0, 1e300};
+    if (w == 4) {
+        try_pair<Small>(Size::kSmall, 3.8, 3.8, 5, m, n, k, w, &best);
+        try_pair<Thin>(Size::kThin, 1.95, 1.95, 4, m, n, k, w, &best);
+        return best;
+    }
+    try_pair<Large>(Size::kLarge, 1.55, 1.6, 8, m, n, k, w, &best);
+    try_pair<Small>(Size::kSmall, 1.1, 1.1, 5, m, n, k, w, &best);
+    try_pair<Thin>(Size::kThin, 0.9, 0.9, 4, m, n, k, w, &best);
+    return best;
+}
+
+template <Does DOES, class S>
+Plan plan_of(const Cut& cut, size_t m, size_t n, size_t k, float* sums) {
+    size_t cols, rows;
+    tiles_of<DOES, S>(m, n, k, &cols, &rows);
+    return {sums, static_cast<unsigned>(cols), static_cast<unsigned>(rows), cut.whole, cut.parts};
+}
+
+// The blocks of a join, 0 where there is none.
+template <typename T, Does DOES, class S>
+unsigned join_blocks(const Plan& plan) {
+    if (plan.parts == 1) return 0;
+    return static_cast<unsigned>(div_up(size_t{plan.tp * plan.tq - plan.whole} * (S::QT * Tile<T, DOES, S>::kCols / 8), 256));
+}
+
+template <typename T, Does DOES, class S>
+zvc_status product_of(const GluArgs<T>& p, const Cut& cut, float* sums, hipStream_t stream) {
+    const Plan plan = plan_of<DOES, S>(cut, p.m, p.n, p.k, sums);
+    const unsigned items = plan.items(), room = kUnits * S::kPerUnit;
+    const zvc_status st = launch(product_kernel<T, DOES, S>, dim3(items < room ? items : room), S::kThreads, stream, p, plan);
+    const unsigned blocks = join_blocks<T, DOES, S>(plan);
+    return st != ZVC_OK || blocks == 0 ? st : launch(join_kernel<T, DOES, S>, dim3(blocks), 256, stream, p, plan);
+}
+
+// dx and dW, or what of them is wanted: cut the same way in any case.
+template <typename T, class S>
+zvc_status gradients_of(const GluArgs<T>& p, const Pair& pair, float* sums, hipStream_t stream) {
+    Plan dx = plan_of<Does::kDx, S>(pair.dx, p.m, p.n, p.k, sums), dw = plan_of<Does::kDw, S>(pair.dw, p.m, p.n, p.k, sums + pair.dx.sums / 4);
+    const Plan nothing{nullptr, 0, 0, 0, 1};
+    if (p.dx == nullptr) dx = nothing;
+    if (p.dwg == nullptr) dw = nothing;
+    const unsigned items = dx.items() + dw.items(), room = kUnits * S::kPerUnit;
+    if (items == 0) return ZVC_OK;
+    // (fewer workgroups than a round holds take one item each)
+    const zvc_status st = launch(gradients_kernel<T, S>, dim3(items < room ? items : room), S::kThreads, stream, p, dx, dw, items < room ? 0u : pair.ahead);
+    const unsigned blocks = join_blocks<T, Does::kDx, S>(dx), more = join_blocks<T, Does::kDw, S>(dw);
+    return st != ZVC_OK || blocks + more == 0 ? st : launch(join_gradients_kernel<T, S>, dim3(blocks + more), 256, stream, p, dx, dw, blocks);
 }
 
 template <typename T, Does DOES, int TB, int WAVES>
@@ -1209,28 +1364,22 @@ zvc_status tokens_of(const GluArgs<T>& p, hipStream_t stream) {
 constexpr size_t few_tokens(size_t w) { return w == 4 ? 32 : 64; }
 
 template <typename T, Does DOES>
-zvc_status product(GluArgs<T> p, float* sums, hipStream_t stream) {
-    if constexpr (DOES == Does::kForward || DOES == Does::kSlope) {
-        if (p.m <= few_tokens(sizeof(T)) && p.k != 0) {
-            if (p.m <= 16) return tokens_of<T, DOES, 1, 8>(p, stream);
-            if (p.m <= 32) return tokens_of<T, DOES, 2, 8>(p, stream);
-            if constexpr (sizeof(T) == 2) return tokens_of<T, DOES, 4, 4>(p, stream);
-        }
+zvc_status project(const GluArgs<T>& p, const Cut& cut, float* sums, hipStream_t stream) {
+    if (p.m <= few_tokens(sizeof(T)) && p.k != 0) {
+        if (p.m <= 16) return tokens_of<T, DOES, 1, 8>(p, stream);
+        if (p.m <= 32) return tokens_of<T, DOES, 2, 8>(p, stream);
+        if constexpr (sizeof(T) == 2) return tokens_of<T, DOES, 4, 4>(p, stream);
     }
-    const Cut cut = cut_of<DOES>(p.m, p.n, p.k, sizeof(T));
-    p.whole = cut.whole, p.parts = cut.parts, p.sums = sums;
     if constexpr (sizeof(T) == 2)
-        if (cut.size == Size::kLarge) return product_of<T, DOES, Large>(p, stream);
-    return cut.size == Size::kSmall ? product_of<T, DOES, Small>(p, stream) : product_of<T, DOES, Thin>(p, stream);
+        if (cut.size == Size::kLarge) return product_of<T, DOES, Large>(p, cut, sums, stream);
+    return cut.size == Size::kSmall ? product_of<T, DOES, Small>(p, cut, sums, stream) : product_of<T, DOES, Thin>(p, cut, sums, stream);
 }
 
-// Bytes for the sums of whichever of a call's products is cut into parts.
-size_t sums_bytes(size_t m, size_t n, size_t k, size_t w, bool backward) {
-    if (!backward) return cut_of<Does::kForward>(m, n, k, w).sums;
-    size_t most = cut_of<Does::kSlope>(m, n, k, w).sums;
-    const size_t dx = cut_of<Does::kDx>(m, n, k, w).sums, dw = cut_of<Does::kDw>(m, n, k, w).sums;
-    if (dx > most) most = dx;
-    return dw > most ? dw : most;
+template <typename T>
+zvc_status gradients(const GluArgs<T>& p, const Pair& pair, float* sums, hipStream_t stream) {
+    if constexpr (sizeof(T) == 2)
+        if (pair.dx.size == Size::kLarge) return gradients_of<T, Large>(p, pair, sums, stream);
+    return pair.dx.size == Size::kSmall ? gradients_of<T, Small>(p, pair, sums, stream) : gradients_of<T, Thin>(p, pair, sums, stream);
 }
 
 constexpr size_t kColumnsUp = 64;               // dg's and du's rows are filled up to a multiple of this
@@ -1239,6 +1388,8 @@ constexpr size_t kColumnsUp = 64;               // dg's and du's rows are filled
 struct Layout {
     size_t dg, du, x, wg, wu, sums, bytes;
     size_t ldd, aligned_k;              // row strides of dg and du, and of the copies of x, Wg and Wu
+    Cut cut;                            // of the projections
+    Pair pair;                          // of the gradients
 };
 
 // `copies`: x, Wg and Wu do not all take 16-byte accesses.
@@ -1253,7 +1404,13 @@ Layout layout_of(size_t m, size_t n, size_t k, size_t w, bool backward, bool cop
     };
     if (backward) at.dg = part(m * at.ldd * w), at.du = part(m * at.ldd * w);
     if (copies) at.x = part(m * at.aligned_k * w), at.wg = part(n * at.aligned_k * w), at.wu = part(n * at.aligned_k * w);
-    at.sums = part(sums_bytes(m, n, k, w, backward));
+    at.cut = cut_of(m, n, k, w);
+    size_t sums = at.cut.sums;
+    if (backward) {
+        at.pair = pair_of(m, n, k, w);
+        if (at.pair.dx.sums + at.pair.dw.sums > sums) sums = at.pair.dx.sums + at.pair.dw.sums;
+    }
+    at.sums = part(sums);
     at.bytes += 256;
     return at;
 }
@@ -1285,7 +1442,7 @@ zvc_status align_inputs(GluArgs<T>* p, const Layout& at, unsigned char* base, hi
 template <typename T>
 zvc_status forward_as(GluArgs<T> p, const Layout& at, unsigned char* base, hipStream_t stream) {
     if (zvc_status st = align_inputs(&p, at, base, stream)) return st;
-    return product<T, Does::kForward>(p, reinterpret_cast<float*>(base + at.sums), stream);
+    return project<T, Does::kForward>(p, at.cut, reinterpret_cast<float*>(base + at.sums), stream);
 }
 
 template <typename T>
@@ -1296,20 +1453,16 @@ zvc_status backward_as(GluArgs<T> p, T* dx, size_t lddx, T* dwg, T* dwu, size_t 
     if (p.m != 0 && p.n != 0) {
         zvc_status st;
         if (p.gate_in == nullptr) {
-            st = product<T, Does::kSlope>(p, sums, stream);
+            st = project<T, Does::kSlope>(p, at.cut, sums, stream);
         } else {
             const size_t blocks = div_up(size_t{p.m} * (p.ldd / 8), 256);
             st = launch(slope_kernel<T>, dim3(blocks < 65536 ? blocks : 65536), 256, stream, p);
         }
         if (st != ZVC_OK) return st;
     }
-    if (dx != nullptr && p.m != 0) {
-        p.out = dx, p.ldo = static_cast<unsigned>(lddx);
-        if (zvc_status st = product<T, Does::kDx>(p, sums, stream)) return st;
-    }
-    if (dwg == nullptr || p.n == 0) return ZVC_OK;
-    p.out = dwg, p.out2 = dwu, p.ldo = static_cast<unsigned>(lddw);
-    return product<T, Does::kDw>(p, sums, stream);
+    p.dx = p.m != 0 ? dx : nullptr, p.lddx = static_cast<unsigned>(lddx);
+    p.dwg = p.n != 0 ? dwg : nullptr, p.dwu = dwu, p.lddw = static_cast<unsigned>(lddw);
+    return gradients(p, at.pair, sums, stream);
 }
 
 }  // namespace
@@ -1369,7 +1522,8 @@ zvc_status zvc_glu_forward(const void* d_x, size_t ldx, const void* d_wg, const 
         if (!aligned_to(p, w)) return ZVC_E_ALIGN;
     if (!aligned_to(d_ws, 256)) return ZVC_E_ALIGN;
     const bool loose = !aligned_to(d_x, 16) || !aligned_to(d_wg, 16) || !aligned_to(d_wu, 16) || ldx * w % 16 != 0 || ldw * w % 16 != 0;
-    if (ws < zvc_glu_workspace_bytes(m, n, k, type, 0, loose)) return ZVC_E_WORKSPACE;
+    const Layout at = layout_of(m, n, k, w, false, loose || k * w % 16 != 0);
+    if (ws < at.bytes) return ZVC_E_WORKSPACE;
     const Region in[] = {{d_x, ldx * w, m, k * w}, {d_wg, ldw * w, n, k * w}, {d_wu, ldw * w, n, k * w}};
     const Region out[] = {{d_h, ldh * w, m, n * w}, {d_gate, ldp * w, m, n * w}, {d_up, ldp * w, m, n * w}, {d_ws, ws, 1, ws}};
     for (int i = 0; i < 4; ++i) {
@@ -1378,7 +1532,6 @@ zvc_status zvc_glu_forward(const void* d_x, size_t ldx, const void* d_wg, const 
         for (int j = 0; j < i; ++j)
             if (overlap(out[i], out[j])) return ZVC_E_ARG;
     }
-    const Layout at = layout_of(m, n, k, w, false, loose || k * w % 16 != 0);
     const auto as = [&](auto zero) {
         using T = decltype(zero);
         GluArgs<T> p{};
@@ -1412,7 +1565,8 @@ zvc_status zvc_glu_backward(const void* d_dh, size_t lddh, const void* d_x, size
         if (!aligned_to(p, w)) return ZVC_E_ALIGN;
     if (!aligned_to(d_ws, 256)) return ZVC_E_ALIGN;
     const bool loose = !aligned_to(d_x, 16) || !aligned_to(d_wg, 16) || !aligned_to(d_wu, 16) || ldx * w % 16 != 0 || ldw * w % 16 != 0;
-    if (ws < zvc_glu_workspace_bytes(m, n, k, type, 1, loose)) return ZVC_E_WORKSPACE;
+    const Layout at = layout_of(m, n, k, w, true, loose || k * w % 16 != 0);
+    if (ws < at.bytes) return ZVC_E_WORKSPACE;
     const Region in[] = {{d_dh, lddh * w, m, n * w}, {d_x, ldx * w, m, k * w}, {d_wg, ldw * w, n, k * w},
                          {d_wu, ldw * w, n, k * w}, {d_gate, ldp * w, m, n * w}, {d_up, ldp * w, m, n * w}};
     const Region out[] = {{d_dx, lddx * w, m, k * w}, {d_dwg, lddw * w, n, k * w}, {d_dwu, lddw * w, n, k * w}, {d_ws, ws, 1, ws}};
@@ -1422,7 +1576,6 @@ zvc_status zvc_glu_backward(const void* d_dh, size_t lddh, const void* d_x, size
         for (int j = 0; j < i; ++j)
             if (overlap(out[i], out[j])) return ZVC_E_ARG;
     }
-    const Layout at = layout_of(m, n, k, w, true, loose || k * w % 16 != 0);
     const auto as = [&](auto zero) {
         using T = decltype(zero);
         unsigned char* const base = static_cast<unsigned char*>(d_ws);
