@@ -5,7 +5,7 @@
 //   * product_kernel, gradients_kernel: the large products (both projections with what becomes of them; dx with dWg and dWu),
 //     tiles on the matrix cores, staged from memory straight to LDS, with the activation, dropout and the kept projections, or
 //     their gradients, in the tile's epilogue.  Sums too long for the few tiles there are are cut into parts that a join adds.
-//   * token_kernel: the projections of up to 64 tokens, bound by reading the weights once.
+//   * token_kernel: the projections of up to 128 tokens, bound by reading the weights once.
 //   * slope_kernel: dg and du from kept projections; align_kernel: copies of inputs that do not take 16-byte accesses.
 //
 // Times in the comments are us on one MI355X, where a large copy moves 5.0 TB/s and a large bf16 product of the vendor's library
@@ -26,7 +26,7 @@ namespace {
 using bf16 = __bf16;
 using fp16 = _Float16;
 
-inline size_t div_up(size_t a, size_t b) { return (a + b - 1) / b; }
+__host__ __device__ inline size_t div_up(size_t a, size_t b) { return (a + b - 1) / b; }
 inline size_t round_up(size_t a, size_t b) { return div_up(a, b) * b; }
 
 // ------------------------------------------------------------------ dropout
@@ -362,6 +362,7 @@ template <int LEFT>
 __device__ __forceinline__ void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
 }
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void group_barrier() {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
@@ -935,75 +936,19 @@ __device__ __forceinline__ void finish_group(const GluArgs<T>& p, unsigned row, 
 }
 
 // ------------------------------------------------------------------ few tokens
-// The projections of up to 16 TB tokens.  Every weight is read once and used for all of them, so this is a matter of reading the
-// weights (11264 x 4096, bf16, one token: 32.8, 5.6 TB/s): straight into registers, 128 neighbouring bytes of 32 rows at a time and
-// wave, all of a batch before the first is used (without that 37.3).  A workgroup takes 16 columns of both
-// weights, its WAVES waves take turns along k and their sums meet in LDS.  Workgroups begin at different places along k:
-// rows lie a power of two apart, and the same place in all of them is in few of the memory's channels (without that 35.8).
-// With 64 tokens x takes the longer way: every workgroup reads all of it.
+constexpr int kTokenCols = 16;                  // columns of both weights that a workgroup takes
+
+// The waves' sums of a workgroup's 16 columns of both projections, joined in `sums` in the order of the waves, and what becomes of them.
 template <typename T, Does DOES, int TB, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void token_kernel(GluArgs<T> p) {
-    constexpr int W = sizeof(T), kChunk = 16 / W, kSpan = 128 / W;       // elements of 16 and of 128 bytes
-    constexpr int kBatch = TB == 1 ? 4 : 2;                              // spans on their way together
-    constexpr int kCols = 16, kFrom = 2 + TB;
-    using Frag = typename Fragment<T>::type;
-    __shared__ float4v sums[WAVES][2][TB * 16][kCols / 4];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, quarter = lane >> 4;
-    const unsigned col0 = blockIdx.x * kCols;
-    // (rows and tokens that are not there: the last one again, and what comes of it is left out)
-    const unsigned row = col0 + r < p.n ? col0 + r : p.n - 1;
-    const T* from[kFrom] = {cell(p.wg, row, p.ldw, quarter * kChunk), cell(p.wu, row, p.ldw, quarter * kChunk)};
-#pragma unroll
-    for (int t = 0; t < TB; ++t) {
-        const unsigned at = t * 16 + r, token = at < p.m ? at : p.m - 1;
-        from[2 + t] = cell(p.x, token, p.ldx, quarter * kChunk);
-    }
-    float4v acc[2][TB];
-#pragma unroll
-    for (int t = 0; t < TB; ++t) acc[0][t] = acc[1][t] = float4v{0.f, 0.f, 0.f, 0.f};
-    const auto take = [&](const Frag (&f)[kFrom]) {
-#pragma unroll
-        for (int t = 0; t < TB; ++t)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) acc[c][t] = multiply(f[c], f[2 + t], acc[c][t]);
-    };
-    const unsigned spans = p.k / kSpan, start = spans != 0 ? blockIdx.x * 29 % spans : 0;
-    const auto turn = [&](unsigned span) { return span + start < spans ? span + start : span + start - spans; };
-    unsigned span = wave;
-    for (; span + (kBatch - 1) * WAVES < spans; span += kBatch * WAVES) {
-        Frag f[kBatch][2][kFrom];
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i)
-#pragma unroll
-            for (int o = 0; o < kFrom; ++o)
-#pragma unroll
-                for (int half = 0; half < 2; ++half)
-                    f[i][half][o] = *reinterpret_cast<const Frag*>(from[o] + turn(span + i * WAVES) * kSpan + half * (kSpan / 2));
-        __builtin_amdgcn_sched_barrier(0);                               // (all of them before the first is used)
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) take(f[i][0]), take(f[i][1]);
-    }
-    for (; span * kSpan < p.k; span += WAVES) {                          // (k is whole chunks)
-        const unsigned first = (span < spans ? turn(span) : span) * kSpan;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            Frag f[kFrom];
-            const unsigned at = first + half * (kSpan / 2);
-#pragma unroll
-            for (int o = 0; o < kFrom; ++o) {
-                f[o] = Frag{};
-                if (at + quarter * kChunk < p.k) f[o] = *reinterpret_cast<const Frag*>(from[o] + at);
-            }
-            take(f);
-        }
-    }
+__device__ __forceinline__ void finish_tokens(const GluArgs<T>& p, unsigned col0, int lane, int wave, float4v (*sums)[2][TB * 16][4], const float4v (&acc)[2][TB]) {
+    const int r = lane & 15, quarter = lane >> 4;
 #pragma unroll
     for (int t = 0; t < TB; ++t)
 #pragma unroll
         for (int c = 0; c < 2; ++c) sums[wave][c][t * 16 + r][quarter] = acc[c][t];
     __syncthreads();
     float4v* const flat = &sums[0][0][0][0];
-    constexpr int kFlat = 2 * TB * 16 * kCols / 4;
+    constexpr int kFlat = 2 * TB * 16 * kTokenCols / 4;
     for (int i = threadIdx.x; i < kFlat; i += 64 * WAVES) {
         float4v sum = flat[i];
 #pragma unroll
@@ -1011,7 +956,7 @@ __global__ __launch_bounds__(64 * WAVES) void token_kernel(GluArgs<T> p) {
         flat[i] = sum;
     }
     __syncthreads();
-    constexpr int kGroups = kCols / 8;
+    constexpr int kGroups = kTokenCols / 8;
     static_assert(TB * 16 * kGroups <= 64 * WAVES, "a lane for each group of eight columns");
     const unsigned token = threadIdx.x / kGroups, group = threadIdx.x % kGroups, col = col0 + group * 8;
     if (token >= p.m || token >= TB * 16 || col >= (DOES == Does::kSlope ? p.ldd : p.n)) return;
@@ -1019,6 +964,75 @@ __global__ __launch_bounds__(64 * WAVES) void token_kernel(GluArgs<T> p) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) g.v[e] = sums[0][0][token][group * 2 + e / 4][e % 4], u.v[e] = sums[0][1][token][group * 2 + e / 4][e % 4];
     finish_group<T, DOES>(p, token, col, g, u);
+}
+
+// The projections of up to 16 TB tokens.  Every weight is read once and used for all of them, so this is a matter of reading the
+// weights.  A workgroup takes 16 columns of both; its WAVES waves take turns along the reduction, 128 bytes of it at a time, and
+// their sums meet in LDS.  Each wave stages its own turns' rows, RING of them on their way at a time, and reads them back as the
+// matrix instructions want them: no wave waits for another.  (Read straight into registers, neighbouring lanes want rows that
+// lie apart, and a compute unit gets 14 bytes a cycle: 64 tokens, n = k = 4096, 25.6 | 19.2 so; 11264 x 4096 68 | 48.)  Workgroups
+// begin at different places along the reduction: rows lie a power of two apart, and the same place in all of them is in few of
+// the memory's channels.  Weights from memory, bf16: 11264 x 4096 one token 31.5 (5.9 TB/s), 16 tokens 33.4, 32 tokens 38.2.
+// Every workgroup reads all of x, from the caches: with 64 tokens twice what it reads of the weights.
+template <typename T, Does DOES, int TB, int WAVES, int RING>
+__global__ __launch_bounds__(64 * WAVES) void token_kernel(GluArgs<T> p) {
+    constexpr int W = sizeof(T), kSpan = kStageBytes / W, kStage = (2 * 16 + TB * 16) * kStageBytes;
+    using InW = Operand<T, Lies::kAlong, 16, 1, false>;
+    using InX = Operand<T, Lies::kAlong, TB * 16, 1, false>;
+    using ReadW = Reader<T, Lies::kAlong, 32, 2, false>;
+    using ReadX = Reader<T, Lies::kAlong, TB * 16, TB, false>;
+    constexpr int kLoads = 2 * InW::kLoads + InX::kLoads;
+    __shared__ alignas(1024) unsigned char lds[WAVES * RING * kStage];
+    static_assert(sizeof lds >= sizeof(float4v[WAVES][2][TB * 16][4]), "the sums take the stages' place");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned col0 = blockIdx.x * kTokenCols;
+    const unsigned base = static_cast<unsigned>(reinterpret_cast<uintptr_t>((LdsByte*)lds)) + wave * (RING * kStage);
+    InW in_w;
+    InX in_x;
+    in_w.init(0, lane, p.ldw, col0 < p.n ? p.n - col0 : 0);
+    in_x.init(0, lane, p.ldx, p.m);
+    ReadW read_w;
+    ReadX read_x;
+    read_w.init(base, 0, lane);
+    read_x.init(base + 32 * kStageBytes, 0, lane);
+    const unsigned spans = static_cast<unsigned>(div_up(p.k, kSpan)), start = blockIdx.x * 29 % spans;
+    const unsigned mine = static_cast<unsigned>(wave) < spans ? (spans - 1 - wave) / WAVES + 1 : 0;
+    const uint64_t wg = reinterpret_cast<uint64_t>(cell(p.wg, col0, p.ldw, 0)), wu = reinterpret_cast<uint64_t>(cell(p.wu, col0, p.ldw, 0));
+    const auto fetch = [&](unsigned i) {
+        const unsigned turn = wave + i * WAVES + start, t = (turn < spans ? turn : turn - spans) * kSpan, to = base + i % RING * kStage;
+        const int left = p.k - t;
+        in_w.fetch(wg + t * W, 0, left, to);
+        in_w.fetch(wu + t * W, 0, left, to + 16 * kStageBytes);
+        in_x.fetch(reinterpret_cast<uint64_t>(p.x) + t * W, 0, left, to + 32 * kStageBytes);
+    };
+    float4v acc[2][TB];
+#pragma unroll
+    for (int t = 0; t < TB; ++t) acc[0][t] = acc[1][t] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (unsigned i = 0; i < RING; ++i)
+        if (i < mine) fetch(i);
+    for (unsigned i = 0; i < mine; ++i) {
+        if (i + RING <= mine) wait_loads<(RING - 1) * kLoads>();
+        else wait_loads<0>();
+        const unsigned stage = i % RING * kStage;
+        typename Fragment<T>::type f[2][2 + TB];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            f[half][0] = read_w.read(0, half, stage), f[half][1] = read_w.read(1, half, stage);
+#pragma unroll
+            for (int t = 0; t < TB; ++t) f[half][2 + t] = read_x.read(t, half, stage);
+        }
+        wait_reads();                                                    // before their place is written again
+        if (i + RING < mine) fetch(i + RING);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int t = 0; t < TB; ++t)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) acc[c][t] = multiply(f[half][c], f[half][2 + t], acc[c][t]);
+    }
+    __syncthreads();
+    finish_tokens<T, DOES, TB, WAVES>(p, col0, lane, wave, reinterpret_cast<float4v(*)[2][TB * 16][4]>(lds), acc);
 }
 
 // The parts' sums of the tiles that are summed in parts, joined in the order of the parts.  A lane takes eight neighbouring columns.
@@ -1352,23 +1366,32 @@ zvc_status gradients_of(const GluArgs<T>& p, const Pair& pair, float* sums, hipS
     return st != ZVC_OK || blocks + more == 0 ? st : launch(join_gradients_kernel<T, S>, dim3(blocks + more), 256, stream, p, dx, dw, blocks);
 }
 
-template <typename T, Does DOES, int TB, int WAVES>
+template <typename T, Does DOES, int TB, int WAVES, int RING>
 zvc_status tokens_of(const GluArgs<T>& p, hipStream_t stream) {
     const size_t cols = DOES == Does::kSlope ? p.ldd : p.n;
-    return launch(token_kernel<T, DOES, TB, WAVES>, dim3(div_up(cols, 16)), 64 * WAVES, stream, p);
+    return launch(token_kernel<T, DOES, TB, WAVES, RING>, dim3(div_up(cols, kTokenCols)), 64 * WAVES, stream, p);
 }
 
-// The most tokens that take the kernel for few of them.  us (weights from memory), tiles | that kernel: bf16 n = k = 4096, 1 token
-// 22.6 | 14.2, 16 tokens 22.9 | 15.0, 32 23.1 | 18.7, 64 27.0 | 25.8; n = 11264, 1 token 45.6 | 32.8, 64 tokens 64 | 68;
-// fp32 n = k = 4096, 1 token 40.6 | 26.0, 32 40.9 | 38.8, and from there on the products bound it, 40 at n = 11264 121 | 156.
-constexpr size_t few_tokens(size_t w) { return w == 4 ? 32 : 64; }
+// Whether m tokens take the kernel for few of them.  us (weights from memory), tiles | that kernel: bf16 n = k = 4096, 1 token
+// 22.6 | 13.2, 32 23.1 | 14.7, 64 27.0 | 19.2, 96 30.8 | 23.1, 128 31.3 | 26.7; 11264 x 4096, 1 token 45.6 | 31.5, 64 64 | 48, 96 65.6 | 60.8,
+// 128 67.9 | 71.3; 2816 x 1024, 96 13.5 | 7.7, 128 14.1 | 9.3; 5632 x 2048, 128 27.3 | 28.7.  fp32, where the products come in sooner:
+// n = k = 4096, 32 tokens 38.9 | 29, 48 48.7 | 39; 11264 x 4096, 48 122 | 109, 64 126 | 134; 2816 x 1024, 64 18.3 | 14.5.  So the
+// largest counts only where every workgroup has a compute unit of its own.
+bool few_tokens(size_t m, size_t n, size_t w) { return m <= (w == 4 ? 48 : 96) || (m <= (w == 4 ? 64 : 128) && n <= kUnits * kTokenCols); }
 
 template <typename T, Does DOES>
 zvc_status project(const GluArgs<T>& p, const Cut& cut, float* sums, hipStream_t stream) {
-    if (p.m <= few_tokens(sizeof(T)) && p.k != 0) {
-        if (p.m <= 16) return tokens_of<T, DOES, 1, 8>(p, stream);
-        if (p.m <= 32) return tokens_of<T, DOES, 2, 8>(p, stream);
-        if constexpr (sizeof(T) == 2) return tokens_of<T, DOES, 4, 4>(p, stream);
+    if (p.k != 0 && few_tokens(p.m, p.n, sizeof(T))) {
+        // (waves and ring: most of LDS, as one workgroup or as two of which one reads while the other finishes.  11264 x 4096 bf16, 16 tokens
+        // 4 x 3 33.4, 8 x 3 36.6, 4 x 6 36.9; 32: 4 x 2 38.2, 4 x 3 40.6, 8 x 2 40.7, 2 x 4 44.2; 64: 3 x 2 48.4, 4 x 3 50, 6 x 2 51.7, 2 x 3 56)
+        if (p.m <= 16) return tokens_of<T, DOES, 1, 4, 3>(p, stream);
+        if (p.m <= 32) return tokens_of<T, DOES, 2, 4, 2>(p, stream);
+        if (p.m <= 48) return tokens_of<T, DOES, 3, 4, 2>(p, stream);
+        if constexpr (sizeof(T) == 2) {
+            if (p.m <= 64) return tokens_of<T, DOES, 4, 3, 2>(p, stream);
+            return p.m <= 96 ? tokens_of<T, DOES, 6, 4, 2>(p, stream) : tokens_of<T, DOES, 8, 4, 2>(p, stream);
+        }
+        return tokens_of<T, DOES, 4, 4, 3>(p, stream);
     }
     if constexpr (sizeof(T) == 2)
         if (cut.size == Size::kLarge) return product_of<T, DOES, Large>(p, cut, sums, stream);

@@ -192,6 +192,17 @@ def test_block_sizes(m, n, k, dtype):
         check_block(m, n, k, dtype, name, keep, {"p": p, "seed": 3, "offset": 4})
 
 
+@pytest.mark.parametrize("m", [1, 16, 17, 32, 33, 48, 49, 64, 65, 96, 97, 128, 129])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_block_few_tokens(m, dtype):
+    """Around every number of tokens at which another kernel takes over; sums of less than 128 bytes, of a few times that and
+    of many, with and without a rest; more columns than a workgroup for each compute unit takes."""
+    for n, k in ((24, 8), (40, 136), (264, 1032), (4104, 72)):
+        check_block(m, n, k, dtype, "silu", m % 2 == 0, {"p": 0.1, "seed": m})
+        if k <= 136:
+            check_block(m, n, k, dtype, "relu", m % 2 == 1, {"p": 0.0})
+
+
 @pytest.mark.parametrize("name", ACTS)
 @pytest.mark.parametrize("keep", [False, True])
 @pytest.mark.parametrize("p", [0.0, 0.25, 0.1, 1.0])
