@@ -1188,6 +1188,8 @@ bool stride_ok(size_t ld, size_t cols) { return ld >= cols && ld <= ZVC_FFN_MAX_
 using Large = Shape<4, 2, 4, 8, 2>;             // 256 x 256, eight waves
 using Small = Shape<2, 2, 4, 4, 2>;             // 128 x 128, four waves
 using Thin = Shape<4, 1, 4, 2, 2>;              // 256 x 32, four waves: few tokens
+using Lone = Shape<2, 4, 4, 2, 4>;              // 128 x 128, eight waves, alone on a compute unit: a deeper ring
+using Half = Shape<2, 2, 4, 2, 4>;              // 128 x 64, four waves, the same
 
 constexpr unsigned kUnits = 256;                // compute units
 constexpr double kAlone = 0.6;                  // a stage's time where one workgroup has a compute unit that takes two
@@ -1201,7 +1203,7 @@ void tiles_of(size_t m, size_t n, size_t k, size_t* cols, size_t* rows) {
     *rows = DOES == Does::kDw ? 2 * div_up(n, S::QT) : div_up(m, S::QT);
 }
 
-enum class Size { kLarge, kSmall, kThin };
+enum class Size { kLarge, kSmall, kThin, kLone, kHalf };
 
 // How a product is cut: the tiles' shape, how many tiles are summed whole, and in how many parts of the reduction the others are,
 // to be joined by a second kernel.
@@ -1215,8 +1217,10 @@ struct Cut {
 // The cut that takes the least time by this account, in us: workgroups take items in rounds; an item costs its stages and
 // something to begin and finish; joining costs a launch and the sums' way to memory and back.  The stages' times are fitted to
 // calls with every cut forced in turn (L, S: large and small tiles): 4096 x 5632 x 2048 L 175, S 171, but with outputs kept and
-// other work around them 210 and 250; 2048 x 5632 x 2048 L 101, L in 2 parts behind the first round 98, S 93; 512 x 4096 x 4096
-// S 44, L in 4 parts 50.  The account's choice is within 15 % of the best of them.
+// other work around them 210 and 250; 2048 x 5632 x 2048 L 101, L in 2 parts behind the first round 98, S 93.  The account's choice
+// is within 15 % of the best of them.  Where the tiles are one round or less, a workgroup alone on a compute unit hides memory's
+// latency by a deeper ring: 512 x 4096 x 4096 128 x 128 tiles 42.6 (small 60), 128 x 64 68; 256 x 4096 x 4096 35.3 (43), 128 x 64 33.3;
+// 256 x 2816 x 1024 11.8 (14.3), 128 x 64 11.0; 128 x 11264 x 4096 50.3 (66); but 1024 x 4096 x 4096 78 (73) and 777 x 2730 x 1000 26 (23).
 template <class S>
 void try_cut(Size size, double stage_us, double item_us, size_t m, size_t n, size_t k, size_t w, Cut* best) {
     size_t cols, rows;
@@ -1251,6 +1255,8 @@ Cut cut_of(size_t m, size_t n, size_t k, size_t w) {
     try_cut<Large>(Size::kLarge, 1.45, 8, m, n, k, w, &best);
     try_cut<Small>(Size::kSmall, 0.85, 5, m, n, k, w, &best);
     try_cut<Thin>(Size::kThin, 0.9, 4, m, n, k, w, &best);
+    try_cut<Lone>(Size::kLone, 0.45, 5, m, n, k, w, &best);
+    try_cut<Half>(Size::kHalf, 0.32, 4, m, n, k, w, &best);
     return best;
 }
 
@@ -1373,11 +1379,11 @@ zvc_status tokens_of(const GluArgs<T>& p, hipStream_t stream) {
 }
 
 // Whether m tokens take the kernel for few of them.  us (weights from memory), tiles | that kernel: bf16 n = k = 4096, 1 token
-// 22.6 | 13.2, 32 23.1 | 14.7, 64 27.0 | 19.2, 96 30.8 | 23.1, 128 31.3 | 26.7; 11264 x 4096, 1 token 45.6 | 31.5, 64 64 | 48, 96 65.6 | 60.8,
-// 128 67.9 | 71.3; 2816 x 1024, 96 13.5 | 7.7, 128 14.1 | 9.3; 5632 x 2048, 128 27.3 | 28.7.  fp32, where the products come in sooner:
-// n = k = 4096, 32 tokens 38.9 | 29, 48 48.7 | 39; 11264 x 4096, 48 122 | 109, 64 126 | 134; 2816 x 1024, 64 18.3 | 14.5.  So the
-// largest counts only where every workgroup has a compute unit of its own.
-bool few_tokens(size_t m, size_t n, size_t w) { return m <= (w == 4 ? 48 : 96) || (m <= (w == 4 ? 64 : 128) && n <= kUnits * kTokenCols); }
+// 22.6 | 13.2, 32 23.1 | 14.7, 64 22.7 | 19.6, 96 28.1 | 22.9, 128 28.6 | 26.6; 11264 x 4096, 1 token 45.6 | 31.5, 48 42.7 | 42.5,
+// 64 42.8 | 48.5, 96 46.8 | 60.6; 5632 x 2048, 64 19.5 | 18.6, 96 19.3 | 23.9; 2816 x 1024, 96 10.6 | 7.8, 128 10.6 | 9.4.  fp32, where
+// the products come in sooner: n = k = 4096, 32 tokens 38.9 | 29, 48 48.7 | 39; 11264 x 4096, 48 122 | 109, 64 126 | 134; 2816 x 1024,
+// 64 18.3 | 14.5.  So more than 48 only where every workgroup has a compute unit of its own.
+bool few_tokens(size_t m, size_t n, size_t w) { return m <= 48 || (m <= (w == 4 ? 64 : 128) && n <= kUnits * kTokenCols); }
 
 template <typename T, Does DOES>
 zvc_status project(const GluArgs<T>& p, const Cut& cut, float* sums, hipStream_t stream) {
@@ -1393,8 +1399,11 @@ zvc_status project(const GluArgs<T>& p, const Cut& cut, float* sums, hipStream_t
         }
         return tokens_of<T, DOES, 4, 4, 3>(p, stream);
     }
-    if constexpr (sizeof(T) == 2)
+    if constexpr (sizeof(T) == 2) {
         if (cut.size == Size::kLarge) return product_of<T, DOES, Large>(p, cut, sums, stream);
+        if (cut.size == Size::kLone) return product_of<T, DOES, Lone>(p, cut, sums, stream);
+        if (cut.size == Size::kHalf) return product_of<T, DOES, Half>(p, cut, sums, stream);
+    }
     return cut.size == Size::kSmall ? product_of<T, DOES, Small>(p, cut, sums, stream) : product_of<T, DOES, Thin>(p, cut, sums, stream);
 }
 
