@@ -1187,6 +1187,9 @@ bool stride_ok(size_t ld, size_t cols) { return ld >= cols && ld <= ZVC_FFN_MAX_
 
 using Large = Shape<4, 2, 4, 8, 2>;             // 256 x 256, eight waves
 using Small = Shape<2, 2, 4, 4, 2>;             // 128 x 128, four waves
+// The same for projections, of eight waves, among which an epilogue's long functions hide better: 777 x 2730 x 1000 fp16 with gelu
+// 23.2 -> 21.8, computed again for its gradients 66.0 -> 63.4; with short functions, larger or in fp32 the same within 1 %.
+using Eights = Shape<2, 4, 4, 2, 2>;
 using Thin = Shape<4, 1, 4, 2, 2>;              // 256 x 32, four waves: few tokens
 using Lone = Shape<2, 4, 4, 2, 4>;              // 128 x 128, eight waves, alone on a compute unit: a deeper ring
 using Half = Shape<2, 2, 4, 2, 4>;              // 128 x 64, four waves, the same
@@ -1216,7 +1219,7 @@ struct Cut {
 
 // The cut that takes the least time by this account, in us: workgroups take items in rounds; an item costs its stages and
 // something to begin and finish; joining costs a launch and the sums' way to memory and back.  The stages' times are fitted to
-// calls with every cut forced in turn (L, S: large and small tiles): 4096 x 5632 x 2048 L 175, S 171, but with outputs kept and
+// calls with every cut forced in turn (L, S: large and small tiles, S of four waves): 4096 x 5632 x 2048 L 175, S 171, but with outputs kept and
 // other work around them 210 and 250; 2048 x 5632 x 2048 L 101, L in 2 parts behind the first round 98, S 93.  The account's choice
 // is within 15 % of the best of them.  Where the tiles are one round or less, a workgroup alone on a compute unit hides memory's
 // latency by a deeper ring: 512 x 4096 x 4096 128 x 128 tiles 42.6 (small 60), 128 x 64 68; 256 x 4096 x 4096 35.3 (43), 128 x 64 33.3;
@@ -1248,12 +1251,12 @@ void try_cut(Size size, double stage_us, double item_us, size_t m, size_t n, siz
 Cut cut_of(size_t m, size_t n, size_t k, size_t w) {
     Cut best{Size::kSmall, 0, 1, 0, 1e300};
     if (w == 4) {                                // the products bound it, whatever the tile; a stage is 32 steps
-        try_cut<Small>(Size::kSmall, 3.8, 5, m, n, k, w, &best);
+        try_cut<Eights>(Size::kSmall, 3.8, 5, m, n, k, w, &best);
         try_cut<Thin>(Size::kThin, 1.95, 4, m, n, k, w, &best);
         return best;
     }
     try_cut<Large>(Size::kLarge, 1.45, 8, m, n, k, w, &best);
-    try_cut<Small>(Size::kSmall, 0.85, 5, m, n, k, w, &best);
+    try_cut<Eights>(Size::kSmall, 0.85, 5, m, n, k, w, &best);
     try_cut<Thin>(Size::kThin, 0.9, 4, m, n, k, w, &best);
     try_cut<Lone>(Size::kLone, 0.45, 5, m, n, k, w, &best);
     try_cut<Half>(Size::kHalf, 0.32, 4, m, n, k, w, &best);
@@ -1404,7 +1407,7 @@ zvc_status project(const GluArgs<T>& p, const Cut& cut, float* sums, hipStream_t
         if (cut.size == Size::kLone) return product_of<T, DOES, Lone>(p, cut, sums, stream);
         if (cut.size == Size::kHalf) return product_of<T, DOES, Half>(p, cut, sums, stream);
     }
-    return cut.size == Size::kSmall ? product_of<T, DOES, Small>(p, cut, sums, stream) : product_of<T, DOES, Thin>(p, cut, sums, stream);
+    return cut.size == Size::kSmall ? product_of<T, DOES, Eights>(p, cut, sums, stream) : product_of<T, DOES, Thin>(p, cut, sums, stream);
 }
 
 template <typename T>
