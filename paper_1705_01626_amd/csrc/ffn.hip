@@ -198,15 +198,6 @@ __device__ __forceinline__ void drop_group(const Drop& d, uint64_t offset, uint6
     }
 }
 
-template <typename T>
-__device__ __forceinline__ void drop_some(const T* x, const T* residual, T* y, int count, unsigned keep, float scale) {
-    for (int j = 0; j < count; ++j) {
-        float v = (keep >> j & 1u) != 0 ? static_cast<float>(x[j]) * scale : 0.f;
-        if (residual != nullptr) v += static_cast<float>(residual[j]);
-        y[j] = static_cast<T>(v);
-    }
-}
-
 // y = drop(x) [+ residual].  A lane owns GROUPS times eight consecutive elements, each one counter of the generator.  Memory bounds
 // it, and with 16-bit elements nearly the generator too (20 multiplications for 16 bytes).  33.5 M elements, us and TB/s: bf16
 // 27.3, 4.9 (25.4 without the generator); fp32 49, 5.5; bf16 with a residual at 67 M elements 74.4, 5.4.  GROUPS = 1 | 2 | 4:
@@ -1166,9 +1157,11 @@ zvc_status dropout_as(const void* x, size_t ldx, const void* residual, size_t ld
     const size_t blocks = div_up(div_up(total, 8), static_cast<size_t>(kDropThreads) * kGroups);
     if (blocks > 0x7FFFFFFF) return ZVC_E_ARG;
     // us, as it is | STREAM: bf16 of 67 MB 27.9 | 25.9, 134 MB and a residual 74.6 | 72.0; fp32 of 134 MB 49.4 | 52.4
-    const bool stream_out = sizeof(T) == 2 && total * sizeof(T) > kCacheBytes;
-    return launch(stream_out ? dropout_kernel<T, kGroups, true> : dropout_kernel<T, kGroups, false>, dim3(blocks), kDropThreads, stream,
-                  static_cast<const T*>(x), ldx, static_cast<const T*>(residual), ldr, static_cast<T*>(y), ldy, cols, total, d);
+    void (*kernel)(const T*, size_t, const T*, size_t, T*, size_t, size_t, uint64_t, Drop) = dropout_kernel<T, kGroups, false>;
+    if constexpr (sizeof(T) == 2)
+        if (total * sizeof(T) > kCacheBytes) kernel = dropout_kernel<T, kGroups, true>;
+    return launch(kernel, dim3(blocks), kDropThreads, stream, static_cast<const T*>(x), ldx, static_cast<const T*>(residual), ldr,
+                  static_cast<T*>(y), ldy, cols, total, d);
 }
 
 bool sizes_ok(size_t m, size_t n, size_t k) {
@@ -1399,8 +1392,9 @@ zvc_status project(const GluArgs<T>& p, const Cut& cut, float* sums, hipStream_t
         if constexpr (sizeof(T) == 2) {
             if (p.m <= 64) return tokens_of<T, DOES, 4, 3, 2>(p, stream);
             return p.m <= 96 ? tokens_of<T, DOES, 6, 4, 2>(p, stream) : tokens_of<T, DOES, 8, 4, 2>(p, stream);
+        } else {
+            return tokens_of<T, DOES, 4, 4, 3>(p, stream);
         }
-        return tokens_of<T, DOES, 4, 4, 3>(p, stream);
     }
     if constexpr (sizeof(T) == 2) {
         if (cut.size == Size::kLarge) return product_of<T, DOES, Large>(p, cut, sums, stream);
