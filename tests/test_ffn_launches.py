@@ -12,6 +12,7 @@ import pytest
 
 from paper_1705_01626_amd import build as zvc_build
 from tests.ffn_routes import ROUTES
+from tests.test_device_code import tool
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 FP32, FP16, BF16 = range(3)
@@ -118,7 +119,18 @@ def test_every_cut_is_among_them():
                     assert cuts >= ({"whole", "split"} if (column, shape) == (1, "thin") else {"whole", "split", "mixed"})
 
 
-def test_no_kernel_is_built_that_no_call_launches(fake):
+def device_kernels(where):
+    """The kernels of the library's code object: it can hold some that the host side never names."""
+    fat, code = str(where / "fat"), str(where / "gfx950.co")
+    subprocess.run([tool("llvm-objcopy"), "--dump-section", ".hip_fatbin=" + fat, zvc_build.FFN_LIBRARY, str(where / "rest.so")],
+                   check=True)
+    subprocess.run([tool("clang-offload-bundler"), "--unbundle", "--type=o", "--targets=hipv4-amdgcn-amd-amdhsa--gfx950",
+                    "--input=" + fat, "--output=" + code], check=True)
+    symbols = subprocess.run([tool("llvm-objdump"), "--syms", code], check=True, capture_output=True, text=True).stdout
+    return set(re.findall(r"\b(\w+)\.kd$", symbols, flags=re.M))
+
+
+def test_no_kernel_is_built_that_no_call_launches(fake, tmp_path):
     """The sizes above, some that take copies of unaligned inputs, numbers of tokens around each kernel for few, and dropout."""
     calls = [c for size in ROUTES for dtype in (BF16, FP16, FP32)
              for c in (forward(*size, dtype), backward(*size, dtype), backward(*size, dtype, True))]
@@ -126,4 +138,5 @@ def test_no_kernel_is_built_that_no_call_launches(fake):
     calls += [dropout(rows, cols, dtype) for rows, cols in ((3, 100), (8192, 4096)) for dtype in (BF16, FP16, FP32)]
     kernels, results = run(fake, calls)
     assert all(status == 0 for status, _ in results)
-    assert kernels - {x.name for _, launches in results for x in launches} == set()
+    launched = {x.name for _, launches in results for x in launches}
+    assert launched == kernels == device_kernels(tmp_path)
