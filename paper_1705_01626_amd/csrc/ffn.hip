@@ -252,8 +252,18 @@ struct ActValue {
     float value, slope;
 };
 
-// 1 / (1 + exp(-x)), to a few units in the last place of 32 bits.
-__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
+// 1 / (1 + exp(-x)).  In fp32 to a few units in the last place, by exp of what is below 0, also where it is no normal number.  For
+// 16-bit types by the shortest way: exp's argument is rounded as a multiple of ln 2, which leaves |x| x 2^-24 of the result,
+// 5e-6 at -80, and below -87 the result is 0.
+template <typename T>
+__device__ __forceinline__ float sigmoid(float x) {
+    if constexpr (sizeof(T) == 4) {
+        const float e = expf(-fabsf(x));
+        return (x < 0.f ? e : 1.f) * __builtin_amdgcn_rcpf(1.f + e);
+    } else {
+        return __builtin_amdgcn_rcpf(1.f + __expf(-x));
+    }
+}
 
 // act(g) and its derivative.  relu: a NaN is not <= 0 and stays.
 template <int ACT, typename T>
@@ -261,7 +271,7 @@ __device__ __forceinline__ ActValue activate(float g) {
     if constexpr (ACT == ZVC_RELU) {
         return {g <= 0.f ? 0.f : g, g <= 0.f ? 0.f : 1.f};
     } else if constexpr (ACT == ZVC_SILU) {
-        const float s = sigmoid(g), a = g * s;
+        const float s = sigmoid<T>(g), a = g * s;
         return {a, s + a * (1.f - s)};
     } else if constexpr (ACT == ZVC_GELU) {
         const float density = __expf(-0.5f * g * g);
@@ -281,7 +291,7 @@ __device__ __forceinline__ ActValue activate(float g) {
         return {g * cdf, cdf + g * 0.39894228f * density};
     } else {
         // (1 + tanh(z)) / 2 = sigmoid(2 z)
-        const float s = sigmoid(1.5957691f * (g + 0.044715f * g * g * g)), a = g * s;
+        const float s = sigmoid<T>(1.5957691f * (g + 0.044715f * g * g * g)), a = g * s;
         return {a, s + a * (1.f - s) * 1.5957691f * (1.f + 0.134145f * g * g)};
     }
 }

@@ -106,3 +106,12 @@ def test_a_nan_stays_one(name, dtype, rows):
     there = torch.arange(rows, device=DEV) == 1
     for t, label in zip(activations(g, name, rows), ("h", "du", "slope")):
         assert torch.equal(torch.isnan(t), there), label
+
+
+def test_silu_in_32_bits():
+    """To a few units in the last place wherever it is a normal number: 8 x 2^-24."""
+    g = grid_of(torch.float32, -87, 88)
+    value = g.to(F64) * torch.sigmoid(g.to(F64))
+    bound = 2.0 ** -21 * value.abs() + 2.0 ** -125
+    for t in activations(g, "silu")[:2]:
+        blocks.check(t, (value, bound), "silu")
