@@ -292,7 +292,8 @@ __device__ __forceinline__ ActValue activate(float g) {
     } else {
         // (1 + tanh(z)) / 2 = sigmoid(2 z)
         const float s = sigmoid<T>(1.5957691f * (g + 0.044715f * g * g * g)), a = g * s;
-        return {a, s + a * (1.f - s) * 1.5957691f * (1.f + 0.134145f * g * g)};
+        // (beyond 16 either s or 1 - s is 0: g^2 is held there, or it becomes an infinity and the product a NaN)
+        return {a, s + a * (1.f - s) * 1.5957691f * (1.f + 0.134145f * fminf(g * g, 256.f))};
     }
 }
 

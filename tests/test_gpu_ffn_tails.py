@@ -96,6 +96,17 @@ def test_slopes_relative_to_their_terms(name, dtype):
     blocks.check(activations(g, name)[2], (value, bound), "slope")
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("name", ["relu", *RANGE])
+def test_large_numbers_have_the_limits(name, dtype):
+    """act(g) = g and act' = 1 far above 0, 0 and 0 far below it, up to the largest number of the type."""
+    g = torch.tensor([s * v for s in (1.0, -1.0) for v in (200.0, 1e5, 1e13, 1e18, 3e19, 1e20, 1e30, 3e38)], device=DEV).to(dtype)
+    h, du, slope = activations(g, name)
+    zero = torch.zeros_like(g)
+    assert torch.equal(h, torch.where(g > 0, g, zero)) and torch.equal(du, h)
+    assert torch.equal(slope, (g > 0).to(dtype))
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("name", ["relu", *RANGE])
 @pytest.mark.parametrize("rows", [3, 700])
