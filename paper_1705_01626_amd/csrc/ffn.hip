@@ -1213,10 +1213,10 @@ void tiles_of(size_t m, size_t n, size_t k, size_t* cols, size_t* rows) {
     *rows = DOES == Does::kDw ? 2 * div_up(n, S::QT) : div_up(m, S::QT);
 }
 
-enum class Size { kLarge, kSmall, kThin, kLone, kHalf };
+enum class Size { kLarge, kSmall, kThin, kLone, kHalf, kTokens };
 
 // How a product is cut: the tiles' shape, how many tiles are summed whole, and in how many parts of the reduction the others are,
-// to be joined by a second kernel.
+// to be joined by a second kernel.  kTokens: no tiles, but the kernel for few tokens.
 struct Cut {
     Size size;
     unsigned whole, parts;
@@ -1254,8 +1254,16 @@ void try_cut(Size size, double stage_us, double item_us, size_t m, size_t n, siz
         if (full != tiles) consider(full, parts);
 }
 
+// Whether m tokens take the kernel for few of them.  us (weights from memory), tiles | that kernel: bf16 n = k = 4096, 1 token
+// 22.6 | 13.2, 32 23.1 | 14.7, 64 22.7 | 19.6, 96 28.1 | 22.9, 128 28.6 | 26.6; 11264 x 4096, 1 token 45.6 | 31.5, 48 42.7 | 42.5,
+// 64 42.8 | 48.5, 96 46.8 | 60.6; 5632 x 2048, 64 19.5 | 18.6, 96 19.3 | 23.9; 2816 x 1024, 96 10.6 | 7.8, 128 10.6 | 9.4.  fp32, where
+// the products come in sooner: n = k = 4096, 32 tokens 38.9 | 29, 48 48.7 | 39; 11264 x 4096, 48 122 | 109, 64 126 | 134; 2816 x 1024,
+// 64 18.3 | 14.5.  So more than 48 only where every workgroup has a compute unit of its own.
+bool few_tokens(size_t m, size_t n, size_t w) { return m <= 48 || (m <= (w == 4 ? 64 : 128) && n <= kUnits * kTokenCols); }
+
 // The projections' cut.
 Cut cut_of(size_t m, size_t n, size_t k, size_t w) {
+    if (k != 0 && few_tokens(m, n, w)) return {Size::kTokens, 0, 1, 0, 0};
     Cut best{Size::kSmall, 0, 1, 0, 1e300};
     if (w == 4) {                                // the products bound it, whatever the tile; a stage is 32 steps
         try_cut<Eights>(Size::kSmall, 3.8, 5, m, n, k, w, &best);
@@ -1388,16 +1396,9 @@ zvc_status tokens_of(const GluArgs<T>& p, hipStream_t stream) {
     return launch(token_kernel<T, DOES, TB, WAVES, RING>, dim3(div_up(cols, kTokenCols)), 64 * WAVES, stream, p);
 }
 
-// Whether m tokens take the kernel for few of them.  us (weights from memory), tiles | that kernel: bf16 n = k = 4096, 1 token
-// 22.6 | 13.2, 32 23.1 | 14.7, 64 22.7 | 19.6, 96 28.1 | 22.9, 128 28.6 | 26.6; 11264 x 4096, 1 token 45.6 | 31.5, 48 42.7 | 42.5,
-// 64 42.8 | 48.5, 96 46.8 | 60.6; 5632 x 2048, 64 19.5 | 18.6, 96 19.3 | 23.9; 2816 x 1024, 96 10.6 | 7.8, 128 10.6 | 9.4.  fp32, where
-// the products come in sooner: n = k = 4096, 32 tokens 38.9 | 29, 48 48.7 | 39; 11264 x 4096, 48 122 | 109, 64 126 | 134; 2816 x 1024,
-// 64 18.3 | 14.5.  So more than 48 only where every workgroup has a compute unit of its own.
-bool few_tokens(size_t m, size_t n, size_t w) { return m <= 48 || (m <= (w == 4 ? 64 : 128) && n <= kUnits * kTokenCols); }
-
 template <typename T, Does DOES>
 zvc_status project(const GluArgs<T>& p, const Cut& cut, float* sums, hipStream_t stream) {
-    if (p.k != 0 && few_tokens(p.m, p.n, sizeof(T))) {
+    if (cut.size == Size::kTokens) {
         // (waves and ring: most of LDS, as one workgroup or as two of which one reads while the other finishes.  11264 x 4096 bf16, 16 tokens
         // 4 x 3 33.4, 8 x 3 36.6, 4 x 6 36.9; 32: 4 x 2 38.2, 4 x 3 40.6, 8 x 2 40.7, 2 x 4 44.2; 64: 3 x 2 48.4, 4 x 3 50, 6 x 2 51.7, 2 x 3 56)
         if (p.m <= 16) return tokens_of<T, DOES, 1, 4, 3>(p, stream);
