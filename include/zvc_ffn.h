@@ -69,7 +69,7 @@ uint64_t zvc_dropout_fraction(double p);
 
 /* y = drop(x), or residual + drop(x) where d_residual is not null: rows x cols
  * elements, added and scaled in 32 bits and rounded once.  d_y may be d_x or d_residual itself, at
- * the same row stride. */
+ * the same row stride.  rows times the largest row stride: at most ZVC_FFN_MAX_ELEMENTS. */
 zvc_status zvc_dropout(const void* d_x, size_t ldx, const void* d_residual, size_t ldr, void* d_y, size_t ldy,
                        size_t rows, size_t cols, int type, uint64_t drop, uint64_t seed, uint64_t offset,
                        const uint64_t* d_offset, hipStream_t stream);

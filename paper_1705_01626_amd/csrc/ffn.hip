@@ -185,6 +185,7 @@ __device__ __forceinline__ void store_some(T* at, const Eight& e, int there, boo
 }
 
 constexpr int kDropThreads = 256;
+constexpr unsigned kDropRow = 1u << 20;            // workgroups in a row of the grid: a dimension holds fewer than 2^32 lanes
 
 // Zeros in the place of a group's dropped elements.  Where 16 bits decide all of them each is compared where it lies: the
 // generator and these comparisons are what a 16-bit tensor's call spends beside its traffic.
@@ -206,7 +207,7 @@ template <typename T, int GROUPS, bool STREAM>
 __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const T* x, size_t ldx, const T* residual, size_t ldr,
                                                                T* y, size_t ldy, size_t cols, uint64_t total, Drop d) {
     const uint64_t offset = d.active ? effective_offset(d) : 0;
-    const uint64_t group0 = static_cast<uint64_t>(blockIdx.x) * (kDropThreads * GROUPS) + threadIdx.x;
+    const uint64_t group0 = (static_cast<uint64_t>(blockIdx.y) * kDropRow + blockIdx.x) * (kDropThreads * GROUPS) + threadIdx.x;
     Eight e[GROUPS], r[GROUPS];
     uint64_t row[GROUPS], col[GROUPS];
     bool inside[GROUPS];                                           // eight elements of one row
@@ -1169,12 +1170,12 @@ zvc_status dropout_as(const void* x, size_t ldx, const void* residual, size_t ld
     const uint64_t total = static_cast<uint64_t>(rows) * cols;
     constexpr int kGroups = sizeof(T) == 2 ? 2 : 1;
     const size_t blocks = div_up(div_up(total, 8), static_cast<size_t>(kDropThreads) * kGroups);
-    if (blocks > 0x7FFFFFFF) return ZVC_E_ARG;
+    const dim3 grid(blocks < kDropRow ? blocks : kDropRow, div_up(blocks, kDropRow));
     // us, as it is | STREAM: bf16 of 67 MB 27.9 | 25.9, 134 MB and a residual 74.6 | 72.0; fp32 of 134 MB 49.4 | 52.4
     void (*kernel)(const T*, size_t, const T*, size_t, T*, size_t, size_t, uint64_t, Drop) = dropout_kernel<T, kGroups, false>;
     if constexpr (sizeof(T) == 2)
         if (total * sizeof(T) > kCacheBytes) kernel = dropout_kernel<T, kGroups, true>;
-    return launch(kernel, dim3(blocks), kDropThreads, stream, static_cast<const T*>(x), ldx, static_cast<const T*>(residual), ldr,
+    return launch(kernel, grid, kDropThreads, stream, static_cast<const T*>(x), ldx, static_cast<const T*>(residual), ldr,
                   static_cast<T*>(y), ldy, cols, total, d);
 }
 

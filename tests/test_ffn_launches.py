@@ -140,3 +140,17 @@ def test_no_kernel_is_built_that_no_call_launches(fake, tmp_path):
     assert all(status == 0 for status, _ in results)
     launched = {x.name for _, launches in results for x in launches}
     assert launched == kernels == device_kernels(tmp_path)
+
+
+@pytest.mark.parametrize("dtype,each", [(BF16, 16), (FP32, 8)])
+def test_a_dimension_of_dropouts_grid_holds_its_lanes(fake, dtype, each):
+    """A dimension has fewer than 2^32 lanes; all of them together have every element."""
+    sizes = [(1, 1), (1, 1 << 20), (1, (1 << 31) + 5), (1, (1 << 35) + 8), (1, 1 << 36), (1 << 20, (1 << 16) + 8), (1, 1 << 40)]
+    _, results = run(fake, [dropout(rows, cols, dtype) for rows, cols in sizes])
+    for (rows, cols), (status, launches) in zip(sizes, results):
+        v = launches[0].values
+        assert status == 0 and len(launches) == 1
+        assert v["grid"] * v["block"] < 1 << 32 and v["rows"] < 1 << 16 and v["depth"] == 1
+        assert v["rows"] == 1 or v["grid"] == 1 << 20             # (the kernel numbers workgroups by it)
+        lanes = v["grid"] * v["rows"] * v["block"]
+        assert rows * cols <= lanes * each and (v["rows"] - 1) * (1 << 20) * v["block"] * each < rows * cols
