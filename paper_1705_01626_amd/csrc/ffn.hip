@@ -355,7 +355,8 @@ __device__ __forceinline__ int4v buffer_at(uint64_t address) {
                  __builtin_amdgcn_readfirstlane(static_cast<int>(address >> 32 & 0xFFFF)), static_cast<int>(kReach), kRawBuffer};
 }
 
-// 16 bytes a lane from memory to LDS, lane l's at lds + 16 l.  (No register is written: the wait is wait_loads()'s.)
+// 16 bytes a lane from memory to LDS, lane l's at lds + 16 l.  (No register is written: the wait is wait_loads()'s.  m0 is a register
+// that the compiler keeps for itself and cannot be told of as overwritten; a test reads from the assembly that nothing else uses it.)
 __device__ __forceinline__ void load_to_lds(int4v buffer, unsigned offset, unsigned lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(buffer)
                  : "memory");
