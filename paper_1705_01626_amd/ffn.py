@@ -95,14 +95,14 @@ def _matrix(t: torch.Tensor, rows: int, cols: int, like: torch.Tensor, where: st
     row, col = t.stride() if t.dim() == 2 else (0, 0)
     # (what nearly every call has, with few of the attribute lookups that a call's host time goes to)
     if col == 1 and row >= cols and t.shape == (rows, cols) and t.dtype is like.dtype and t.get_device() == like.get_device():
-        return row
+        return row if rows > 1 else cols               # (one row has no next one, however far away that would be)
     if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
         _refuse(where, "%s is %s, %d x %d expected" % (name, tuple(t.shape), rows, cols))
     if t.dtype != like.dtype or t.device != like.device:
         _refuse(where, "%s is %s on %s, the first tensor is %s on %s" % (name, t.dtype, t.device, like.dtype, like.device))
     if (col != 1 and cols > 1) or (row < cols and rows > 1):
         _refuse(where, "%s has strides %s: rows have to be contiguous and apart" % (name, t.stride()))
-    return row if row >= cols else cols
+    return row if rows > 1 else cols
 
 
 def _fraction(p: float, where: str) -> int:
@@ -170,7 +170,7 @@ def zvc_glu_workspace_bytes(m: int, n: int, k: int, dtype: torch.dtype, backward
 
 
 def _loose(*tensors: torch.Tensor) -> bool:
-    return any(t.data_ptr() % 16 or (t.stride(0) * t.element_size()) % 16 for t in tensors)
+    return any(t.data_ptr() % 16 or (t.shape[0] > 1 and (t.stride(0) * t.element_size()) % 16) for t in tensors)
 
 
 def new_glu_workspace(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, backward: bool = False) -> torch.Tensor:
