@@ -124,6 +124,13 @@ def _on_gpu(where: str, x: torch.Tensor, ws: Optional[torch.Tensor] = None) -> N
         _refuse(where, "the tensors and the workspace have to be on one GPU")
 
 
+def _room(ws: torch.Tensor, where: str) -> int:
+    """The bytes of a workspace.  (An expanded one has more elements than memory.)"""
+    if not ws.is_contiguous():
+        _refuse(where, "the workspace has strides %s: it has to be contiguous" % (ws.stride(),))
+    return ws.numel() * ws.element_size()
+
+
 def _pair(a, b, rows, cols, like, where, names):
     """Addresses and common row stride of two tensors that are both there or both not."""
     if (a is None) != (b is None):
@@ -203,10 +210,11 @@ def zvc_glu_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, h
     ldh = _matrix(h, m, n, x, where, "h")
     gate_at, up_at, ldp = _pair(gate, up, m, n, x, where, ("gate", "up"))
     drop, word = _fraction(p, where), _word(d_offset, x, where)
+    room = _room(ws, where)
     _on_gpu(where, x, ws)
     _check(_native().zvc_glu_forward(x.data_ptr(), ldx, wg, wu, ldw, h.data_ptr(), ldh, gate_at, up_at, ldp, m, n, k,
-                                     code, act, drop, seed, offset, word, ws.data_ptr(),
-                                     ws.numel() * ws.element_size(), _stream_handle(stream)), where)
+                                     code, act, drop, seed, offset, word, ws.data_ptr(), room,
+                                     _stream_handle(stream)), where)
 
 
 def zvc_glu_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
@@ -228,8 +236,9 @@ def zvc_glu_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_
     lddx = k if dx is None else _matrix(dx, m, k, x, where, "dx")
     dwg, dwu, lddw = _pair(dw_gate, dw_up, n, k, x, where, ("dw_gate", "dw_up"))
     drop, word = _fraction(p, where), _word(d_offset, x, where)
+    room = _room(ws, where)
     _on_gpu(where, x, ws)
     _check(_native().zvc_glu_backward(dh.data_ptr(), lddh, x.data_ptr(), ldx, wg, wu, ldw, gate_at, up_at, ldp,
                                       0 if dx is None else dx.data_ptr(), lddx, dwg, dwu, lddw, m, n, k, code, act,
-                                      drop, seed, offset, word, ws.data_ptr(),
-                                      ws.numel() * ws.element_size(), _stream_handle(stream)), where)
+                                      drop, seed, offset, word, ws.data_ptr(), room,
+                                      _stream_handle(stream)), where)

@@ -1,4 +1,4 @@
-"""Row strides as the binding takes them from tensors (no GPU)."""
+"""Row strides, and the workspace's size, as the binding takes them from tensors (no GPU)."""
 import pytest
 import torch
 
@@ -40,3 +40,14 @@ def test_more_rows_keep_theirs():
 def test_the_pair_of_a_single_row():
     a, b = torch.zeros(2, FAR)[:1, :8], torch.zeros(1, 8)
     assert ffn._pair(a, b, 1, 8, a, "call", ("a", "b"))[2] == 8
+
+
+@pytest.mark.parametrize("ws", [torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(1 << 20, dtype=torch.uint8)[::2],
+                                torch.zeros(64, 64, dtype=torch.uint8)[:, :32]])
+def test_a_workspace_with_gaps_or_without_memory_is_refused(ws):
+    """Its number of elements says nothing of the memory behind its address."""
+    x, w, h = torch.zeros(4, 8), torch.zeros(6, 8), torch.zeros(4, 6)
+    for call in (lambda: ffn.zvc_glu_forward(x, w, w, h, ws),
+                 lambda: ffn.zvc_glu_backward(h, x, w, w, x.clone(), w.clone(), w.clone(), ws)):
+        with pytest.raises(zvc.ZvcError, match="contiguous"):
+            call()
