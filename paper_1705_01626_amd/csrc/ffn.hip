@@ -203,7 +203,12 @@ __device__ __forceinline__ void drop_group(const Drop& d, uint64_t offset, uint6
 // it, and with 16-bit elements nearly the generator too (20 multiplications for 16 bytes).  33.5 M elements, us and TB/s: bf16
 // 27.3, 4.9 (25.4 without the generator); fp32 49, 5.5; bf16 with a residual at 67 M elements 74.4, 5.4.  GROUPS = 1 | 2 | 4:
 // bf16 28.8 | 27.3 | 30.4, fp32 with a residual 68.3 | 71.1 | 71.9.
-template <typename T, int GROUPS, bool STREAM>
+//
+// Its stores leave y in the caches for what reads it next.  Past them the call alone takes less, and the codec or a product that reads y
+// more than that; us, as it is | past: bf16 of 96 MB 38.5 | 36, with the codec 73 | 78.3, with a product 116 | 118; 128 MB and a residual
+// 72.8 | 63.2, with a product 161 | 165; 192 MB with the codec 131 | 141.  (An addition behind it: 96 MB 72 | 72, 64 MB and a
+// residual 63 | 55.6, 192 MB and a residual 176.6 | 183.6.)
+template <typename T, int GROUPS>
 __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const T* x, size_t ldx, const T* residual, size_t ldr,
                                                                T* y, size_t ldy, size_t cols, uint64_t total, Drop d) {
     const uint64_t offset = d.active ? effective_offset(d) : 0;
@@ -234,7 +239,7 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const T* x, size_
 #pragma unroll
                 for (int j = 0; j < 8; ++j) e[g].v[j] += r[g].v[j];
             }
-            store8<STREAM>(y + row[g] * ldy + col[g], e[g]);
+            store8(y + row[g] * ldy + col[g], e[g]);
         } else {
             const unsigned keep = d.active ? keep_bits(d, offset, group, words) : 0xFFu;
             uint64_t line = row[g], at = col[g];
@@ -1162,8 +1167,6 @@ zvc_status make_drop(uint64_t drop, uint64_t seed, uint64_t offset, const uint64
     return ZVC_OK;
 }
 
-constexpr size_t kCacheBytes = size_t{32} << 20;   // of the eight XCDs' L2 together
-
 template <typename T>
 zvc_status dropout_as(const void* x, size_t ldx, const void* residual, size_t ldr, void* y, size_t ldy, size_t rows,
                       size_t cols, const Drop& d, hipStream_t stream) {
@@ -1172,11 +1175,7 @@ zvc_status dropout_as(const void* x, size_t ldx, const void* residual, size_t ld
     constexpr int kGroups = sizeof(T) == 2 ? 2 : 1;
     const size_t blocks = div_up(div_up(total, 8), static_cast<size_t>(kDropThreads) * kGroups);
     const dim3 grid(blocks < kDropRow ? blocks : kDropRow, div_up(blocks, kDropRow));
-    // us, as it is | STREAM: bf16 of 67 MB 27.9 | 25.9, 134 MB and a residual 74.6 | 72.0; fp32 of 134 MB 49.4 | 52.4
-    void (*kernel)(const T*, size_t, const T*, size_t, T*, size_t, size_t, uint64_t, Drop) = dropout_kernel<T, kGroups, false>;
-    if constexpr (sizeof(T) == 2)
-        if (total * sizeof(T) > kCacheBytes) kernel = dropout_kernel<T, kGroups, true>;
-    return launch(kernel, grid, kDropThreads, stream, static_cast<const T*>(x), ldx, static_cast<const T*>(residual), ldr,
+    return launch(dropout_kernel<T, kGroups>, grid, kDropThreads, stream, static_cast<const T*>(x), ldx, static_cast<const T*>(residual), ldr,
                   static_cast<T*>(y), ldy, cols, total, d);
 }
 

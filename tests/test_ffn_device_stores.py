@@ -1,0 +1,14 @@
+"""Where the stores of libzvc_ffn.so's kernels go, read from their assembly (no GPU)."""
+import re
+
+from tests.test_device_code import functions
+from tests.test_ffn_device_code import assembly  # noqa: F401 (a fixture)
+
+
+def test_dropout_leaves_its_output_to_the_caches(assembly):  # noqa: F811
+    """The next operation reads it: past the caches the call alone is faster and the two together slower."""
+    kernels = functions(assembly, "dropout_kernel")
+    assert len(kernels) == 3
+    for name, body in kernels.items():
+        stores = re.findall(r"^\s*(global_store_\w+ .*?)(?:\s*//.*)?$", body, flags=re.M)
+        assert len(stores) >= 2 and not any(re.search(r"\bnt\b", x) for x in stores), name
