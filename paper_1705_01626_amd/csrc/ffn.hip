@@ -134,17 +134,18 @@ __device__ __forceinline__ Eight load8(const T* at) {
     return out;
 }
 
-// STREAM: past the caches' replacement, for an output that they cannot hold.
-template <bool STREAM = false, typename T>
-__device__ __forceinline__ void store8(T* at, const Eight& e) {
+// past: past the caches' replacement, for an output that they cannot hold; `at` is then a multiple of 16 bytes.  (Stores of
+// different alignment: of equal ones behind a branch the compiler makes one, an ordinary one.)
+template <typename T>
+__device__ __forceinline__ void store8(T* at, const Eight& e, bool past = false) {
     constexpr int kPer = 16 / sizeof(T);
-    using Quad = unsigned __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    using Quad = unsigned __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int h = 0; h < 8 / kPer; ++h) {
         Pack<T> p;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) p.v[j] = static_cast<T>(e.v[h * kPer + j]);
-        if constexpr (STREAM) {
+        if (past) {
             Quad q;
             __builtin_memcpy(&q, &p, 16);
             __builtin_nontemporal_store(q, reinterpret_cast<Quad*>(at + h * kPer));
@@ -583,13 +584,11 @@ __device__ __forceinline__ int columns_left(unsigned n, unsigned col) { return c
 
 // What becomes of a lane's strip of a tile, eight columns of QB rows 16 apart: straight code, row after row (the fences keep the
 // compiler from working on all rows at once, out of registers), and what is rare in another place (a tile's code that the
-// instruction cache has to fetch anew costs 3 us).  The large tiles' outputs go past the caches, which would
-// not keep them, and leave the operands there (long prompt 2295 | 2253 us, 8192 tokens kept 375 | 361); dg and du, which
-// are read next, do not (largest backward 3557 | 3605).
+// instruction cache has to fetch anew costs 3 us).
 template <typename T, Does DOES, class S>
-__device__ __forceinline__ void finish_tile(const GluArgs<T>& p, unsigned row, unsigned col, bool full, float4v (&acc)[S::PB][S::QB]) {
+__device__ __forceinline__ void finish_tile(const GluArgs<T>& p, unsigned row, unsigned col, bool full, bool past, float4v (&acc)[S::PB][S::QB]) {
     static_assert(S::QB <= 8, "a bit for each of a lane's elements");
-    constexpr bool kStream = S::QT >= 256;
+    if constexpr (S::QT < 256) past = false;                     // (code that these tiles do not need)
     if (col >= (DOES == Does::kSlope ? p.ldd : p.n)) return;     // (dg and du are written up to their rows' ends)
     const int there = columns_left(p.n, col);
     uint64_t keep = ~uint64_t{0};
@@ -645,8 +644,8 @@ __device__ __forceinline__ void finish_tile(const GluArgs<T>& p, unsigned row, u
                 take(j, g, u);
                 kept8(p, keeps(j), g, u);
                 if (row + j * 16 < p.m) {
-                    store8<kStream>(cell(p.gate, row + j * 16, p.ldp, col), g);
-                    store8<kStream>(cell(p.up, row + j * 16, p.ldp, col), u);
+                    store8(cell(p.gate, row + j * 16, p.ldp, col), g, past);
+                    store8(cell(p.up, row + j * 16, p.ldp, col), u, past);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -658,7 +657,7 @@ __device__ __forceinline__ void finish_tile(const GluArgs<T>& p, unsigned row, u
                 take(j, g, u);
                 Eight h = forward8<decltype(act)::value>(p, g, u);
                 if (p.d.active) drop8(keeps(j), h);
-                if (row + j * 16 < p.m) store8<kStream>(cell(p.h, row + j * 16, p.ldh, col), h);
+                if (row + j * 16 < p.m) store8(cell(p.h, row + j * 16, p.ldh, col), h, past);
                 __builtin_amdgcn_sched_barrier(0);
             }
         });
@@ -666,10 +665,12 @@ __device__ __forceinline__ void finish_tile(const GluArgs<T>& p, unsigned row, u
 }
 
 // How one product is cut into work items: tp x tq tiles, of which the first `whole` are summed in one go and the others in `parts`
-// parts of the reduction each, whose sums lie part by part, tile by tile as they lie in it, and are joined.
+// parts of the reduction each, whose sums lie part by part, tile by tile as they lie in it, and are joined.  past: the outputs of the
+// large tiles go past the caches.
 struct Plan {
     float* sums;
     unsigned tp, tq, whole, parts;
+    bool past;
     __host__ __device__ unsigned items() const { return whole + (tp * tq - whole) * parts; }
 };
 
@@ -855,7 +856,7 @@ __device__ __forceinline__ void work(const GluArgs<T>& p, const Plan& plan, unsi
                     *reinterpret_cast<float4v*>(sums + (row_in + j * 16) * S::PT + at) = acc[i][j];
                 }
         } else if constexpr (kFold) {
-            finish_tile<T, DOES, S>(p, row_first, col0 + wp * 32 + quarter * 8, col0 + wp * 32 + 32 <= p.n, acc);
+            finish_tile<T, DOES, S>(p, row_first, col0 + wp * 32 + quarter * 8, col0 + wp * 32 + 32 <= p.n, plan.past, acc);
         } else {
             const unsigned rows = DOES == Does::kDw ? p.n : p.m;
             T* const out = DOES == Does::kDx ? p.dx : second ? p.dwu : p.dwg;
@@ -1357,7 +1358,7 @@ template <Does DOES, class S>
 Plan plan_of(const Cut& cut, size_t m, size_t n, size_t k, float* sums) {
     size_t cols, rows;
     tiles_of<DOES, S>(m, n, k, &cols, &rows);
-    return {sums, static_cast<unsigned>(cols), static_cast<unsigned>(rows), cut.whole, cut.parts};
+    return {sums, static_cast<unsigned>(cols), static_cast<unsigned>(rows), cut.whole, cut.parts, false};
 }
 
 // The blocks of a join, 0 where there is none.
@@ -1367,9 +1368,24 @@ unsigned join_blocks(const Plan& plan) {
     return static_cast<unsigned>(div_up(size_t{plan.tp * plan.tq - plan.whole} * (S::QT * Tile<T, DOES, S>::kCols / 8), 256));
 }
 
+constexpr size_t kCacheBytes = size_t{256} << 20;  // of the cache in front of the memory
+
+// Whether a forward call's outputs go past the caches and leave the operands there: as much as the caches hold or more, in rows that are
+// whole halves of the memory's 128 bytes (others are written in pieces that nothing puts together any more).  us, past | not, relu
+// and dropout, alone, with a product that reads h, with the codec that reads the kept projections or else h: 8192 x 5632 x 2048 kept
+// (264 MB in all) 340 | 370, 474 | 495, 399 | 403; 16384 x 8192 x 512 (256) 309 | 333, 473 | 507, 395 | 401; 16384 x 11264 x 1024 (352) 680 | 740, 942 | 988, 790 | 838.
+// Less: 8192 x 4096 x 1024 kept (192) 164 | 151, 222 | 208, 212 | 190; 1024 x 8192 x 128 kept (48) 25 | 20.6, 41 | 35, 43 | 39; 8192 x 5632 x 2048 (88)
+// 312 | 316, 441 | 442, 343 | 345.  Rows of 11280 bytes: 8192 x 5640 x 2048 kept 434 | 389, 589 | 543, 492 | 417; of 11328 343 | 374, 486 | 518, 400 | 408.
+template <typename T>
+bool past_caches(const GluArgs<T>& p) {
+    const auto whole = [&](const T* at, unsigned ld) { return at == nullptr || (aligned_to(at, 64) && size_t{ld} * sizeof(T) % 64 == 0); };
+    return size_t{p.m} * p.n * sizeof(T) * (p.gate != nullptr ? 3 : 1) >= kCacheBytes && whole(p.h, p.ldh) && whole(p.gate, p.ldp) && whole(p.up, p.ldp);
+}
+
 template <typename T, Does DOES, class S>
 zvc_status product_of(const GluArgs<T>& p, const Cut& cut, float* sums, hipStream_t stream) {
-    const Plan plan = plan_of<DOES, S>(cut, p.m, p.n, p.k, sums);
+    Plan plan = plan_of<DOES, S>(cut, p.m, p.n, p.k, sums);
+    plan.past = DOES == Does::kForward && S::QT >= 256 && past_caches(p);
     const unsigned items = plan.items(), room = kUnits * S::kPerUnit;
     const zvc_status st = launch(product_kernel<T, DOES, S>, dim3(items < room ? items : room), S::kThreads, stream, p, plan);
     const unsigned blocks = join_blocks<T, DOES, S>(plan);
@@ -1380,7 +1396,7 @@ zvc_status product_of(const GluArgs<T>& p, const Cut& cut, float* sums, hipStrea
 template <typename T, class S>
 zvc_status gradients_of(const GluArgs<T>& p, const Pair& pair, float* sums, hipStream_t stream) {
     Plan dx = plan_of<Does::kDx, S>(pair.dx, p.m, p.n, p.k, sums), dw = plan_of<Does::kDw, S>(pair.dw, p.m, p.n, p.k, sums + pair.dx.sums / 4);
-    const Plan nothing{nullptr, 0, 0, 0, 1};
+    const Plan nothing{nullptr, 0, 0, 0, 1, false};
     if (p.dx == nullptr) dx = nothing;
     if (p.dwg == nullptr) dw = nothing;
     const unsigned items = dx.items() + dw.items(), room = kUnits * S::kPerUnit;

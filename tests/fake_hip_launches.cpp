@@ -16,13 +16,14 @@ std::string text, names;
 struct Plan {
     float* sums;
     unsigned tp, tq, whole, parts;
+    bool past;
 };
 void say_plan(const char* label, const void* at) {
     Plan p;
     std::memcpy(&p, at, sizeof p);
     char line[200];
-    std::snprintf(line, sizeof line, " %s_tiles=%u %s_whole=%u %s_parts=%u %s_sums=%zu", label, p.tp * p.tq, label, p.whole, label,
-                  p.parts, label, reinterpret_cast<size_t>(p.sums));
+    std::snprintf(line, sizeof line, " %s_tiles=%u %s_whole=%u %s_parts=%u %s_sums=%zu %s_past=%d", label, p.tp * p.tq, label,
+                  p.whole, label, p.parts, label, reinterpret_cast<size_t>(p.sums), label, p.past);
     text += line;
 }
 bool is(const std::string& name, const char* kernel) { return name.find(kernel) != std::string::npos; }

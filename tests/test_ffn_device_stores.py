@@ -12,3 +12,15 @@ def test_dropout_leaves_its_output_to_the_caches(assembly):  # noqa: F811
     for name, body in kernels.items():
         stores = re.findall(r"^\s*(global_store_\w+ .*?)(?:\s*//.*)?$", body, flags=re.M)
         assert len(stores) >= 2 and not any(re.search(r"\bnt\b", x) for x in stores), name
+
+
+def test_large_tiles_have_both_kinds_of_stores(assembly):  # noqa: F811
+    """A call that asks for stores past the caches gets them, and one that does not does not: of two alike behind a branch the
+    compiler would have made one."""
+    kernels = {name: body for name, body in functions(assembly, "product_kernel").items()
+               if "DoesE0E" in name and "Li4ELi2ELi4ELi8E" in name}
+    assert len(kernels) == 2
+    for name, body in kernels.items():
+        stores = re.findall(r"^\s*(global_store_dwordx4 .*?)(?:\s*//.*)?$", body, flags=re.M)
+        past = sum(bool(re.search(r"\bnt\b", x)) for x in stores)
+        assert past >= 6 * 8 and len(stores) - past >= 6 * 8, name            # four activations, gate and up; eight rows a lane

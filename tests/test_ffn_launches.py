@@ -73,8 +73,8 @@ def run(fake, calls):
     return set(kernels), [(status, [Launch(line) for line in lines]) for status, lines in results]
 
 
-def forward(m, n, k, dtype, keep=False, drop=0, room=ROOM):
-    return ["zvc_glu_forward", [AT[0], k, AT[1], AT[2], k, AT[3], n, AT[4] * keep, AT[5] * keep, n, m, n, k, dtype, 1, drop, 1,
+def forward(m, n, k, dtype, keep=False, drop=0, room=ROOM, h=AT[3], ldh=0, gate=AT[4], ldp=0):
+    return ["zvc_glu_forward", [AT[0], k, AT[1], AT[2], k, h, ldh or n, gate * keep, AT[5] * keep, ldp or n, m, n, k, dtype, 1, drop, 1,
                                 2, 0, AT[9], room, 0]]
 
 
@@ -154,3 +154,23 @@ def test_a_dimension_of_dropouts_grid_holds_its_lanes(fake, dtype, each):
         assert v["rows"] == 1 or v["grid"] == 1 << 20             # (the kernel numbers workgroups by it)
         lanes = v["grid"] * v["rows"] * v["block"]
         assert rows * cols <= lanes * each and (v["rows"] - 1) * (1 << 20) * v["block"] * each < rows * cols
+
+
+@pytest.mark.parametrize("past,call", [
+    # as much as the caches hold, 256 MB, or more
+    (1, {"m": 16384, "n": 8192, "k": 512}), (0, {"m": 16383, "n": 8192, "k": 512}), (1, {"m": 16384, "n": 11264, "k": 4096}),
+    (1, {"m": 8192, "n": 5632, "k": 2048, "keep": True}), (0, {"m": 8192, "n": 5632, "k": 2048}),
+    (0, {"m": 1024, "n": 8192, "k": 128, "keep": True}), (0, {"m": 2000, "n": 2056, "k": 136}),
+    # rows in whole halves of 128 bytes
+    (1, {"m": 16384, "n": 11296, "k": 4096}), (0, {"m": 16384, "n": 11288, "k": 4096}), (0, {"m": 16384, "n": 11264, "k": 4096, "h": AT[3] + 32}),
+    (0, {"m": 16384, "n": 11264, "k": 4096, "ldh": 11272}), (1, {"m": 16384, "n": 11264, "k": 4096, "ldh": 11296}),
+    (0, {"m": 16384, "n": 11264, "k": 4096, "keep": True, "gate": AT[4] + 16}), (0, {"m": 16384, "n": 11264, "k": 4096, "keep": True, "ldp": 11265}),
+    (1, {"m": 16384, "n": 11264, "k": 4096, "ldp": 11265})])
+def test_what_goes_past_the_caches(fake, past, call):
+    """A forward call's outputs where they do not fit and are written in whole pieces; never dg and du, which are read next."""
+    for dtype in (BF16, FP16):
+        _, results = run(fake, [forward(dtype=dtype, **call), backward(call["m"], call["n"], call["k"], dtype)])
+        (status, first), (_, again) = results
+        product = [x for x in first if x.kernel == "product_kernel"]
+        assert status == 0 and product[0].route().startswith("large") and product[0].values["p_past"] == past
+        assert all(x.values.get(of + "_past", 0) == 0 for x in again for of in ("p", "dx", "dw"))
