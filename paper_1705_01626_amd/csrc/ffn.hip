@@ -1368,18 +1368,22 @@ unsigned join_blocks(const Plan& plan) {
     return static_cast<unsigned>(div_up(size_t{plan.tp * plan.tq - plan.whole} * (S::QT * Tile<T, DOES, S>::kCols / 8), 256));
 }
 
-constexpr size_t kCacheBytes = size_t{256} << 20;  // of the cache in front of the memory
+constexpr size_t kCacheBytes = size_t{256} << 20, kL2Bytes = size_t{32} << 20;      // in front of the memory; of the XCDs' L2 together
+constexpr unsigned kLongSum = 2048;              // k from which on the products take longer than the outputs' way to memory
 
-// Whether a forward call's outputs go past the caches and leave the operands there: as much as the caches hold or more, in rows that are
-// whole halves of the memory's 128 bytes (others are written in pieces that nothing puts together any more).  us, past | not, relu
-// and dropout, alone, with a product that reads h, with the codec that reads the kept projections or else h: 8192 x 5632 x 2048 kept
-// (264 MB in all) 340 | 370, 474 | 495, 399 | 403; 16384 x 8192 x 512 (256) 309 | 333, 473 | 507, 395 | 401; 16384 x 11264 x 1024 (352) 680 | 740, 942 | 988, 790 | 838.
-// Less: 8192 x 4096 x 1024 kept (192) 164 | 151, 222 | 208, 212 | 190; 1024 x 8192 x 128 kept (48) 25 | 20.6, 41 | 35, 43 | 39; 8192 x 5632 x 2048 (88)
-// 312 | 316, 441 | 442, 343 | 345.  Rows of 11280 bytes: 8192 x 5640 x 2048 kept 434 | 389, 589 | 543, 492 | 417; of 11328 343 | 374, 486 | 518, 400 | 408.
+// Whether a forward call's outputs go past the caches and leave the operands there: as much as the caches hold or more, or an h
+// larger than L2 behind long sums; in rows that are whole halves of the memory's 128 bytes (others are written in pieces that nothing
+// puts together any more).  us, past | not, relu and dropout, alone, with a product that reads h, with the codec that reads the kept
+// projections or else h: 8192 x 5632 x 2048 kept (264 MB in all) 340 | 370, 474 | 495, 399 | 403; 16384 x 8192 x 512 (256) 309 | 333, 473 | 507,
+// 395 | 401; 16384 x 11264 x 1024 (352) 680 | 740, 942 | 988, 790 | 838.  Short sums and less: 8192 x 4096 x 1024 kept (192) 164 | 151, 222 | 208,
+// 212 | 190; 1024 x 8192 x 128 kept (48) 25 | 20.6, 41 | 35, 43 | 39.  Long sums and less, three sets of inputs in turn: 4096 x 5632 x 2048 (44) 159 | 169,
+// kept (132) 178 | 189; 8192 x 4096 x 2048 kept (192) 245 | 274; in a chain of eight blocks, each with its product and dropout, the first
+// 269 | 271, 291 | 291, with the codec 331 | 324.  Rows of 11280 bytes: 8192 x 5640 x 2048 kept 434 | 389, 589 | 543, 492 | 417; of 11328 343 | 374, 486 | 518, 400 | 408.
 template <typename T>
 bool past_caches(const GluArgs<T>& p) {
     const auto whole = [&](const T* at, unsigned ld) { return at == nullptr || (aligned_to(at, 64) && size_t{ld} * sizeof(T) % 64 == 0); };
-    return size_t{p.m} * p.n * sizeof(T) * (p.gate != nullptr ? 3 : 1) >= kCacheBytes && whole(p.h, p.ldh) && whole(p.gate, p.ldp) && whole(p.up, p.ldp);
+    const size_t bytes = size_t{p.m} * p.n * sizeof(T), all = p.gate != nullptr ? 3 * bytes : bytes;
+    return (all >= kCacheBytes || (p.k >= kLongSum && bytes > kL2Bytes)) && whole(p.h, p.ldh) && whole(p.gate, p.ldp) && whole(p.up, p.ldp);
 }
 
 template <typename T, Does DOES, class S>

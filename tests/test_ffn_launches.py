@@ -159,15 +159,18 @@ def test_a_dimension_of_dropouts_grid_holds_its_lanes(fake, dtype, each):
 @pytest.mark.parametrize("past,call", [
     # as much as the caches hold, 256 MB, or more
     (1, {"m": 16384, "n": 8192, "k": 512}), (0, {"m": 16383, "n": 8192, "k": 512}), (1, {"m": 16384, "n": 11264, "k": 4096}),
-    (1, {"m": 8192, "n": 5632, "k": 2048, "keep": True}), (0, {"m": 8192, "n": 5632, "k": 2048}),
-    (0, {"m": 1024, "n": 8192, "k": 128, "keep": True}), (0, {"m": 2000, "n": 2056, "k": 136}),
+    (1, {"m": 16384, "n": 2816, "k": 1024, "keep": True}), (0, {"m": 16384, "n": 2816, "k": 1024}),
+    # behind long sums more than 32 MB of h
+    (1, {"m": 4096, "n": 5632, "k": 2048}), (0, {"m": 4096, "n": 5632, "k": 2047, "keep": True}), (0, {"m": 4096, "n": 4096, "k": 2048}),
+    (1, {"m": 4097, "n": 4096, "k": 4096}), (0, {"m": 1024, "n": 8192, "k": 128, "keep": True}), (0, {"m": 2000, "n": 2056, "k": 136}),
     # rows in whole halves of 128 bytes
     (1, {"m": 16384, "n": 11296, "k": 4096}), (0, {"m": 16384, "n": 11288, "k": 4096}), (0, {"m": 16384, "n": 11264, "k": 4096, "h": AT[3] + 32}),
     (0, {"m": 16384, "n": 11264, "k": 4096, "ldh": 11272}), (1, {"m": 16384, "n": 11264, "k": 4096, "ldh": 11296}),
     (0, {"m": 16384, "n": 11264, "k": 4096, "keep": True, "gate": AT[4] + 16}), (0, {"m": 16384, "n": 11264, "k": 4096, "keep": True, "ldp": 11265}),
     (1, {"m": 16384, "n": 11264, "k": 4096, "ldp": 11265})])
 def test_what_goes_past_the_caches(fake, past, call):
-    """A forward call's outputs where they do not fit and are written in whole pieces; never dg and du, which are read next."""
+    """A forward call's outputs where the caches do not hold them or the products take long, written in whole pieces; never dg and du,
+    which are read next."""
     for dtype in (BF16, FP16):
         _, results = run(fake, [forward(dtype=dtype, **call), backward(call["m"], call["n"], call["k"], dtype)])
         (status, first), (_, again) = results
