@@ -55,7 +55,9 @@ typedef enum zvc_type { ZVC_FP32 = 0, ZVC_FP16 = 1, ZVC_BF16 = 2 } zvc_type;
 
 /* act(g).  relu: max(g, 0), with derivative 0 at 0; silu: g / (1 + exp(-g)); gelu:
  * g times the normal distribution function of g; gelu_tanh: its approximation
- * g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2.  A NaN stays one. */
+ * g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2.  A NaN stays one.
+ * Computed in 32 bits: relative to the value within (16 + 9 z) 2^-24, z the argument of its exp (silu |g|,
+ * gelu g^2 / 2), and gelu of 16-bit types within 2^-15 more. */
 typedef enum zvc_activation { ZVC_RELU = 0, ZVC_SILU = 1, ZVC_GELU = 2, ZVC_GELU_TANH = 3 } zvc_activation;
 
 /* The largest n, k and row stride. */
@@ -93,7 +95,8 @@ zvc_status zvc_glu_forward(const void* d_x, size_t ldx, const void* d_wg, const 
  * the forward call.  d_gate and d_up as that call left them (or after a round trip through
  * the codec), or both null: then the projections are computed again, which
  * costs half as much again and keeps nothing.  dg and du are rounded to the element type between
- * the products.  d_dx may be null, and so may both of d_dwg and d_dwu: what is null is not computed. */
+ * the products (fp16: what is beyond 65504 there becomes an infinity, also where the gradients
+ * themselves would not).  d_dx may be null, and so may both of d_dwg and d_dwu: what is null is not computed. */
 zvc_status zvc_glu_backward(const void* d_dh, size_t lddh, const void* d_x, size_t ldx, const void* d_wg,
                             const void* d_wu, size_t ldw, const void* d_gate, const void* d_up, size_t ldp, void* d_dx,
                             size_t lddx, void* d_dwg, void* d_dwu, size_t lddw, size_t m, size_t n, size_t k, int type,

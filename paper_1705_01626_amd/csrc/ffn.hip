@@ -8,8 +8,9 @@
 //   * token_kernel: the projections of up to 128 tokens, bound by reading the weights once.
 //   * slope_kernel: dg and du from kept projections; align_kernel: copies of inputs that do not take 16-byte accesses.
 //
-// Times in the comments are us on one MI355X, where a large copy moves 5.0 TB/s and a large bf16 product of the vendor's library
-// reaches 1260 to 1460 TFLOP/s (fp32 155).
+// Times in the comments are us on one MI355X, where a large copy moves 4.8 to 5.0 TB/s and a large bf16 product of the vendor's library
+// reaches 1230 to 1460 TFLOP/s (fp32 155): calls one behind the other over several sets of tensors.  Cards differ by 6 % in long
+// products, and the first milliseconds on a card that was idle run up to a third longer; both sides of a comparison ran in turn.
 
 #include "zvc_ffn.h"
 
@@ -755,9 +756,9 @@ constexpr unsigned kNone = ~0u;                  // no work item
 
 // Workgroups take tiles until there are none left; the next tile's first stages are on their way while a tile is finished.
 //
-// What bounds it, with the large tile: the card's power.  16384 x 11264 x 4096 (forward, bf16) takes 2220 to 2260, 1340 to 1360
-// TFLOP/s: 0.485 for each step of k, at which the matrix cores are busy for 87 % of the cycles of a clock that is held near
-// 1.7 GHz, and the rest to begin and finish 22 tiles.  LDS is next: a half stage's reads take 768 of its 1024 cycles.  Four waves
+// What bounds it, with the large tile: the card's power.  16384 x 11264 x 4096 (forward, bf16) takes 2170 to 2300 on different cards, 1310
+// to 1390 TFLOP/s.  Where it took 2220 to 2260: 0.485 for each step of k, at which the matrix cores are busy for 87 % of the cycles of a
+// clock that is held near 1.7 GHz, and the rest to begin and finish 22 tiles.  LDS is next: a half stage's reads take 768 of its 1024 cycles.  Four waves
 // of 128 x 128 with sums in accumulation registers read a third less, 0.472 a step, and finish tiles so much slower that it
 // is 2700 in all; instructions of 32 x 32 2430; a ring of five half stages 2660; one wave at a raised priority 2360; without the
 // reads between the products 2540; with tiles that are not persistent and epilogues with a branch per element 2440.  Small tiles
