@@ -20,6 +20,7 @@ LIBRARY = os.path.join(PKG, "libzvc.so")
 FFN_SOURCE = os.path.join(PKG, "csrc", "ffn.hip")
 FFN_LIBRARY = os.path.join(PKG, "libzvc_ffn.so")
 FFN_HEADER = os.path.join(ROOT, "include", "zvc_ffn.h")
+SHARED = [os.path.join(PKG, "csrc", name) for name in ("elements.h", "tiles.h")]
 CALLS_SOURCE = os.path.join(PKG, "csrc", "calls.cpp")
 HEADER = os.path.join(ROOT, "include", "zvc.h")
 CALLS = os.path.join(PKG, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))   # no other interpreter loads it
@@ -67,7 +68,7 @@ def ensure_built() -> str:
     """Build only what is not built yet (or whose sources are newer)."""
     if _older(LIBRARY, SOURCE, HEADER):
         build()
-    if _older(FFN_LIBRARY, FFN_SOURCE, FFN_HEADER, HEADER):
+    if _older(FFN_LIBRARY, FFN_SOURCE, *SHARED, FFN_HEADER, HEADER):
         build_ffn()
     if _older(CALLS, CALLS_SOURCE, HEADER, FFN_HEADER):
         build_calls()
