@@ -1,5 +1,6 @@
 """Compile in-tree: csrc/zvc.hip -> paper_1705_01626_amd/libzvc.so (the HIP library of the codec),
-csrc/ffn.hip -> libzvc_ffn.so (that of the training operators), csrc/adamw.hip -> libzvc_adamw.so (the optimizer's step) and csrc/calls.cpp -> paper_1705_01626_amd/_calls.<interpreter's tag>.so (their entry from Python,
+csrc/ffn.hip -> libzvc_ffn.so (that of the training operators), csrc/experts.hip -> libzvc_experts.so (mixtures of experts),
+csrc/adamw.hip -> libzvc_adamw.so (the optimizer's step) and csrc/calls.cpp -> paper_1705_01626_amd/_calls.<interpreter's tag>.so (their entry from Python,
 which is left out where the interpreter's headers are not installed).
 
 Usage: python -m paper_1705_01626_amd.build
@@ -20,6 +21,9 @@ LIBRARY = os.path.join(PKG, "libzvc.so")
 FFN_SOURCE = os.path.join(PKG, "csrc", "ffn.hip")
 FFN_LIBRARY = os.path.join(PKG, "libzvc_ffn.so")
 FFN_HEADER = os.path.join(ROOT, "include", "zvc_ffn.h")
+EXPERTS_SOURCE = os.path.join(PKG, "csrc", "experts.hip")
+EXPERTS_LIBRARY = os.path.join(PKG, "libzvc_experts.so")
+EXPERTS_HEADER = os.path.join(ROOT, "include", "zvc_experts.h")
 ADAMW_SOURCE = os.path.join(PKG, "csrc", "adamw.hip")
 ADAMW_LIBRARY = os.path.join(PKG, "libzvc_adamw.so")
 ADAMW_HEADER = os.path.join(ROOT, "include", "zvc_adamw.h")
@@ -46,6 +50,12 @@ def build(output: str = LIBRARY, extra=()) -> str:
 
 def build_ffn(output: str = FFN_LIBRARY, extra=()) -> str:
     cmd = [HIPCC, *FLAGS, *extra, "-I", os.path.join(ROOT, "include"), "-o", output, FFN_SOURCE]
+    subprocess.run(cmd, check=True)
+    return output
+
+
+def build_experts(output: str = EXPERTS_LIBRARY, extra=()) -> str:
+    cmd = [HIPCC, *FLAGS, *extra, "-I", os.path.join(ROOT, "include"), "-o", output, EXPERTS_SOURCE]
     subprocess.run(cmd, check=True)
     return output
 
@@ -79,9 +89,11 @@ def ensure_built() -> str:
         build()
     if _older(FFN_LIBRARY, FFN_SOURCE, *SHARED, FFN_HEADER, HEADER):
         build_ffn()
+    if _older(EXPERTS_LIBRARY, EXPERTS_SOURCE, *SHARED, EXPERTS_HEADER, FFN_HEADER, HEADER):
+        build_experts()
     if _older(ADAMW_LIBRARY, ADAMW_SOURCE, *SHARED, ADAMW_HEADER, FFN_HEADER, HEADER):
         build_adamw()
-    if _older(CALLS, CALLS_SOURCE, HEADER, FFN_HEADER, ADAMW_HEADER):
+    if _older(CALLS, CALLS_SOURCE, HEADER, FFN_HEADER, EXPERTS_HEADER, ADAMW_HEADER):
         build_calls()
     return LIBRARY
 
@@ -89,5 +101,6 @@ def ensure_built() -> str:
 if __name__ == "__main__":
     print(build(extra=sys.argv[1:]))
     print(build_ffn(extra=sys.argv[1:]))
+    print(build_experts(extra=sys.argv[1:]))
     print(build_adamw(extra=sys.argv[1:]))
     print(build_calls())

@@ -1,5 +1,5 @@
-// Python entry to the device calls of libzvc (include/zvc.h), libzvc_ffn (include/zvc_ffn.h) and libzvc_adamw
-// (include/zvc_adamw.h): the same arguments as the C functions, as integers, and the status as the result.  A call through
+// Python entry to the device calls of libzvc (include/zvc.h), libzvc_ffn (include/zvc_ffn.h), libzvc_experts
+// (include/zvc_experts.h) and libzvc_adamw (include/zvc_adamw.h): the same arguments as the C functions, as integers, and the status as the result.  A call through
 // ctypes converts its nine or ten arguments one object at a time, 3 us of a call
 // whose kernel takes 4; here they are read from the interpreter's argument array.
 // The interpreter lock is released during the call, as ctypes does.
@@ -8,6 +8,7 @@
 
 #include "zvc.h"
 #include "zvc_adamw.h"
+#include "zvc_experts.h"
 #include "zvc_ffn.h"
 
 #include <dlfcn.h>
@@ -86,6 +87,7 @@ bool bind(void* library, const char* name) {
     DO(zvc_prefetch)
 #define ZVC_FFN_FUNCTIONS(DO) \
     DO(zvc_dropout) DO(zvc_glu_workspace_bytes) DO(zvc_glu_forward) DO(zvc_glu_backward)
+#define ZVC_EXPERTS_FUNCTIONS(DO) DO(zvc_route) DO(zvc_route_backward) DO(zvc_expert_product) DO(zvc_expert_gradients)
 #define ZVC_ADAMW_FUNCTIONS(DO) DO(zvc_adamw)
 
 void* library_at(PyObject* path) {
@@ -114,6 +116,14 @@ PyObject* open_ffn_library(PyObject*, PyObject* path) {
     Py_RETURN_NONE;
 }
 
+// open_experts(path): the same for the mixtures of experts.
+PyObject* open_experts_library(PyObject*, PyObject* path) {
+    void* library = library_at(path);
+    if (library == nullptr) return nullptr;
+    ZVC_EXPERTS_FUNCTIONS(ZVC_BIND)
+    Py_RETURN_NONE;
+}
+
 // open_adamw(path): the same for the optimizer's step.
 PyObject* open_adamw_library(PyObject*, PyObject* path) {
     void* library = library_at(path);
@@ -126,11 +136,13 @@ PyObject* open_adamw_library(PyObject*, PyObject* path) {
 PyMethodDef methods[] = {
     {"open", open_library, METH_O, nullptr},
     {"open_ffn", open_ffn_library, METH_O, nullptr},
+    {"open_experts", open_experts_library, METH_O, nullptr},
     {"open_adamw", open_adamw_library, METH_O, nullptr},
 #define ZVC_ENTRY(NAME) \
     {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<&NAME>)), METH_FASTCALL, nullptr},
     ZVC_FUNCTIONS(ZVC_ENTRY)
     ZVC_FFN_FUNCTIONS(ZVC_ENTRY)
+    ZVC_EXPERTS_FUNCTIONS(ZVC_ENTRY)
     ZVC_ADAMW_FUNCTIONS(ZVC_ENTRY)
 #undef ZVC_ENTRY
     {nullptr, nullptr, 0, nullptr}};
