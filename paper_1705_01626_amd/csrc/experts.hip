@@ -294,45 +294,409 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs p) {
 }
 
 // ------------------------------------------------------------------ the experts' products
-template <typename T>
-struct ExpertArgs {
-    const T *x, *w, *dy;
-    T *y, *dx, *dw;
-    size_t ldx, ldw, sw, ldy, lddx, lddw, sdw;
-    const int64_t* offsets;
-    unsigned m, experts, n, k;
-};
-
-__device__ __forceinline__ unsigned start_of(const int64_t* offsets, unsigned e, unsigned m) {
-    int64_t most = 0;
-    for (unsigned i = 0; i <= e; ++i) most = max(most, offsets[i]);
-    return static_cast<unsigned>(min(most, static_cast<int64_t>(m)));
-}
-
+//
+// Every product is  out[row][col] = sum over t of Q(row, t) P(col, t)  within one expert, in the terms of tiles.h:  forward  P = W, Q = x;
+// dx  P = W by columns, Q = dy;  dW  P = x by columns, Q = dy by columns, the sum over the expert's rows.
 enum class Does { kForward, kDx, kDw };
 
-// A thread for each element of an output, one expert after the other.
-template <typename T, Does DOES>
-__global__ __launch_bounds__(256) void plain_kernel(ExpertArgs<T> p) {
-    const unsigned e = blockIdx.z, begin = start_of(p.offsets, e, p.m), end = start_of(p.offsets, e + 1, p.m);
-    const unsigned cols = DOES == Does::kForward ? p.n : p.k, col = blockIdx.x * 64 + threadIdx.x % 64;
-    const unsigned rows = DOES == Does::kDw ? p.n : end - begin;
-    if (col >= cols) return;
-    for (unsigned row = blockIdx.y * 4 + threadIdx.x / 64; row < rows; row += gridDim.y * 4) {
-        float sum = 0.f;
-        if constexpr (DOES == Does::kForward) {
-            for (unsigned t = 0; t < p.k; ++t)
-                sum += static_cast<float>(p.x[(begin + row) * p.ldx + t]) * static_cast<float>(p.w[e * p.sw + col * p.ldw + t]);
-            p.y[(begin + row) * p.ldy + col] = static_cast<T>(sum);
-        } else if constexpr (DOES == Does::kDx) {
-            for (unsigned t = 0; t < p.n; ++t)
-                sum += static_cast<float>(p.dy[(begin + row) * p.ldy + t]) * static_cast<float>(p.w[e * p.sw + t * p.ldw + col]);
-            p.dx[(begin + row) * p.lddx + col] = static_cast<T>(sum);
-        } else {
-            for (unsigned t = begin; t < end; ++t)
-                sum += static_cast<float>(p.dy[t * p.ldy + row]) * static_cast<float>(p.x[t * p.ldx + col]);
-            p.dw[e * p.sdw + row * p.lddw + col] = static_cast<T>(sum);
+template <typename T>
+struct ExpertArgs {
+    const T *p, *q;
+    T* out;
+    size_t sp, so;                       // from an expert's P, or its output, to the next one's
+    const int64_t* offsets;
+    unsigned ldp, ldq, ldo, m, experts, cols, rows, length;   // rows: of dW; length: of the sum (dW: unused)
+};
+
+// Where each expert's rows begin and which tile is its first, in LDS.  (As many words as there can be experts, no more: with the
+// smaller tiles' rings two workgroups fill a compute unit's LDS.)
+struct Groups {
+    unsigned *starts, *firsts;
+    unsigned experts, end, items;
+
+    __device__ __forceinline__ unsigned start(unsigned e) const { return e < experts ? starts[e] : end; }
+    __device__ __forceinline__ unsigned rows(unsigned e) const { return start(e + 1) - start(e); }
+    // The expert of a tile: the last one whose first tile is not behind it.
+    __device__ __forceinline__ unsigned expert_of(unsigned item, int lane) const {
+        unsigned low = 0, left = experts;
+        while (left > 1) {
+            const unsigned stride = (left + 63) / 64, at = lane * stride;
+            const bool before = at < left && firsts[low + at] <= item;
+            const unsigned last = static_cast<unsigned>(__popcll(__ballot(before))) - 1;
+            low += last * stride;
+            left = min(stride, left - last * stride);
         }
+        return __builtin_amdgcn_readfirstlane(low);
+    }
+};
+
+// f over a workgroup's threads in their order, inclusive; the last one's in `all`.  `room`: a word for each wave.
+template <int THREADS, typename F>
+__device__ __forceinline__ unsigned running(unsigned x, unsigned* room, unsigned* all, F f) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const unsigned before = __shfl_up(x, d);
+        x = lane >= d ? f(x, before) : x;
+    }
+    if (lane == 63) room[wave] = x;
+    __syncthreads();
+    unsigned sum = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        if (w == wave && w != 0) x = f(x, sum);
+        sum = w == 0 ? room[0] : f(sum, room[w]);
+    }
+    *all = sum;
+    __syncthreads();
+    return x;
+}
+
+// Offsets that go down count as the one before, and none lies outside the rows: no table holds what would lead out of them.
+template <int THREADS>
+__device__ __forceinline__ Groups groups_of(const int64_t* offsets, unsigned experts, unsigned m, unsigned across, unsigned tile_rows, unsigned* table, unsigned* room) {
+    constexpr unsigned kEach = ZVC_EXPERTS_MAX / THREADS;
+    Groups g{table, table + ZVC_EXPERTS_MAX, experts, 0, 0};
+    unsigned at[kEach + 1], most = 0;
+#pragma unroll
+    for (unsigned j = 0; j < kEach; ++j) {
+        const unsigned e = threadIdx.x * kEach + j;
+        const int64_t offset = e <= experts ? offsets[e] : 0;
+        most = max(most, static_cast<unsigned>(min(max(offset, int64_t{0}), static_cast<int64_t>(m))));
+        at[j] = most;
+    }
+    const int64_t last = experts == ZVC_EXPERTS_MAX ? offsets[experts] : 0;
+    unsigned all;
+    const unsigned through = running<THREADS>(most, room, &all, [](unsigned a, unsigned b) { return max(a, b); });
+    const unsigned before = __shfl_up(through, 1);
+    if ((threadIdx.x & 63) == 63) room[threadIdx.x >> 6] = through;
+    __syncthreads();
+    const unsigned carried = (threadIdx.x & 63) != 0 ? before : threadIdx.x != 0 ? room[(threadIdx.x >> 6) - 1] : 0;
+    __syncthreads();
+#pragma unroll
+    for (unsigned j = 0; j < kEach; ++j) at[j] = max(at[j], carried);
+    g.end = max(all, static_cast<unsigned>(min(max(last, int64_t{0}), static_cast<int64_t>(m))));
+#pragma unroll
+    for (unsigned j = 0; j < kEach; ++j)
+        if (threadIdx.x * kEach + j < experts) g.starts[threadIdx.x * kEach + j] = at[j];
+    __syncthreads();
+    unsigned own[kEach], sum = 0;
+#pragma unroll
+    for (unsigned j = 0; j < kEach; ++j) {
+        const unsigned e = threadIdx.x * kEach + j;
+        own[j] = e < experts ? across * ((g.rows(e) + tile_rows - 1) / tile_rows) : 0;
+        sum += own[j];
+    }
+    unsigned first = running<THREADS>(sum, room, &g.items, [](unsigned a, unsigned b) { return a + b; }) - sum;
+#pragma unroll
+    for (unsigned j = 0; j < kEach; ++j) {
+        const unsigned e = threadIdx.x * kEach + j;
+        if (e < experts) g.firsts[e] = first;
+        first += own[j];
+    }
+    __syncthreads();
+    return g;
+}
+
+// One workgroup's view of a tile.
+template <typename T, Does DOES, class S>
+struct Tile {
+    static constexpr Lies kP = DOES == Does::kForward ? Lies::kAlong : Lies::kAcross, kQ = DOES == Does::kDw ? Lies::kAcross : Lies::kAlong;
+    static constexpr int W = sizeof(T), kSteps = kStageBytes / W;
+    using InP = Operand<T, kP, S::PT, S::kWavesAll, false>;
+    using InQ = Operand<T, kQ, S::QT, S::kWavesAll, false>;
+
+    unsigned col0, row0, end;            // of the output; the first row that is not the tile's expert's
+    unsigned length, stages;
+    T* out;
+    const T *p, *q;
+    InP in_p;
+    InQ in_q;
+
+    // Tiles of an expert are walked in bands of some rows: what the workgroups of an XCD read at a time then fits its L2.
+    __device__ __forceinline__ void locate(unsigned at, unsigned tp, unsigned tq) {
+        constexpr unsigned kBand = DOES == Does::kForward ? 8 : 4;
+        const unsigned band = at / (kBand * tp), in_band = at % (kBand * tp), height = tq - band * kBand < kBand ? tq - band * kBand : kBand;
+        col0 = in_band / height * S::PT;
+        row0 = (band * kBand + in_band % height) * S::QT;
+    }
+    __device__ __forceinline__ void init(const ExpertArgs<T>& a, const Groups& g, unsigned items, unsigned item, int wave, int lane) {
+        const unsigned at = place_of(item, items), tp = (a.cols + S::PT - 1) / S::PT;
+        unsigned e;
+        if constexpr (DOES == Does::kDw) {
+            const unsigned tq = (a.rows + S::QT - 1) / S::QT;
+            e = at / (tp * tq);
+            locate(at - e * (tp * tq), tp, tq);
+            const unsigned begin = __builtin_amdgcn_readfirstlane(g.start(e));
+            end = a.rows;
+            length = __builtin_amdgcn_readfirstlane(g.start(e + 1)) - begin;
+            p = cell(a.p, begin, a.ldp, col0);
+            q = cell(a.q, begin, a.ldq, row0);
+            out = a.out + e * a.so;
+        } else {
+            e = g.expert_of(at, lane);
+            const unsigned begin = __builtin_amdgcn_readfirstlane(g.start(e));
+            end = __builtin_amdgcn_readfirstlane(g.start(e + 1));
+            locate(at - __builtin_amdgcn_readfirstlane(g.firsts[e]), tp, (end - begin + S::QT - 1) / S::QT);
+            row0 += begin;
+            length = a.length;
+            p = a.p + e * a.sp;
+            p = DOES == Does::kForward ? cell(p, col0, a.ldp, 0) : p + col0;
+            q = cell(a.q, row0, a.ldq, 0);
+            out = a.out;
+        }
+        stages = (length + kSteps - 1) / kSteps;
+        in_p.init(wave, lane, a.ldp, a.cols - col0 < S::PT ? a.cols - col0 : S::PT);
+        in_q.init(wave, lane, a.ldq, end - row0 < S::QT ? end - row0 : S::QT);
+    }
+    __device__ __forceinline__ void fetch(const ExpertArgs<T>& a, unsigned s, unsigned lds) const {
+        const uint64_t step_p = DOES == Does::kForward ? kStageBytes : uint64_t{kSteps} * W * a.ldp;
+        const uint64_t step_q = DOES == Does::kDw ? uint64_t{kSteps} * W * a.ldq : kStageBytes;
+        const int left = static_cast<int>(length - s * kSteps);
+        in_p.fetch(reinterpret_cast<uint64_t>(p) + s * step_p, 0, left, lds);
+        in_q.fetch(reinterpret_cast<uint64_t>(q) + s * step_q, 0, left, lds + S::PT * kStageBytes);
+    }
+};
+
+// A tile's sums as they go out: a lane has four neighbouring columns of each of its blocks.
+template <typename T, class S>
+__device__ __forceinline__ void store_tile(T* out, unsigned ldo, unsigned rows, unsigned cols, unsigned row_first, unsigned col_first, bool full, const float4v (&acc)[S::PB][S::QB]) {
+    struct Four { T v[4]; };
+    const auto four = [&](int i, int j) {
+        Four f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f.v[e] = static_cast<T>(acc[i][j][e]);
+        return f;
+    };
+#pragma unroll
+    for (int j = 0; j < S::QB; ++j) {
+        T* const at = cell(out, row_first + j * 16, ldo, col_first);
+        if (row_first + j * 16 >= rows) continue;
+        if (full) {
+#pragma unroll
+            for (int i = 0; i < S::PB; ++i) {
+                const Four f = four(i, j);
+                __builtin_memcpy(at + i * 16, &f, sizeof f);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < S::PB; ++i) {
+                const Four f = four(i, j);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col_first + i * 16 + e < cols) at[i * 16 + e] = f.v[e];
+            }
+        }
+    }
+}
+
+// The sums of a stage that lies in LDS.
+template <typename T, Does DOES, class S>
+struct Multiplier {
+    using Where = Tile<T, DOES, S>;
+    using ReadP = Reader<T, Where::kP, S::PT, S::PB, false>;
+    using ReadQ = Reader<T, Where::kQ, S::QT, S::QB, false>;
+    using Frag = typename Fragment<T>::type;
+    ReadP out_p;
+    ReadQ out_q;
+    Frag a[2][S::PB], b[2][S::QB];
+    float4v acc[S::PB][S::QB];
+
+    __device__ __forceinline__ void init(unsigned base, int wp, int wq, int lane) {
+        out_p.init(base, wp, lane);
+        out_q.init(base + S::PT * kStageBytes, wq, lane);
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < S::PB; ++i)
+#pragma unroll
+            for (int j = 0; j < S::QB; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
+    }
+    template <int HALF>
+    __device__ __forceinline__ void read(unsigned stage) {
+#pragma unroll
+        for (int i = 0; i < S::PB; ++i) a[HALF][i] = out_p.read(i, HALF, stage);
+#pragma unroll
+        for (int j = 0; j < S::QB; ++j) b[HALF][j] = out_q.read(j, HALF, stage);
+    }
+    template <int HALF>
+    __device__ __forceinline__ void product() {
+#pragma unroll
+        for (int j = 0; j < S::QB; ++j)
+#pragma unroll
+            for (int i = 0; i < S::PB; ++i) acc[i][j] = multiply(a[HALF][i], b[HALF][j], acc[i][j]);
+        interleave<ReadP::kReads + ReadQ::kReads, S::PB * S::QB * (sizeof(T) == 4 ? 4 : 1)>();
+    }
+};
+
+// Workgroups take tiles until there are none left; the next tile's first stages are on their way while a tile is finished.
+template <typename T, Does DOES, class S, typename Next>
+__device__ __forceinline__ void work(const ExpertArgs<T>& p, const Groups& groups, unsigned items, unsigned base, int lane, Next next) {
+    using Where = Tile<T, DOES, S>;
+    constexpr int kRing = S::kRing;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wp = wave % S::WP, wq = wave / S::WP, r = lane & 15, quarter = lane >> 4;
+    Multiplier<T, DOES, S> x;
+    x.init(base, wp, wq, lane);
+    Where tile;
+    const auto begin = [&](unsigned item) {
+        tile.init(p, groups, items, item, wave, lane);
+#pragma unroll
+        for (unsigned i = 0; i < kRing; ++i)
+            if (i < tile.stages) tile.fetch(p, i, base + i * S::kStage);
+    };
+    // Waits until the loads of `stages` stages at most are on their way, if as many as the ring holds were asked for.
+    constexpr int kLoads = Where::InP::kLoads + Where::InQ::kLoads;
+    const auto wait_stages = [&](auto stages, bool full) {
+        constexpr int kLeft = decltype(stages)::value * kLoads;
+        if (kLeft != 0 && full) wait_loads<kLeft>();
+        else wait_loads<0>();
+    };
+    const auto place = [&](unsigned s) { return (s & (kRing - 1)) * S::kStage; };
+    static_assert((kRing & (kRing - 1)) == 0, "stages take places in turn");
+    unsigned item = next();
+    if (item == kNone) return;
+    begin(item);
+    while (item != kNone) {
+        x.clear();
+        // A stage is multiplied in two halves.  While a half's products run, the next half is read from LDS; between
+        // the halves everyone has read the stage, and its place takes the one after the ring's last.
+        if (tile.stages != 0) {                  // (dW of an expert without rows: 0)
+            wait_stages(std::integral_constant<int, kRing - 1>{}, kRing <= tile.stages);
+            group_barrier();
+            x.template read<0>(0);
+            for (unsigned s = 0; s < tile.stages; ++s) {
+                x.template read<1>(place(s));
+                x.template product<0>();
+                wait_stages(std::integral_constant<int, kRing - 2>{}, s + kRing <= tile.stages);
+                group_barrier();                 // stage s + 1 is there, and everyone has read stage s
+                if (s + kRing < tile.stages) tile.fetch(p, s + kRing, base + place(s));
+                x.template read<0>(place(s + 1));    // (behind the last stage: what the place held, for nothing)
+                x.template product<1>();
+            }
+        }
+        const unsigned row0 = tile.row0, col0 = tile.col0, end = tile.end;
+        T* const out = tile.out;
+        item = next();
+        group_barrier();                         // (the reads for nothing are done)
+        if (item != kNone) begin(item);
+        store_tile<T, S>(out, p.ldo, end, p.cols, row0 + wq * S::QB * 16 + r, col0 + wp * S::PB * 16 + quarter * 4, col0 + (wp + 1) * S::PB * 16 <= p.cols, x.acc);
+    }
+}
+
+// A ring's places, and the experts' tables behind them.
+template <class S>
+__device__ __forceinline__ unsigned char* room_of() {
+    __shared__ alignas(1024) unsigned char lds[S::kRing * S::kStage + 2 * ZVC_EXPERTS_MAX * sizeof(unsigned)];
+    static_assert(S::kPerUnit * sizeof lds <= 160 << 10, "a compute unit's LDS");
+    return lds;
+}
+template <class S>
+__device__ __forceinline__ Groups tables(const int64_t* offsets, unsigned experts, unsigned m, unsigned cols, unsigned char* lds) {
+    return groups_of<S::kThreads>(offsets, experts, m, (cols + S::PT - 1) / S::PT, S::QT, reinterpret_cast<unsigned*>(lds + S::kRing * S::kStage),
+                                  reinterpret_cast<unsigned*>(lds));
+}
+__device__ __forceinline__ unsigned address(unsigned char* lds) { return static_cast<unsigned>(reinterpret_cast<uintptr_t>((LdsByte*)lds)); }
+
+template <typename T, class S>
+__global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(ExpertArgs<T> p) {
+    unsigned char* const lds = room_of<S>();
+    const Groups g = tables<S>(p.offsets, p.experts, p.m, p.cols, lds);
+    work<T, Does::kForward, S>(p, g, g.items, address(lds), threadIdx.x & 63, Turns{blockIdx.x, g.items});
+}
+
+// dx, and behind it dW, in one go: either alone leaves compute units idle in its last round.  `dw_items`, and dx.cols, may be 0.
+template <typename T, class S>
+__global__ __launch_bounds__(S::kThreads, S::kPerUnit) void gradients_kernel(ExpertArgs<T> dx, ExpertArgs<T> dw, unsigned dw_items) {
+    unsigned char* const lds = room_of<S>();
+    const Groups g = tables<S>(dx.offsets, dx.experts, dx.m, dx.cols, lds);
+    // (a lane's number that is had again at any time: no register holds the thread's through both)
+    const int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
+    const unsigned first = g.items % gridDim.x, mine = blockIdx.x >= first ? blockIdx.x - first : blockIdx.x + gridDim.x - first;
+    work<T, Does::kDx, S>(dx, g, g.items, address(lds), lane, Turns{blockIdx.x, g.items});
+    work<T, Does::kDw, S>(dw, g, dw_items, address(lds), lane, Turns{mine, dw_items});
+}
+
+// ------------------------------------------------------------------ operands that do not take 16-byte accesses
+// The same places in LDS by way of registers: 16 bytes at any element, and single elements at an operand's ends, beyond which are zeros.
+template <typename T, Lies LIES, int SIDE, int WAVES>
+struct LooseOperand {
+    using Op = Operand<T, LIES, SIDE, WAVES, false>;
+    static constexpr int kPer = 16 / sizeof(T);
+    Op op;
+    Pack<T> v[Op::kLoads];
+
+    // `left`: of the reduction; `side`: rows (kAlong) or columns (kAcross) that exist.
+    __device__ __forceinline__ void load(const T* base, size_t ld, int side, int left) {
+#pragma unroll
+        for (int i = 0; i < Op::kLoads; ++i) {
+            const int row = (op.first + i) * Op::kRowsPerLoad + op.lane_row, col = op.logical(row) / static_cast<int>(sizeof(T));
+            const int rows = LIES == Lies::kAlong ? side : left, there = (LIES == Lies::kAlong ? left : side) - col;
+            const T* const at = base + row * ld + col;
+            v[i] = Pack<T>{};
+            if (row < rows && there >= kPer) {
+                __builtin_memcpy(&v[i], at, 16);
+            } else if (row < rows) {
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+                    if (j < there) v[i].v[j] = at[j];
+            }
+        }
+    }
+    __device__ __forceinline__ void store(unsigned lds, int lane) const {
+#pragma unroll
+        for (int i = 0; i < Op::kLoads; ++i)
+            *reinterpret_cast<__attribute__((address_space(3))) int4v*>(lds_at(lds + (op.first + i) * 1024 + lane * 16)) = __builtin_bit_cast(int4v, v[i]);
+    }
+};
+
+template <typename T, Does DOES, class S>
+__global__ __launch_bounds__(S::kThreads, S::kPerUnit) void loose_kernel(ExpertArgs<T> p, unsigned dw_items) {
+    static_assert(S::kRing == 2, "one stage is read while the next is written");
+    unsigned char* const lds = room_of<S>();
+    const Groups g = tables<S>(p.offsets, p.experts, p.m, p.cols, lds);
+    using Where = Tile<T, DOES, S>;
+    constexpr int kSteps = Where::kSteps;
+    const unsigned base = address(lds), items = DOES == Does::kDw ? dw_items : g.items;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wp = wave % S::WP, wq = wave / S::WP, r = lane & 15, quarter = lane >> 4;
+    Multiplier<T, DOES, S> x;
+    x.init(base, wp, wq, lane);
+    Where tile;
+    LooseOperand<T, Where::kP, S::PT, S::kWavesAll> in_p;
+    LooseOperand<T, Where::kQ, S::QT, S::kWavesAll> in_q;
+    in_p.op.init(wave, lane, 0, 0);
+    in_q.op.init(wave, lane, 0, 0);
+    for (unsigned item = blockIdx.x; item < items; item += gridDim.x) {
+        tile.init(p, g, items, item, wave, lane);
+        const int side_p = min(static_cast<int>(p.cols - tile.col0), S::PT), side_q = min(static_cast<int>(tile.end - tile.row0), S::QT);
+        const auto load = [&](unsigned s) {
+            const size_t step_p = size_t{s} * kSteps * (DOES == Does::kForward ? 1 : p.ldp), step_q = size_t{s} * kSteps * (DOES == Does::kDw ? p.ldq : 1);
+            const int left = min(static_cast<int>(tile.length - s * kSteps), kSteps);
+            in_p.load(tile.p + step_p, p.ldp, side_p, left);
+            in_q.load(tile.q + step_q, p.ldq, side_q, left);
+        };
+        const auto store = [&](unsigned s) {
+            in_p.store(base + (s & 1) * S::kStage, lane);
+            in_q.store(base + (s & 1) * S::kStage + S::PT * kStageBytes, lane);
+        };
+        x.clear();
+        if (tile.stages != 0) {
+            load(0);
+            store(0);
+            __syncthreads();
+        }
+        for (unsigned s = 0; s < tile.stages; ++s) {
+            if (s + 1 < tile.stages) load(s + 1);
+            x.template read<0>((s & 1) * S::kStage);
+            x.template read<1>((s & 1) * S::kStage);
+            x.template product<0>();
+            x.template product<1>();
+            if (s + 1 < tile.stages) store(s + 1);
+            __syncthreads();
+        }
+        store_tile<T, S>(tile.out, p.ldo, tile.end, p.cols, tile.row0 + wq * S::QB * 16 + r, tile.col0 + wp * S::PB * 16 + quarter * 4,
+                         tile.col0 + (wp + 1) * S::PB * 16 <= p.cols, x.acc);
     }
 }
 
@@ -372,6 +736,70 @@ zvc_status route_backward_as(const RouteBackArgs& p, hipStream_t stream) {
     return with_chunks<T>(p.experts, [&](auto chunks) {
         return launch(route_backward_kernel<T, decltype(chunks)::value>, dim3(div_up(p.m, 256 / kRowLanes)), 256, stream, p);
     });
+}
+
+using Large = Shape<4, 2, 4, 8, 2>;             // 256 x 256, eight waves
+using Eights = Shape<2, 4, 4, 2, 2>;            // 128 x 128, eight waves
+using Small = Shape<2, 2, 4, 4, 2>;             // 128 x 128, four waves
+using Thin = Shape<4, 1, 4, 2, 2>;              // 256 x 32, four waves
+
+// Upper bound of the tiles by rows: every expert's last one may be short.
+template <class S>
+size_t row_tiles(size_t m, size_t experts) { return m / S::QT + (experts < m ? experts : m); }
+
+unsigned grid_of(size_t items, unsigned room) { return static_cast<unsigned>(items < room ? items : room); }
+
+template <typename T, class S>
+zvc_status product_of(const ExpertArgs<T>& p, hipStream_t stream) {
+    const size_t items = row_tiles<S>(p.m, p.experts) * div_up(p.cols, S::PT);
+    return launch(product_kernel<T, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, p);
+}
+
+template <typename T, class S>
+zvc_status gradients_of(const ExpertArgs<T>& dx, const ExpertArgs<T>& dw, hipStream_t stream) {
+    const size_t dw_items = div_up(dw.cols, S::PT) * div_up(dw.rows, S::QT) * dw.experts;
+    const size_t items = row_tiles<S>(dx.m, dx.experts) * div_up(dx.cols, S::PT) + dw_items;
+    return launch(gradients_kernel<T, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, dx, dw, static_cast<unsigned>(dw_items));
+}
+
+template <typename T, Does DOES>
+zvc_status loose_of(const ExpertArgs<T>& p, hipStream_t stream) {
+    using S = Small;
+    const size_t dw_items = DOES == Does::kDw ? div_up(p.cols, S::PT) * div_up(p.rows, S::QT) * p.experts : 0;
+    const size_t items = DOES == Does::kDw ? dw_items : row_tiles<S>(p.m, p.experts) * div_up(p.cols, S::PT);
+    return launch(loose_kernel<T, DOES, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, p, static_cast<unsigned>(dw_items));
+}
+
+// Whether an operand's rows take 16-byte accesses.
+template <typename T>
+bool takes_16(const T* at, size_t ld, size_t stride) { return aligned_to(at, 16) && ld * sizeof(T) % 16 == 0 && stride * sizeof(T) % 16 == 0; }
+
+template <typename T>
+zvc_status forward_as(const ExpertArgs<T>& p, hipStream_t stream) {
+    if (!takes_16(p.p, p.ldp, p.sp) || !takes_16(p.q, p.ldq, 0) || p.length * sizeof(T) % 16 != 0) return loose_of<T, Does::kForward>(p, stream);
+    const size_t average = p.m / p.experts;
+    if (average <= 48) return product_of<T, Thin>(p, stream);
+    if constexpr (sizeof(T) == 2)
+        if (average >= 256) return product_of<T, Large>(p, stream);
+    return product_of<T, Eights>(p, stream);
+}
+
+template <typename T>
+zvc_status backward_as(ExpertArgs<T> dx, ExpertArgs<T> dw, hipStream_t stream) {
+    if (dx.cols != 0 && (!takes_16(dx.p, dx.ldp, dx.sp) || !takes_16(dx.q, dx.ldq, 0) || dx.length * sizeof(T) % 16 != 0)) {
+        if (zvc_status st = loose_of<T, Does::kDx>(dx, stream)) return st;
+        dx.cols = 0;
+    }
+    if (dw.cols != 0 && (!takes_16(dw.p, dw.ldp, 0) || !takes_16(dw.q, dw.ldq, 0))) {
+        if (zvc_status st = loose_of<T, Does::kDw>(dw, stream)) return st;
+        dw.cols = 0;
+    }
+    if (dx.cols == 0 && dw.cols == 0) return ZVC_OK;
+    const size_t average = dx.m / dx.experts;
+    if (average <= 48) return gradients_of<T, Thin>(dx, dw, stream);
+    if constexpr (sizeof(T) == 2)
+        if (average >= 256) return gradients_of<T, Large>(dx, dw, stream);
+    return gradients_of<T, Small>(dx, dw, stream);
 }
 
 bool expert_sizes_ok(size_t m, size_t experts, size_t n, size_t k) {
@@ -475,10 +903,11 @@ zvc_status zvc_expert_product(const void* d_x, size_t ldx, const void* d_w, size
     const auto as = [&](auto zero) {
         using T = decltype(zero);
         ExpertArgs<T> p{};
-        p.x = static_cast<const T*>(d_x), p.w = static_cast<const T*>(d_w), p.y = static_cast<T*>(d_y);
-        p.ldx = ldx, p.ldw = ldw, p.sw = sw, p.ldy = ldy, p.offsets = d_offsets;
-        p.m = static_cast<unsigned>(m), p.experts = static_cast<unsigned>(experts), p.n = static_cast<unsigned>(n), p.k = static_cast<unsigned>(k);
-        return launch(plain_kernel<T, Does::kForward>, dim3(div_up(n, 64), m < 256 ? div_up(m, 4) : 64, experts), 256, stream, p);
+        p.p = static_cast<const T*>(d_w), p.ldp = static_cast<unsigned>(ldw), p.sp = sw;
+        p.q = static_cast<const T*>(d_x), p.ldq = static_cast<unsigned>(ldx);
+        p.out = static_cast<T*>(d_y), p.ldo = static_cast<unsigned>(ldy), p.offsets = d_offsets;
+        p.m = static_cast<unsigned>(m), p.experts = static_cast<unsigned>(experts), p.cols = static_cast<unsigned>(n), p.length = static_cast<unsigned>(k);
+        return forward_as(p, stream);
     };
     return type == ZVC_FP32 ? as(0.f) : type == ZVC_FP16 ? as(fp16{}) : as(bf16{});
 }
@@ -513,14 +942,17 @@ zvc_status zvc_expert_gradients(const void* d_dy, size_t lddy, const void* d_x, 
     const auto as = [&](auto zero) {
         using T = decltype(zero);
         ExpertArgs<T> p{};
-        p.x = static_cast<const T*>(d_x), p.w = static_cast<const T*>(d_w), p.dy = static_cast<const T*>(d_dy);
-        p.dx = static_cast<T*>(d_dx), p.dw = static_cast<T*>(d_dw);
-        p.ldx = ldx, p.ldw = ldw, p.sw = sw, p.ldy = lddy, p.lddx = lddx, p.lddw = lddw, p.sdw = sdw, p.offsets = d_offsets;
-        p.m = static_cast<unsigned>(m), p.experts = static_cast<unsigned>(experts), p.n = static_cast<unsigned>(n), p.k = static_cast<unsigned>(k);
-        if (want_dx)
-            if (zvc_status st = launch(plain_kernel<T, Does::kDx>, dim3(div_up(k, 64), m < 256 ? div_up(m, 4) : 64, experts), 256, stream, p)) return st;
-        if (want_dw) return launch(plain_kernel<T, Does::kDw>, dim3(div_up(k, 64), n < 256 ? div_up(n, 4) : 64, experts), 256, stream, p);
-        return ZVC_OK;
+        p.offsets = d_offsets, p.m = static_cast<unsigned>(m), p.experts = static_cast<unsigned>(experts);
+        ExpertArgs<T> dx = p, dw = p;
+        dx.p = static_cast<const T*>(d_w), dx.ldp = static_cast<unsigned>(ldw), dx.sp = sw;
+        dx.q = static_cast<const T*>(d_dy), dx.ldq = static_cast<unsigned>(lddy);
+        dx.out = static_cast<T*>(d_dx), dx.ldo = static_cast<unsigned>(lddx);
+        dx.cols = want_dx ? static_cast<unsigned>(k) : 0, dx.length = static_cast<unsigned>(n);
+        dw.p = static_cast<const T*>(d_x), dw.ldp = static_cast<unsigned>(ldx);
+        dw.q = static_cast<const T*>(d_dy), dw.ldq = static_cast<unsigned>(lddy);
+        dw.out = static_cast<T*>(d_dw), dw.ldo = static_cast<unsigned>(lddw), dw.so = sdw;
+        dw.cols = want_dw ? static_cast<unsigned>(k) : 0, dw.rows = static_cast<unsigned>(n);
+        return backward_as(dx, dw, stream);
     };
     return type == ZVC_FP32 ? as(0.f) : type == ZVC_FP16 ? as(fp16{}) : as(bf16{});
 }
