@@ -398,6 +398,19 @@ __device__ __forceinline__ Groups groups_of(const int64_t* offsets, unsigned exp
     return g;
 }
 
+// dW's tiles: workgroups go to the eight XCDs in turn, and each XCD takes a part of every expert's, since experts differ in what a tile costs.
+// Parts are rounded up; what they have too much is no tile.
+struct Parts {
+    unsigned at, items, each, tiles;
+    __device__ __forceinline__ unsigned operator()() {
+        while (at < items && at % 8 * each + at / 8 % each >= tiles) at += gridDim.x;
+        const unsigned item = at;
+        at += gridDim.x;
+        return item < items ? item : kNone;
+    }
+};
+__host__ __device__ inline unsigned parts_of(unsigned tiles) { return (tiles + 7) / 8; }
+
 // One workgroup's view of a tile.
 template <typename T, Does DOES, class S>
 struct Tile {
@@ -421,12 +434,12 @@ struct Tile {
         row0 = (band * kBand + in_band % height) * S::QT;
     }
     __device__ __forceinline__ void init(const ExpertArgs<T>& a, const Groups& g, unsigned items, unsigned item, int wave, int lane) {
-        const unsigned at = place_of(item, items), tp = (a.cols + S::PT - 1) / S::PT;
+        const unsigned tp = (a.cols + S::PT - 1) / S::PT;
         unsigned e;
         if constexpr (DOES == Does::kDw) {
-            const unsigned tq = (a.rows + S::QT - 1) / S::QT;
-            e = at / (tp * tq);
-            locate(at - e * (tp * tq), tp, tq);
+            const unsigned tq = (a.rows + S::QT - 1) / S::QT, each = parts_of(tp * tq);
+            e = item / 8 / each;
+            locate(item % 8 * each + (item / 8 - e * each), tp, tq);
             const unsigned begin = __builtin_amdgcn_readfirstlane(g.start(e));
             end = a.rows;
             length = __builtin_amdgcn_readfirstlane(g.start(e + 1)) - begin;
@@ -434,6 +447,7 @@ struct Tile {
             q = cell(a.q, begin, a.ldq, row0);
             out = a.out + e * a.so;
         } else {
+            const unsigned at = place_of(item, items);
             e = g.expert_of(at, lane);
             const unsigned begin = __builtin_amdgcn_readfirstlane(g.start(e));
             end = __builtin_amdgcn_readfirstlane(g.start(e + 1));
@@ -458,33 +472,81 @@ struct Tile {
     }
 };
 
-// A tile's sums as they go out: a lane has four neighbouring columns of each of its blocks.
+// Two numbers of 16 bits in a word.
+template <typename T>
+__device__ __forceinline__ unsigned pack(float a, float b) {
+    struct Two { T a, b; };
+    return __builtin_bit_cast(unsigned, Two{static_cast<T>(a), static_cast<T>(b)});
+}
+
+// A lane's sums of 16 rows of a strip, as they go out: `pieces` of 16 bytes at (row, column of the strip).
+//
+// The matrix instructions leave a lane four neighbouring columns of each of its blocks in row r, r the lane's number within 16.  fp32: these
+// are 16 bytes.  16-bit types: neighbouring quarters of the wave exchange halves of a pair of blocks, after which a lane has eight
+// neighbouring columns, of two pairs; then neighbouring lanes exchange pairs, after which the even one has a piece of 128 neighbouring bytes of row r for
+// itself and r + 1, and the odd one of r - 1 and r.  So an instruction writes whole lines of 128 bytes.
 template <typename T, class S>
-__device__ __forceinline__ void store_tile(T* out, unsigned ldo, unsigned rows, unsigned cols, unsigned row_first, unsigned col_first, bool full, const float4v (&acc)[S::PB][S::QB]) {
-    struct Four { T v[4]; };
-    const auto four = [&](int i, int j) {
-        Four f;
+struct Strip {
+    static constexpr bool kNarrow = sizeof(T) == 2;
+    static constexpr int kPieces = kNarrow ? S::PB / 2 : S::PB;
+    static_assert(!kNarrow || S::PB == 4, "lines of 128 bytes");
+    using Words2 = unsigned __attribute__((ext_vector_type(2)));
+    int4v v[kPieces];
+
+    static __device__ __forceinline__ int row(int piece, int lane) { return kNarrow ? (lane & 14) + piece : lane & 15; }
+    static __device__ __forceinline__ int col(int piece, int lane) {
+        const int quarter = lane >> 4;
+        return kNarrow ? (lane & 1) * 32 + (quarter & 1) * 16 + (quarter >> 1) * 8 : piece * 16 + quarter * 4;
+    }
+    __device__ __forceinline__ void take(const float4v (&acc)[S::PB][S::QB], int j, int lane) {
+        if constexpr (kNarrow) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f.v[e] = static_cast<T>(acc[i][j][e]);
-        return f;
-    };
+            for (int i = 0; i < 2; ++i) {
+                const float4v a = acc[2 * i][j], b = acc[2 * i + 1][j];
+                const Words2 low = __builtin_amdgcn_permlane16_swap(pack<T>(a[0], a[1]), pack<T>(b[0], b[1]), false, false);
+                const Words2 high = __builtin_amdgcn_permlane16_swap(pack<T>(a[2], a[3]), pack<T>(b[2], b[3]), false, false);
+                v[i] = int4v{static_cast<int>(low[0]), static_cast<int>(high[0]), static_cast<int>(low[1]), static_cast<int>(high[1])};
+            }
+            const bool odd = lane & 1;
 #pragma unroll
-    for (int j = 0; j < S::QB; ++j) {
-        T* const at = cell(out, row_first + j * 16, ldo, col_first);
-        if (row_first + j * 16 >= rows) continue;
-        if (full) {
-#pragma unroll
-            for (int i = 0; i < S::PB; ++i) {
-                const Four f = four(i, j);
-                __builtin_memcpy(at + i * 16, &f, sizeof f);
+            for (int w = 0; w < 4; ++w) {
+                const int own = odd ? v[1][w] : v[0][w], given = odd ? v[0][w] : v[1][w];
+                const int got = __builtin_amdgcn_update_dpp(0, given, 0xB1, 0xF, 0xF, false);        // the neighbour's
+                v[0][w] = odd ? got : own;
+                v[1][w] = odd ? own : got;
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < S::PB; ++i) {
-                const Four f = four(i, j);
+            for (int i = 0; i < S::PB; ++i) v[i] = __builtin_bit_cast(int4v, acc[i][j]);
+        }
+    }
+};
+
+// A wave's strip of a tile goes out.
+template <typename T, class S>
+__device__ __forceinline__ void store_strip(T* out, unsigned ldo, unsigned rows, unsigned cols, unsigned row0, unsigned col0, int lane, const float4v (&acc)[S::PB][S::QB]) {
+    using Out = Strip<T, S>;
+    constexpr int kPer = 16 / sizeof(T);
+    const bool whole = row0 + S::QB * 16 <= rows && col0 + S::PB * 16 <= cols;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (col_first + i * 16 + e < cols) at[i * 16 + e] = f.v[e];
+    for (int j = 0; j < S::QB; ++j) {
+        Out strip;
+        strip.take(acc, j, lane);
+#pragma unroll
+        for (int i = 0; i < Out::kPieces; ++i) {
+            const unsigned row = row0 + j * 16 + Out::row(i, lane), col = col0 + Out::col(i, lane);
+            T* const at = cell(out, row, ldo, col);
+            if (whole) {
+                __builtin_memcpy(at, &strip.v[i], 16);
+            } else if (row < rows) {
+                const Pack<T> f = __builtin_bit_cast(Pack<T>, strip.v[i]);
+                if (col + kPer <= cols) {
+                    __builtin_memcpy(at, &f, 16);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e)
+                        if (col + e < cols) at[e] = f.v[e];
+                }
             }
         }
     }
@@ -535,7 +597,7 @@ __device__ __forceinline__ void work(const ExpertArgs<T>& p, const Groups& group
     using Where = Tile<T, DOES, S>;
     constexpr int kRing = S::kRing;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wp = wave % S::WP, wq = wave / S::WP, r = lane & 15, quarter = lane >> 4;
+    const int wp = wave % S::WP, wq = wave / S::WP;
     Multiplier<T, DOES, S> x;
     x.init(base, wp, wq, lane);
     Where tile;
@@ -580,7 +642,7 @@ __device__ __forceinline__ void work(const ExpertArgs<T>& p, const Groups& group
         item = next();
         group_barrier();                         // (the reads for nothing are done)
         if (item != kNone) begin(item);
-        store_tile<T, S>(out, p.ldo, end, p.cols, row0 + wq * S::QB * 16 + r, col0 + wp * S::PB * 16 + quarter * 4, col0 + (wp + 1) * S::PB * 16 <= p.cols, x.acc);
+        store_strip<T, S>(out, p.ldo, end, p.cols, row0 + wq * S::QB * 16, col0 + wp * S::PB * 16, lane, x.acc);
     }
 }
 
@@ -605,16 +667,16 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(Exper
     work<T, Does::kForward, S>(p, g, g.items, address(lds), threadIdx.x & 63, Turns{blockIdx.x, g.items});
 }
 
-// dx, and behind it dW, in one go: either alone leaves compute units idle in its last round.  `dw_items`, and dx.cols, may be 0.
+// dx, and behind it dW, in one go: either alone leaves compute units idle in its last round.  dw_tiles: of one expert; it, and dx.cols, may be 0.
 template <typename T, class S>
-__global__ __launch_bounds__(S::kThreads, S::kPerUnit) void gradients_kernel(ExpertArgs<T> dx, ExpertArgs<T> dw, unsigned dw_items) {
+__global__ __launch_bounds__(S::kThreads, S::kPerUnit) void gradients_kernel(ExpertArgs<T> dx, ExpertArgs<T> dw, unsigned dw_tiles) {
     unsigned char* const lds = room_of<S>();
     const Groups g = tables<S>(dx.offsets, dx.experts, dx.m, dx.cols, lds);
     // (a lane's number that is had again at any time: no register holds the thread's through both)
     const int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
     const unsigned first = g.items % gridDim.x, mine = blockIdx.x >= first ? blockIdx.x - first : blockIdx.x + gridDim.x - first;
     work<T, Does::kDx, S>(dx, g, g.items, address(lds), lane, Turns{blockIdx.x, g.items});
-    work<T, Does::kDw, S>(dw, g, dw_items, address(lds), lane, Turns{mine, dw_items});
+    work<T, Does::kDw, S>(dw, g, dw_tiles, address(lds), lane, Parts{mine, 8 * parts_of(dw_tiles) * dw.experts, parts_of(dw_tiles), dw_tiles});
 }
 
 // ------------------------------------------------------------------ operands that do not take 16-byte accesses
@@ -651,15 +713,15 @@ struct LooseOperand {
 };
 
 template <typename T, Does DOES, class S>
-__global__ __launch_bounds__(S::kThreads, S::kPerUnit) void loose_kernel(ExpertArgs<T> p, unsigned dw_items) {
+__global__ __launch_bounds__(S::kThreads, S::kPerUnit) void loose_kernel(ExpertArgs<T> p, unsigned dw_tiles) {
     static_assert(S::kRing == 2, "one stage is read while the next is written");
     unsigned char* const lds = room_of<S>();
     const Groups g = tables<S>(p.offsets, p.experts, p.m, p.cols, lds);
     using Where = Tile<T, DOES, S>;
     constexpr int kSteps = Where::kSteps;
-    const unsigned base = address(lds), items = DOES == Does::kDw ? dw_items : g.items;
+    const unsigned base = address(lds);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wp = wave % S::WP, wq = wave / S::WP, r = lane & 15, quarter = lane >> 4;
+    const int wp = wave % S::WP, wq = wave / S::WP;
     Multiplier<T, DOES, S> x;
     x.init(base, wp, wq, lane);
     Where tile;
@@ -667,8 +729,12 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void loose_kernel(ExpertA
     LooseOperand<T, Where::kQ, S::QT, S::kWavesAll> in_q;
     in_p.op.init(wave, lane, 0, 0);
     in_q.op.init(wave, lane, 0, 0);
-    for (unsigned item = blockIdx.x; item < items; item += gridDim.x) {
-        tile.init(p, g, items, item, wave, lane);
+    const unsigned each = parts_of(dw_tiles);
+    Turns turns{blockIdx.x, g.items};
+    Parts parts{blockIdx.x, 8 * each * p.experts, each, dw_tiles};
+    const auto next = [&]() { return DOES == Does::kDw ? parts() : turns(); };
+    for (unsigned item = next(); item != kNone; item = next()) {
+        tile.init(p, g, g.items, item, wave, lane);
         const int side_p = min(static_cast<int>(p.cols - tile.col0), S::PT), side_q = min(static_cast<int>(tile.end - tile.row0), S::QT);
         const auto load = [&](unsigned s) {
             const size_t step_p = size_t{s} * kSteps * (DOES == Does::kForward ? 1 : p.ldp), step_q = size_t{s} * kSteps * (DOES == Does::kDw ? p.ldq : 1);
@@ -695,8 +761,7 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void loose_kernel(ExpertA
             if (s + 1 < tile.stages) store(s + 1);
             __syncthreads();
         }
-        store_tile<T, S>(tile.out, p.ldo, tile.end, p.cols, tile.row0 + wq * S::QB * 16 + r, tile.col0 + wp * S::PB * 16 + quarter * 4,
-                         tile.col0 + (wp + 1) * S::PB * 16 <= p.cols, x.acc);
+        store_strip<T, S>(tile.out, p.ldo, tile.end, p.cols, tile.row0 + wq * S::QB * 16, tile.col0 + wp * S::PB * 16, lane, x.acc);
     }
 }
 
@@ -757,17 +822,17 @@ zvc_status product_of(const ExpertArgs<T>& p, hipStream_t stream) {
 
 template <typename T, class S>
 zvc_status gradients_of(const ExpertArgs<T>& dx, const ExpertArgs<T>& dw, hipStream_t stream) {
-    const size_t dw_items = div_up(dw.cols, S::PT) * div_up(dw.rows, S::QT) * dw.experts;
-    const size_t items = row_tiles<S>(dx.m, dx.experts) * div_up(dx.cols, S::PT) + dw_items;
-    return launch(gradients_kernel<T, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, dx, dw, static_cast<unsigned>(dw_items));
+    const size_t dw_tiles = div_up(dw.cols, S::PT) * div_up(dw.rows, S::QT);
+    const size_t items = row_tiles<S>(dx.m, dx.experts) * div_up(dx.cols, S::PT) + dw_tiles * dw.experts;
+    return launch(gradients_kernel<T, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, dx, dw, static_cast<unsigned>(dw_tiles));
 }
 
 template <typename T, Does DOES>
 zvc_status loose_of(const ExpertArgs<T>& p, hipStream_t stream) {
     using S = Small;
-    const size_t dw_items = DOES == Does::kDw ? div_up(p.cols, S::PT) * div_up(p.rows, S::QT) * p.experts : 0;
-    const size_t items = DOES == Does::kDw ? dw_items : row_tiles<S>(p.m, p.experts) * div_up(p.cols, S::PT);
-    return launch(loose_kernel<T, DOES, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, p, static_cast<unsigned>(dw_items));
+    const size_t dw_tiles = DOES == Does::kDw ? div_up(p.cols, S::PT) * div_up(p.rows, S::QT) : 0;
+    const size_t items = DOES == Does::kDw ? dw_tiles * p.experts : row_tiles<S>(p.m, p.experts) * div_up(p.cols, S::PT);
+    return launch(loose_kernel<T, DOES, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, p, static_cast<unsigned>(dw_tiles));
 }
 
 // Whether an operand's rows take 16-byte accesses.
