@@ -552,6 +552,23 @@ __device__ __forceinline__ void store_strip(T* out, unsigned ldo, unsigned rows,
     }
 }
 
+// Four neighbouring sums, `left` of which are columns; `any`: one at least.
+template <typename T>
+__device__ __forceinline__ void store_four(T* at, float4v sum, unsigned left, bool any) {
+    struct Four { T v[4]; };
+    Four f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f.v[e] = static_cast<T>(sum[e]);
+    if (!any) return;
+    if (left >= 4) {
+        __builtin_memcpy(at, &f, sizeof f);
+    } else {
+#pragma unroll
+        for (unsigned e = 0; e < 4; ++e)
+            if (e < left) at[e] = f.v[e];
+    }
+}
+
 // The sums of a stage that lies in LDS.
 template <typename T, Does DOES, class S>
 struct Multiplier {
@@ -680,35 +697,47 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void gradients_kernel(Exp
 }
 
 // ------------------------------------------------------------------ operands that do not take 16-byte accesses
-// The same places in LDS by way of registers: 16 bytes at any element, and single elements at an operand's ends, beyond which are zeros.
+// x moved towards its low end by `bytes`, 0 to 16, zeros behind it.
+__device__ __forceinline__ int4v moved_down(int4v x, int bytes) {
+    const auto whole = __builtin_bit_cast(unsigned __int128, x);
+    return __builtin_bit_cast(int4v, bytes < 16 ? whole >> (8 * bytes) : static_cast<unsigned __int128>(0));
+}
+
+// The same places in LDS by way of registers: 16 bytes at any element, zeros beyond an operand's ends.  Where a row ends within the 16 bytes, the row's
+// last 16 are read and moved into place; rows of fewer are read element by element.
 template <typename T, Lies LIES, int SIDE, int WAVES>
 struct LooseOperand {
     using Op = Operand<T, LIES, SIDE, WAVES, false>;
     static constexpr int kPer = 16 / sizeof(T);
     Op op;
-    Pack<T> v[Op::kLoads];
+    int4v v[Op::kLoads];
 
-    // `left`: of the reduction; `side`: rows (kAlong) or columns (kAcross) that exist.
-    __device__ __forceinline__ void load(const T* base, size_t ld, int side, int left) {
+    // `left`: of the reduction; `side`: rows (kAlong) or columns (kAcross) that exist; `shorter`: rows have less than 16 bytes in all.
+    __device__ __forceinline__ void load(const T* base, size_t ld, int side, int left, bool shorter) {
 #pragma unroll
         for (int i = 0; i < Op::kLoads; ++i) {
             const int row = (op.first + i) * Op::kRowsPerLoad + op.lane_row, col = op.logical(row) / static_cast<int>(sizeof(T));
             const int rows = LIES == Lies::kAlong ? side : left, there = (LIES == Lies::kAlong ? left : side) - col;
+            v[i] = int4v{0, 0, 0, 0};
+            if (row >= rows || there <= 0) continue;
             const T* const at = base + row * ld + col;
-            v[i] = Pack<T>{};
-            if (row < rows && there >= kPer) {
-                __builtin_memcpy(&v[i], at, 16);
-            } else if (row < rows) {
+            if (!shorter) {
+                const int missing = there < kPer ? kPer - there : 0;
+                __builtin_memcpy(&v[i], at - missing, 16);
+                if (missing != 0) v[i] = moved_down(v[i], missing * static_cast<int>(sizeof(T)));
+            } else {
+                Pack<T> one = {};
 #pragma unroll
                 for (int j = 0; j < kPer; ++j)
-                    if (j < there) v[i].v[j] = at[j];
+                    if (j < there) one.v[j] = at[j];
+                v[i] = __builtin_bit_cast(int4v, one);
             }
         }
     }
     __device__ __forceinline__ void store(unsigned lds, int lane) const {
 #pragma unroll
         for (int i = 0; i < Op::kLoads; ++i)
-            *reinterpret_cast<__attribute__((address_space(3))) int4v*>(lds_at(lds + (op.first + i) * 1024 + lane * 16)) = __builtin_bit_cast(int4v, v[i]);
+            *reinterpret_cast<__attribute__((address_space(3))) int4v*>(lds_at(lds + (op.first + i) * 1024 + lane * 16)) = v[i];
     }
 };
 
@@ -736,11 +765,13 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void loose_kernel(ExpertA
     for (unsigned item = next(); item != kNone; item = next()) {
         tile.init(p, g, g.items, item, wave, lane);
         const int side_p = min(static_cast<int>(p.cols - tile.col0), S::PT), side_q = min(static_cast<int>(tile.end - tile.row0), S::QT);
+        const bool short_p = (DOES == Does::kForward ? p.length : p.cols) * sizeof(T) < 16;
+        const bool short_q = (DOES == Does::kDw ? p.rows : p.length) * sizeof(T) < 16;
         const auto load = [&](unsigned s) {
             const size_t step_p = size_t{s} * kSteps * (DOES == Does::kForward ? 1 : p.ldp), step_q = size_t{s} * kSteps * (DOES == Does::kDw ? p.ldq : 1);
-            const int left = min(static_cast<int>(tile.length - s * kSteps), kSteps);
-            in_p.load(tile.p + step_p, p.ldp, side_p, left);
-            in_q.load(tile.q + step_q, p.ldq, side_q, left);
+            const int left = static_cast<int>(tile.length - s * kSteps);
+            in_p.load(tile.p + step_p, p.ldp, side_p, left, short_p);
+            in_q.load(tile.q + step_q, p.ldq, side_q, left, short_q);
         };
         const auto store = [&](unsigned s) {
             in_p.store(base + (s & 1) * S::kStage, lane);
@@ -763,6 +794,230 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void loose_kernel(ExpertA
         }
         store_strip<T, S>(tile.out, p.ldo, tile.end, p.cols, tile.row0 + wq * S::QB * 16, tile.col0 + wp * S::PB * 16, lane, x.acc);
     }
+}
+
+// ------------------------------------------------------------------ small products
+// What a small kernel's workgroup works on.
+struct Place {
+    unsigned expert, begin, end, at;         // its rows; the tile's number among the expert's
+};
+
+// The expert and its tile that number `item` is, `across` tiles for every `tile_rows` rows of an expert; false behind the last.  Each wave looks for itself:
+// a lane has some neighbouring experts.
+__device__ __forceinline__ bool find_tile(const int64_t* offsets, unsigned experts, unsigned m, unsigned across, unsigned tile_rows, unsigned item, int lane, Place* out) {
+    const unsigned each = (experts + 63) / 64, first = lane * each;
+    const auto offset = [&](unsigned e) { return static_cast<unsigned>(min(max(offsets[min(e, experts)], int64_t{0}), static_cast<int64_t>(m))); };
+    unsigned most = 0;
+    for (unsigned j = 0; j < each; ++j) most = max(most, offset(first + j));
+    unsigned through = most;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const unsigned before = __shfl_up(through, d);
+        through = lane >= d ? max(through, before) : through;
+    }
+    const unsigned carried = __shfl_up(through, 1);
+    const unsigned entry = lane != 0 ? carried : 0;
+    const auto tiles = [&](unsigned begin, unsigned end) { return (end - begin + tile_rows - 1) / tile_rows * across; };
+    unsigned sum = 0, begin = max(entry, offset(first));
+    for (unsigned j = 0; j < each && first + j < experts; ++j) {
+        const unsigned end = max(begin, offset(first + j + 1));
+        sum += tiles(begin, end);
+        begin = end;
+    }
+    unsigned total = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const unsigned before = __shfl_up(total, d);
+        total += lane >= d ? before : 0;
+    }
+    const uint64_t behind = __ballot(total > item);
+    if (behind == 0) return false;
+    const int owner = __ffsll(static_cast<unsigned long long>(behind)) - 1;
+    Place p{0, 0, 0, item - (total - sum)};
+    if (lane == owner) {
+        begin = max(entry, offset(first));
+        for (unsigned j = 0; j < each && first + j < experts; ++j) {
+            const unsigned end = max(begin, offset(first + j + 1)), own = tiles(begin, end);
+            if (p.at < own) {
+                p.expert = first + j, p.begin = begin, p.end = end;
+                break;
+            }
+            p.at -= own;
+            begin = end;
+        }
+    }
+    *out = {static_cast<unsigned>(__builtin_amdgcn_readlane(p.expert, owner)), static_cast<unsigned>(__builtin_amdgcn_readlane(p.begin, owner)),
+            static_cast<unsigned>(__builtin_amdgcn_readlane(p.end, owner)), static_cast<unsigned>(__builtin_amdgcn_readlane(p.at, owner))};
+    return true;
+}
+
+// An expert's rows.
+__device__ __forceinline__ void find_rows(const int64_t* offsets, unsigned expert, unsigned m, int lane, unsigned* begin, unsigned* end) {
+    int64_t most = 0;
+    for (unsigned e = lane; e <= expert; e += 64) most = max(most, offsets[e]);
+    unsigned start = static_cast<unsigned>(min(most, static_cast<int64_t>(m)));
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) start = max(start, static_cast<unsigned>(__shfl_xor(start, d)));
+    const int64_t next = offsets[expert + 1];
+    *begin = __builtin_amdgcn_readfirstlane(start);
+    *end = __builtin_amdgcn_readfirstlane(max(start, static_cast<unsigned>(min(max(next, int64_t{0}), static_cast<int64_t>(m)))));
+}
+
+constexpr int kSoloWaves = 4, kSoloCols = 64;
+
+struct SoloSplit {
+    float* sums;                         // part by part, tile by tile
+    unsigned tiles, parts, dw_tiles;     // at most, of all experts; of a tile's sum; dW: of one expert
+};
+
+// Tiles of 64 columns and 16 QB rows.  SPLIT: the workgroup's waves take turns along the reduction, each with a ring of its own in LDS, and meet there at the end;
+// no wave waits for another.  Else each wave has a tile of its own, four side by side.  LOOSE: operands come by way of registers.
+template <typename T, Does DOES, int QB, bool SPLIT, bool LOOSE>
+__global__ __launch_bounds__(64 * kSoloWaves) void solo_kernel(ExpertArgs<T> p, SoloSplit split) {
+    using S = Shape<1, 1, 4, QB, 2>;
+    constexpr Lies kP = DOES == Does::kForward ? Lies::kAlong : Lies::kAcross, kQ = DOES == Does::kDw ? Lies::kAcross : Lies::kAlong;
+    constexpr int W = sizeof(T), kSteps = kStageBytes / W, kRing = LOOSE ? 1 : 2, kRow = kSoloCols + 4;
+    constexpr int kSums = SPLIT ? kSoloWaves * S::QT * kRow * 4 : 0, kStages = kSoloWaves * kRing * S::kStage;
+    __shared__ alignas(1024) unsigned char lds[kSums > kStages ? kSums : kStages];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr unsigned kWide = SPLIT ? kSoloCols : kSoloCols * kSoloWaves;       // columns of a workgroup
+    const unsigned tp = (p.cols + kWide - 1) / kWide, id = place_of(blockIdx.x, gridDim.x), item = id / split.parts, part = id - item * split.parts;
+    Place place;
+    unsigned length, rows_end, row0, col0;
+    const T *from_p, *from_q;
+    T* out = p.out;
+    if constexpr (DOES == Does::kDw) {
+        place.expert = item / split.dw_tiles, place.at = item - place.expert * split.dw_tiles;
+        find_rows(p.offsets, place.expert, p.m, lane, &place.begin, &place.end);
+        const unsigned tq = (p.rows + S::QT - 1) / S::QT;
+        col0 = place.at / tq * kWide, row0 = place.at % tq * S::QT;
+        length = place.end - place.begin, rows_end = p.rows;
+        out += place.expert * p.so;
+    } else {
+        if (!find_tile(p.offsets, p.experts, p.m, tp, S::QT, item, lane, &place)) return;
+        const unsigned tq = (place.end - place.begin + S::QT - 1) / S::QT;
+        col0 = place.at / tq * kWide, row0 = place.begin + place.at % tq * S::QT;
+        length = p.length, rows_end = place.end;
+    }
+    if constexpr (!SPLIT) col0 += wave * kSoloCols;
+    if (!SPLIT && col0 >= p.cols) return;
+    if constexpr (DOES == Does::kDw) {
+        from_p = cell(p.p, place.begin, p.ldp, col0), from_q = cell(p.q, place.begin, p.ldq, row0);
+    } else {
+        from_p = p.p + place.expert * p.sp;
+        from_p = DOES == Does::kForward ? cell(from_p, col0, p.ldp, 0) : from_p + col0;
+        from_q = cell(p.q, row0, p.ldq, 0);
+    }
+    const unsigned stages = (length + kSteps - 1) / kSteps, begin = static_cast<unsigned>(uint64_t{stages} * part / split.parts),
+                   end = static_cast<unsigned>(uint64_t{stages} * (part + 1) / split.parts);
+    const unsigned first = begin + (SPLIT ? wave : 0), step = SPLIT ? kSoloWaves : 1, mine = first < end ? (end - first + step - 1) / step : 0;
+    const size_t step_p = size_t{kSteps} * (DOES == Does::kForward ? 1 : p.ldp), step_q = size_t{kSteps} * (DOES == Does::kDw ? p.ldq : 1);
+    const unsigned base = address(lds) + wave * (kRing * S::kStage);
+    const int side_p = min(static_cast<int>(p.cols - col0), kSoloCols), side_q = min(static_cast<int>(rows_end - row0), S::QT);
+    Multiplier<T, DOES, S> x;
+    x.init(base, 0, 0, lane);
+    x.clear();
+    const auto multiply_stage = [&](unsigned stage) {
+        x.template read<0>(stage);
+        x.template read<1>(stage);
+    };
+    if constexpr (LOOSE) {
+        LooseOperand<T, kP, S::PT, 1> in_p;
+        LooseOperand<T, kQ, S::QT, 1> in_q;
+        in_p.op.init(0, lane, 0, 0);
+        in_q.op.init(0, lane, 0, 0);
+        const bool short_p = (DOES == Does::kForward ? p.length : p.cols) * W < 16, short_q = (DOES == Does::kDw ? p.rows : p.length) * W < 16;
+        const auto load = [&](unsigned i) {
+            const unsigned s = first + i * step;
+            const int left = static_cast<int>(length - s * kSteps);
+            in_p.load(from_p + s * step_p, p.ldp, side_p, left, short_p);
+            in_q.load(from_q + s * step_q, p.ldq, side_q, left, short_q);
+        };
+        if (mine != 0) load(0);
+        for (unsigned i = 0; i < mine; ++i) {
+            in_p.store(base, lane);
+            in_q.store(base + S::PT * kStageBytes, lane);
+            if (i + 1 < mine) load(i + 1);
+            wait_reads();                                            // (what was stored is there)
+            multiply_stage(0);
+            x.template product<0>();
+            x.template product<1>();
+        }
+    } else {
+        Operand<T, kP, S::PT, 1, false> in_p;
+        Operand<T, kQ, S::QT, 1, false> in_q;
+        in_p.init(0, lane, p.ldp, side_p);
+        in_q.init(0, lane, p.ldq, side_q);
+        constexpr int kLoads = decltype(in_p)::kLoads + decltype(in_q)::kLoads;
+        const auto fetch = [&](unsigned i) {
+            const unsigned s = first + i * step, to = base + (i % kRing) * S::kStage;
+            const int left = static_cast<int>(length - s * kSteps);
+            in_p.fetch(reinterpret_cast<uint64_t>(from_p + s * step_p), 0, left, to);
+            in_q.fetch(reinterpret_cast<uint64_t>(from_q + s * step_q), 0, left, to + S::PT * kStageBytes);
+        };
+#pragma unroll
+        for (unsigned i = 0; i < kRing; ++i)
+            if (i < mine) fetch(i);
+        for (unsigned i = 0; i < mine; ++i) {
+            if (i + kRing <= mine) wait_loads<(kRing - 1) * kLoads>();
+            else wait_loads<0>();
+            multiply_stage((i % kRing) * S::kStage);
+            wait_reads();                                            // before their place is written again
+            if (i + kRing < mine) fetch(i + kRing);
+            x.template product<0>();
+            x.template product<1>();
+        }
+    }
+    if constexpr (!SPLIT) {
+        store_strip<T, S>(out, p.ldo, rows_end, p.cols, row0, col0, lane, x.acc);
+    } else {
+        __syncthreads();
+        float* const sums = reinterpret_cast<float*>(lds);
+        const int r = lane & 15, quarter = lane >> 4;
+#pragma unroll
+        for (int j = 0; j < QB; ++j)
+#pragma unroll
+            for (int i = 0; i < S::PB; ++i)
+                *reinterpret_cast<float4v*>(sums + (wave * S::QT + j * 16 + r) * kRow + i * 16 + quarter * 4) = x.acc[i][j];
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < QB; ++j) {                               // 16 rows of 64 columns: four neighbouring ones a thread
+            const unsigned row_in = j * 16 + threadIdx.x / 16, col_in = threadIdx.x % 16 * 4, row = row0 + row_in, col = col0 + col_in;
+            float4v sum = *reinterpret_cast<const float4v*>(sums + row_in * kRow + col_in);
+#pragma unroll
+            for (int w = 1; w < kSoloWaves; ++w) sum += *reinterpret_cast<const float4v*>(sums + (w * S::QT + row_in) * kRow + col_in);
+            if (split.parts > 1) {
+                *reinterpret_cast<float4v*>(split.sums + ((size_t{part} * split.tiles + item) * S::QT + row_in) * kSoloCols + col_in) = sum;
+            } else if (row < rows_end) {
+                store_four(cell(out, row, p.ldo, col), sum, p.cols - col, col < p.cols);
+            }
+        }
+    }
+}
+
+// The parts' sums of tiles of 64 columns and 16 QB rows, joined in the order of the parts: a workgroup takes 16 rows of a tile.
+template <typename T, Does DOES, int QB>
+__global__ __launch_bounds__(256) void solo_join_kernel(ExpertArgs<T> p, SoloSplit split) {
+    constexpr unsigned kRows = 16 * QB;
+    const int lane = threadIdx.x & 63;
+    const unsigned item = blockIdx.x / QB, row_in = blockIdx.x % QB * 16 + threadIdx.x / 16, col_in = threadIdx.x % 16 * 4;
+    Place place;
+    unsigned row, col, rows_end;
+    T* out = p.out;
+    if constexpr (DOES == Does::kDw) {
+        const unsigned tq = (p.rows + kRows - 1) / kRows, expert = item / split.dw_tiles, at = item - expert * split.dw_tiles;
+        out += expert * p.so;
+        row = at % tq * kRows + row_in, col = at / tq * kSoloCols + col_in, rows_end = p.rows;
+    } else {
+        if (!find_tile(p.offsets, p.experts, p.m, (p.cols + kSoloCols - 1) / kSoloCols, kRows, item, lane, &place)) return;
+        const unsigned tq = (place.end - place.begin + kRows - 1) / kRows;
+        row = place.begin + place.at % tq * kRows + row_in, col = place.at / tq * kSoloCols + col_in, rows_end = place.end;
+    }
+    if (row >= rows_end || col >= p.cols) return;
+    float4v sum{0.f, 0.f, 0.f, 0.f};
+    for (unsigned part = 0; part < split.parts; ++part)
+        sum += *reinterpret_cast<const float4v*>(split.sums + ((size_t{part} * split.tiles + item) * kRows + row_in) * kSoloCols + col_in);
+    store_four(cell(out, row, p.ldo, col), sum, p.cols - col, true);
 }
 
 // ------------------------------------------------------------------ host side
@@ -806,24 +1061,60 @@ zvc_status route_backward_as(const RouteBackArgs& p, hipStream_t stream) {
 using Large = Shape<4, 2, 4, 8, 2>;             // 256 x 256, eight waves
 using Eights = Shape<2, 4, 4, 2, 2>;            // 128 x 128, eight waves
 using Small = Shape<2, 2, 4, 4, 2>;             // 128 x 128, four waves
-using Thin = Shape<4, 1, 4, 2, 2>;              // 256 x 32, four waves
+
+// Which kernel takes a product: persistent tiles, tiles by way of registers, or the small kernels (their rows; kEach: a tile a wave).
+enum class Kind { kLarge, kSmall, kLoose, kSolo16, kSolo64, kEach };
+
+struct Choice {
+    Kind kind;
+    unsigned parts;                             // of a small kernel's sums
+    size_t sums;                                // their bytes
+};
 
 // Upper bound of the tiles by rows: every expert's last one may be short.
-template <class S>
-size_t row_tiles(size_t m, size_t experts) { return m / S::QT + (experts < m ? experts : m); }
+size_t row_tiles(size_t m, size_t experts, size_t tile) { return m / tile + (experts < m ? experts : m); }
+
+// Parts of the sums of a small kernel where its tiles do not fill the compute units.
+Choice solo_choice(Kind kind, size_t tiles, size_t rows, size_t stages) {
+    constexpr size_t kSlots = 2 * kUnits;
+    size_t parts = tiles == 0 ? 1 : kSlots / tiles;
+    if (parts > stages / (2 * kSoloWaves)) parts = stages / (2 * kSoloWaves);
+    if (parts > 16) parts = 16;
+    if (parts < 2) return {kind, 1, 0};
+    return {kind, static_cast<unsigned>(parts), parts * tiles * rows * kSoloCols * sizeof(float)};
+}
+
+// Of y or dx: `cols` columns, sums over `length`.
+Choice choose_rows(size_t m, size_t experts, size_t cols, size_t length, size_t w, bool loose) {
+    const size_t average = m / experts, stages = div_up(length, kStageBytes / w), across = div_up(cols, kSoloCols);
+    if (average <= 16) return solo_choice(Kind::kSolo16, row_tiles(m, experts, 16) * across, 16, stages);
+    const size_t tiles = row_tiles(m, experts, 64) * across;
+    if (average <= 64 || tiles <= 4 * kUnits) return solo_choice(Kind::kSolo64, tiles, 64, stages);
+    if (loose) return {Kind::kLoose, 1, 0};
+    return {w == 2 && average >= 256 ? Kind::kLarge : Kind::kSmall, 1, 0};
+}
+
+// Of dW.
+Choice choose_dw(size_t m, size_t experts, size_t n, size_t k, size_t w, bool loose) {
+    const size_t average = m / experts, stages = div_up(average, kStageBytes / w), tiles = div_up(n, 64) * div_up(k, kSoloCols) * experts;
+    if (stages <= 4) return {Kind::kEach, 1, 0};
+    if (tiles <= 4 * kUnits) return solo_choice(Kind::kSolo64, tiles, 64, stages);
+    if (loose) return {Kind::kLoose, 1, 0};
+    return {w == 2 && average >= 256 ? Kind::kLarge : Kind::kSmall, 1, 0};
+}
 
 unsigned grid_of(size_t items, unsigned room) { return static_cast<unsigned>(items < room ? items : room); }
 
 template <typename T, class S>
 zvc_status product_of(const ExpertArgs<T>& p, hipStream_t stream) {
-    const size_t items = row_tiles<S>(p.m, p.experts) * div_up(p.cols, S::PT);
+    const size_t items = row_tiles(p.m, p.experts, S::QT) * div_up(p.cols, S::PT);
     return launch(product_kernel<T, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, p);
 }
 
 template <typename T, class S>
 zvc_status gradients_of(const ExpertArgs<T>& dx, const ExpertArgs<T>& dw, hipStream_t stream) {
     const size_t dw_tiles = div_up(dw.cols, S::PT) * div_up(dw.rows, S::QT);
-    const size_t items = row_tiles<S>(dx.m, dx.experts) * div_up(dx.cols, S::PT) + dw_tiles * dw.experts;
+    const size_t items = row_tiles(dx.m, dx.experts, S::QT) * div_up(dx.cols, S::PT) + dw_tiles * dw.experts;
     return launch(gradients_kernel<T, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, dx, dw, static_cast<unsigned>(dw_tiles));
 }
 
@@ -831,8 +1122,24 @@ template <typename T, Does DOES>
 zvc_status loose_of(const ExpertArgs<T>& p, hipStream_t stream) {
     using S = Small;
     const size_t dw_tiles = DOES == Does::kDw ? div_up(p.cols, S::PT) * div_up(p.rows, S::QT) : 0;
-    const size_t items = DOES == Does::kDw ? dw_tiles * p.experts : row_tiles<S>(p.m, p.experts) * div_up(p.cols, S::PT);
+    const size_t items = DOES == Does::kDw ? dw_tiles * p.experts : row_tiles(p.m, p.experts, S::QT) * div_up(p.cols, S::PT);
     return launch(loose_kernel<T, DOES, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, p, static_cast<unsigned>(dw_tiles));
+}
+
+template <typename T, Does DOES, int QB, bool SPLIT, bool LOOSE>
+zvc_status solo_as(const ExpertArgs<T>& p, unsigned parts, float* sums, hipStream_t stream) {
+    const size_t wide = SPLIT ? kSoloCols : kSoloCols * kSoloWaves, across = div_up(p.cols, wide), dw_tiles = across * div_up(p.rows, 16 * QB);
+    const size_t tiles = DOES == Does::kDw ? dw_tiles * p.experts : row_tiles(p.m, p.experts, 16 * QB) * across;
+    const SoloSplit split = {sums, static_cast<unsigned>(tiles), parts, static_cast<unsigned>(dw_tiles)};
+    const zvc_status st = launch(solo_kernel<T, DOES, QB, SPLIT, LOOSE>, dim3(static_cast<unsigned>(tiles * parts)), 64 * kSoloWaves, stream, p, split);
+    if constexpr (SPLIT)
+        if (st == ZVC_OK && parts > 1) return launch(solo_join_kernel<T, DOES, QB>, dim3(static_cast<unsigned>(tiles * QB)), 256, stream, p, split);
+    return st;
+}
+
+template <typename T, Does DOES, int QB, bool SPLIT>
+zvc_status solo_of(const ExpertArgs<T>& p, const Choice& choice, bool loose, float* sums, hipStream_t stream) {
+    return loose ? solo_as<T, DOES, QB, SPLIT, true>(p, choice.parts, sums, stream) : solo_as<T, DOES, QB, SPLIT, false>(p, choice.parts, sums, stream);
 }
 
 // Whether an operand's rows take 16-byte accesses.
@@ -840,30 +1147,41 @@ template <typename T>
 bool takes_16(const T* at, size_t ld, size_t stride) { return aligned_to(at, 16) && ld * sizeof(T) % 16 == 0 && stride * sizeof(T) % 16 == 0; }
 
 template <typename T>
-zvc_status forward_as(const ExpertArgs<T>& p, hipStream_t stream) {
-    if (!takes_16(p.p, p.ldp, p.sp) || !takes_16(p.q, p.ldq, 0) || p.length * sizeof(T) % 16 != 0) return loose_of<T, Does::kForward>(p, stream);
-    const size_t average = p.m / p.experts;
-    if (average <= 48) return product_of<T, Thin>(p, stream);
+zvc_status forward_as(const ExpertArgs<T>& p, float* sums, hipStream_t stream) {
+    const bool loose = !takes_16(p.p, p.ldp, p.sp) || !takes_16(p.q, p.ldq, 0) || p.length * sizeof(T) % 16 != 0;
+    const Choice choice = choose_rows(p.m, p.experts, p.cols, p.length, sizeof(T), loose);
+    if (choice.kind == Kind::kSolo16) return solo_of<T, Does::kForward, 1, true>(p, choice, loose, sums, stream);
+    if (choice.kind == Kind::kSolo64) return solo_of<T, Does::kForward, 4, true>(p, choice, loose, sums, stream);
+    if (choice.kind == Kind::kLoose) return loose_of<T, Does::kForward>(p, stream);
     if constexpr (sizeof(T) == 2)
-        if (average >= 256) return product_of<T, Large>(p, stream);
+        if (choice.kind == Kind::kLarge) return product_of<T, Large>(p, stream);
     return product_of<T, Eights>(p, stream);
 }
 
 template <typename T>
-zvc_status backward_as(ExpertArgs<T> dx, ExpertArgs<T> dw, hipStream_t stream) {
-    if (dx.cols != 0 && (!takes_16(dx.p, dx.ldp, dx.sp) || !takes_16(dx.q, dx.ldq, 0) || dx.length * sizeof(T) % 16 != 0)) {
-        if (zvc_status st = loose_of<T, Does::kDx>(dx, stream)) return st;
+zvc_status backward_as(ExpertArgs<T> dx, ExpertArgs<T> dw, float* sums, hipStream_t stream) {
+    const bool loose_dx = !takes_16(dx.p, dx.ldp, dx.sp) || !takes_16(dx.q, dx.ldq, 0) || dx.length * sizeof(T) % 16 != 0;
+    const bool loose_dw = !takes_16(dw.p, dw.ldp, 0) || !takes_16(dw.q, dw.ldq, 0);
+    const Choice of_dx = choose_rows(dx.m, dx.experts, dx.cols, dx.length, sizeof(T), loose_dx);
+    const Choice of_dw = choose_dw(dw.m, dw.experts, dw.rows, dw.cols, sizeof(T), loose_dw);
+    const auto tiles = [](const Choice& c) { return c.kind == Kind::kLarge || c.kind == Kind::kSmall; };
+    if (dx.cols != 0 && !tiles(of_dx)) {
+        const zvc_status st = of_dx.kind == Kind::kSolo16   ? solo_of<T, Does::kDx, 1, true>(dx, of_dx, loose_dx, sums, stream)
+                              : of_dx.kind == Kind::kSolo64 ? solo_of<T, Does::kDx, 4, true>(dx, of_dx, loose_dx, sums, stream)
+                                                            : loose_of<T, Does::kDx>(dx, stream);
+        if (st != ZVC_OK) return st;
         dx.cols = 0;
     }
-    if (dw.cols != 0 && (!takes_16(dw.p, dw.ldp, 0) || !takes_16(dw.q, dw.ldq, 0))) {
-        if (zvc_status st = loose_of<T, Does::kDw>(dw, stream)) return st;
+    if (dw.cols != 0 && !tiles(of_dw)) {
+        const zvc_status st = of_dw.kind == Kind::kEach     ? solo_of<T, Does::kDw, 4, false>(dw, of_dw, loose_dw, sums, stream)
+                              : of_dw.kind == Kind::kSolo64 ? solo_of<T, Does::kDw, 4, true>(dw, of_dw, loose_dw, sums, stream)
+                                                            : loose_of<T, Does::kDw>(dw, stream);
+        if (st != ZVC_OK) return st;
         dw.cols = 0;
     }
     if (dx.cols == 0 && dw.cols == 0) return ZVC_OK;
-    const size_t average = dx.m / dx.experts;
-    if (average <= 48) return gradients_of<T, Thin>(dx, dw, stream);
     if constexpr (sizeof(T) == 2)
-        if (average >= 256) return gradients_of<T, Large>(dx, dw, stream);
+        if ((dx.cols != 0 ? of_dx : of_dw).kind == Kind::kLarge) return gradients_of<T, Large>(dx, dw, stream);
     return gradients_of<T, Small>(dx, dw, stream);
 }
 
@@ -944,7 +1262,15 @@ zvc_status zvc_route_backward(const float* d_dweights, const void* d_logits, siz
 }
 
 size_t zvc_expert_workspace_bytes(size_t m, size_t experts, size_t n, size_t k, int type, int backward) {
-    return type_bytes(type) == 0 || !expert_sizes_ok(m, experts, n, k) ? 0 : 256;
+    const size_t w = type_bytes(type);
+    if (w == 0 || !expert_sizes_ok(m, experts, n, k)) return 0;
+    size_t sums = 0;
+    for (const bool loose : {false, true}) {
+        const auto most = [&](const Choice& c) { sums = c.sums > sums ? c.sums : sums; };
+        if (backward == 0) most(choose_rows(m, experts, n, k, w, loose));
+        else most(choose_rows(m, experts, k, n, w, loose)), most(choose_dw(m, experts, n, k, w, loose));
+    }
+    return 256 + round_up(sums, 256);
 }
 
 zvc_status zvc_expert_product(const void* d_x, size_t ldx, const void* d_w, size_t ldw, size_t sw, const int64_t* d_offsets, void* d_y,
@@ -972,7 +1298,7 @@ zvc_status zvc_expert_product(const void* d_x, size_t ldx, const void* d_w, size
         p.q = static_cast<const T*>(d_x), p.ldq = static_cast<unsigned>(ldx);
         p.out = static_cast<T*>(d_y), p.ldo = static_cast<unsigned>(ldy), p.offsets = d_offsets;
         p.m = static_cast<unsigned>(m), p.experts = static_cast<unsigned>(experts), p.cols = static_cast<unsigned>(n), p.length = static_cast<unsigned>(k);
-        return forward_as(p, stream);
+        return forward_as(p, static_cast<float*>(d_ws), stream);
     };
     return type == ZVC_FP32 ? as(0.f) : type == ZVC_FP16 ? as(fp16{}) : as(bf16{});
 }
@@ -1017,7 +1343,7 @@ zvc_status zvc_expert_gradients(const void* d_dy, size_t lddy, const void* d_x, 
         dw.q = static_cast<const T*>(d_dy), dw.ldq = static_cast<unsigned>(lddy);
         dw.out = static_cast<T*>(d_dw), dw.ldo = static_cast<unsigned>(lddw), dw.so = sdw;
         dw.cols = want_dw ? static_cast<unsigned>(k) : 0, dw.rows = static_cast<unsigned>(n);
-        return backward_as(dx, dw, stream);
+        return backward_as(dx, dw, static_cast<float*>(d_ws), stream);
     };
     return type == ZVC_FP32 ? as(0.f) : type == ZVC_FP16 ? as(fp16{}) : as(bf16{});
 }
