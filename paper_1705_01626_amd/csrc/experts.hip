@@ -870,18 +870,17 @@ struct SoloSplit {
     unsigned tiles, parts, dw_tiles;     // at most, of all experts; of a tile's sum; dW: of one expert
 };
 
-// Tiles of 64 columns and 16 QB rows.  SPLIT: the workgroup's waves take turns along the reduction, each with a ring of its own in LDS, and meet there at the end;
-// no wave waits for another.  Else each wave has a tile of its own, four side by side.  LOOSE: operands come by way of registers.
-template <typename T, Does DOES, int QB, bool SPLIT, bool LOOSE>
+// Tiles of 64 columns and 16 QB rows.  The workgroup's waves take turns along the reduction, each with a ring of its own in LDS, and meet there at the end;
+// no wave waits for another.  LOOSE: operands come by way of registers.
+template <typename T, Does DOES, int QB, bool LOOSE>
 __global__ __launch_bounds__(64 * kSoloWaves) void solo_kernel(ExpertArgs<T> p, SoloSplit split) {
     using S = Shape<1, 1, 4, QB, 2>;
     constexpr Lies kP = DOES == Does::kForward ? Lies::kAlong : Lies::kAcross, kQ = DOES == Does::kDw ? Lies::kAcross : Lies::kAlong;
     constexpr int W = sizeof(T), kSteps = kStageBytes / W, kRing = LOOSE ? 1 : 2, kRow = kSoloCols + 4;
-    constexpr int kSums = SPLIT ? kSoloWaves * S::QT * kRow * 4 : 0, kStages = kSoloWaves * kRing * S::kStage;
+    constexpr int kSums = kSoloWaves * S::QT * kRow * 4, kStages = kSoloWaves * kRing * S::kStage;
     __shared__ alignas(1024) unsigned char lds[kSums > kStages ? kSums : kStages];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    constexpr unsigned kWide = SPLIT ? kSoloCols : kSoloCols * kSoloWaves;       // columns of a workgroup
-    const unsigned tp = (p.cols + kWide - 1) / kWide, id = place_of(blockIdx.x, gridDim.x), item = id / split.parts, part = id - item * split.parts;
+    const unsigned tp = (p.cols + kSoloCols - 1) / kSoloCols, id = place_of(blockIdx.x, gridDim.x), item = id / split.parts, part = id - item * split.parts;
     Place place;
     unsigned length, rows_end, row0, col0;
     const T *from_p, *from_q;
@@ -890,17 +889,15 @@ __global__ __launch_bounds__(64 * kSoloWaves) void solo_kernel(ExpertArgs<T> p, 
         place.expert = item / split.dw_tiles, place.at = item - place.expert * split.dw_tiles;
         find_rows(p.offsets, place.expert, p.m, lane, &place.begin, &place.end);
         const unsigned tq = (p.rows + S::QT - 1) / S::QT;
-        col0 = place.at / tq * kWide, row0 = place.at % tq * S::QT;
+        col0 = place.at / tq * kSoloCols, row0 = place.at % tq * S::QT;
         length = place.end - place.begin, rows_end = p.rows;
         out += place.expert * p.so;
     } else {
         if (!find_tile(p.offsets, p.experts, p.m, tp, S::QT, item, lane, &place)) return;
         const unsigned tq = (place.end - place.begin + S::QT - 1) / S::QT;
-        col0 = place.at / tq * kWide, row0 = place.begin + place.at % tq * S::QT;
+        col0 = place.at / tq * kSoloCols, row0 = place.begin + place.at % tq * S::QT;
         length = p.length, rows_end = place.end;
     }
-    if constexpr (!SPLIT) col0 += wave * kSoloCols;
-    if (!SPLIT && col0 >= p.cols) return;
     if constexpr (DOES == Does::kDw) {
         from_p = cell(p.p, place.begin, p.ldp, col0), from_q = cell(p.q, place.begin, p.ldq, row0);
     } else {
@@ -910,7 +907,7 @@ __global__ __launch_bounds__(64 * kSoloWaves) void solo_kernel(ExpertArgs<T> p, 
     }
     const unsigned stages = (length + kSteps - 1) / kSteps, begin = static_cast<unsigned>(uint64_t{stages} * part / split.parts),
                    end = static_cast<unsigned>(uint64_t{stages} * (part + 1) / split.parts);
-    const unsigned first = begin + (SPLIT ? wave : 0), step = SPLIT ? kSoloWaves : 1, mine = first < end ? (end - first + step - 1) / step : 0;
+    const unsigned first = begin + wave, mine = first < end ? (end - first + kSoloWaves - 1) / kSoloWaves : 0;
     const size_t step_p = size_t{kSteps} * (DOES == Does::kForward ? 1 : p.ldp), step_q = size_t{kSteps} * (DOES == Does::kDw ? p.ldq : 1);
     const unsigned base = address(lds) + wave * (kRing * S::kStage);
     const int side_p = min(static_cast<int>(p.cols - col0), kSoloCols), side_q = min(static_cast<int>(rows_end - row0), S::QT);
@@ -928,7 +925,7 @@ __global__ __launch_bounds__(64 * kSoloWaves) void solo_kernel(ExpertArgs<T> p, 
         in_q.op.init(0, lane, 0, 0);
         const bool short_p = (DOES == Does::kForward ? p.length : p.cols) * W < 16, short_q = (DOES == Does::kDw ? p.rows : p.length) * W < 16;
         const auto load = [&](unsigned i) {
-            const unsigned s = first + i * step;
+            const unsigned s = first + i * kSoloWaves;
             const int left = static_cast<int>(length - s * kSteps);
             in_p.load(from_p + s * step_p, p.ldp, side_p, left, short_p);
             in_q.load(from_q + s * step_q, p.ldq, side_q, left, short_q);
@@ -950,7 +947,7 @@ __global__ __launch_bounds__(64 * kSoloWaves) void solo_kernel(ExpertArgs<T> p, 
         in_q.init(0, lane, p.ldq, side_q);
         constexpr int kLoads = decltype(in_p)::kLoads + decltype(in_q)::kLoads;
         const auto fetch = [&](unsigned i) {
-            const unsigned s = first + i * step, to = base + (i % kRing) * S::kStage;
+            const unsigned s = first + i * kSoloWaves, to = base + (i % kRing) * S::kStage;
             const int left = static_cast<int>(length - s * kSteps);
             in_p.fetch(reinterpret_cast<uint64_t>(from_p + s * step_p), 0, left, to);
             in_q.fetch(reinterpret_cast<uint64_t>(from_q + s * step_q), 0, left, to + S::PT * kStageBytes);
@@ -968,29 +965,25 @@ __global__ __launch_bounds__(64 * kSoloWaves) void solo_kernel(ExpertArgs<T> p, 
             x.template product<1>();
         }
     }
-    if constexpr (!SPLIT) {
-        store_strip<T, S>(out, p.ldo, rows_end, p.cols, row0, col0, lane, x.acc);
-    } else {
-        __syncthreads();
-        float* const sums = reinterpret_cast<float*>(lds);
-        const int r = lane & 15, quarter = lane >> 4;
+    __syncthreads();
+    float* const sums = reinterpret_cast<float*>(lds);
+    const int r = lane & 15, quarter = lane >> 4;
 #pragma unroll
-        for (int j = 0; j < QB; ++j)
+    for (int j = 0; j < QB; ++j)
 #pragma unroll
-            for (int i = 0; i < S::PB; ++i)
-                *reinterpret_cast<float4v*>(sums + (wave * S::QT + j * 16 + r) * kRow + i * 16 + quarter * 4) = x.acc[i][j];
-        __syncthreads();
+        for (int i = 0; i < S::PB; ++i)
+            *reinterpret_cast<float4v*>(sums + (wave * S::QT + j * 16 + r) * kRow + i * 16 + quarter * 4) = x.acc[i][j];
+    __syncthreads();
 #pragma unroll
-        for (int j = 0; j < QB; ++j) {                               // 16 rows of 64 columns: four neighbouring ones a thread
-            const unsigned row_in = j * 16 + threadIdx.x / 16, col_in = threadIdx.x % 16 * 4, row = row0 + row_in, col = col0 + col_in;
-            float4v sum = *reinterpret_cast<const float4v*>(sums + row_in * kRow + col_in);
+    for (int j = 0; j < QB; ++j) {                               // 16 rows of 64 columns: four neighbouring ones a thread
+        const unsigned row_in = j * 16 + threadIdx.x / 16, col_in = threadIdx.x % 16 * 4, row = row0 + row_in, col = col0 + col_in;
+        float4v sum = *reinterpret_cast<const float4v*>(sums + row_in * kRow + col_in);
 #pragma unroll
-            for (int w = 1; w < kSoloWaves; ++w) sum += *reinterpret_cast<const float4v*>(sums + (w * S::QT + row_in) * kRow + col_in);
-            if (split.parts > 1) {
-                *reinterpret_cast<float4v*>(split.sums + ((size_t{part} * split.tiles + item) * S::QT + row_in) * kSoloCols + col_in) = sum;
-            } else if (row < rows_end) {
-                store_four(cell(out, row, p.ldo, col), sum, p.cols - col, col < p.cols);
-            }
+        for (int w = 1; w < kSoloWaves; ++w) sum += *reinterpret_cast<const float4v*>(sums + (w * S::QT + row_in) * kRow + col_in);
+        if (split.parts > 1) {
+            *reinterpret_cast<float4v*>(split.sums + ((size_t{part} * split.tiles + item) * S::QT + row_in) * kSoloCols + col_in) = sum;
+        } else if (row < rows_end) {
+            store_four(cell(out, row, p.ldo, col), sum, p.cols - col, col < p.cols);
         }
     }
 }
@@ -1062,45 +1055,73 @@ using Large = Shape<4, 2, 4, 8, 2>;             // 256 x 256, eight waves
 using Eights = Shape<2, 4, 4, 2, 2>;            // 128 x 128, eight waves
 using Small = Shape<2, 2, 4, 4, 2>;             // 128 x 128, four waves
 
-// Which kernel takes a product: persistent tiles, tiles by way of registers, or the small kernels (their rows; kEach: a tile a wave).
-enum class Kind { kLarge, kSmall, kLoose, kSolo16, kSolo64, kEach };
+// Which kernel takes a product: persistent tiles of 256 x 256 or 128 x 128, the latter by way of registers, or the small kernels by their rows.
+enum class Kind { kLarge, kSmall, kLoose, kSolo16, kSolo64 };
 
 struct Choice {
     Kind kind;
     unsigned parts;                             // of a small kernel's sums
     size_t sums;                                // their bytes
+    double cost;
 };
 
 // Upper bound of the tiles by rows: every expert's last one may be short.
 size_t row_tiles(size_t m, size_t experts, size_t tile) { return m / tile + (experts < m ? experts : m); }
+// How many there will be: an expert's last tile is half full on the average.
+double expected_tiles(size_t m, size_t experts, size_t tile) {
+    const double used = static_cast<double>(experts < m ? experts : m), each = used > 0 ? static_cast<double>(m) / used / tile + 0.5 : 0;
+    return used * (each > 1 ? each : 1);
+}
 
-// Parts of the sums of a small kernel where its tiles do not fill the compute units.
-Choice solo_choice(Kind kind, size_t tiles, size_t rows, size_t stages) {
-    constexpr size_t kSlots = 2 * kUnits;
-    size_t parts = tiles == 0 ? 1 : kSlots / tiles;
+// The account that chooses, in us: tiles in rounds of those that run at a time, each its stages and something to begin and finish.  Fitted to calls
+// with every kernel forced in turn (m rows evenly over E experts, n, k; weights from memory), L large, S small tiles, s16 and s64 the small kernels:
+//   bf16 forward  8 x 32, 2048, 2048: S 25.6, s16 18.9, s64 21.5    8 x 128, 2048, 2048: S 27.3, s16 36.4, s64 29.3    64 x 64, 2048, 128: S 14.2, s16 59.1, s64 64.7
+//                 2 x 256, 512, 2048: S 24.0, s16 10.0, s64 16.5    16 x 512, 1024, 1024: L 30.7, S 29.4, s64 58.8    16 x 512, 5632, 2048: L 229, S 251
+//   fp32 forward  8 x 64, 2048, 2048: S 134, s16 72.5, s64 79.7     8 x 256, 2048, 2048: S 241, s16 195, s64 193      16 x 512, 1024, 1024: S 188, s16 209, s64 195
+//   dW            bf16 1 x 4000, 256, 512: S 43.5, s64 12.6         bf16 8 x 256, 2048, 2048: L 33.6, S 31.5, s64 168  fp32 2 x 1024, 512, 2048: S 80.9, s64 52.5
+//   (tiles of 256 x 32 and small kernels with a tile for each wave were slower than these or the same everywhere)
+constexpr double kLaunchUs = 5, kJoinUs = 3, kSumsPerUs = 3e6;
+
+Choice large_choice(double tiles, double stages) { return {Kind::kLarge, 1, 0, kLaunchUs + std::ceil(tiles / kUnits) * (1.45 * stages + 10)}; }
+
+Choice small_choice(double tiles, double stages, size_t w, bool loose) {
+    double us;
+    if (w == 4) us = std::ceil(tiles / kUnits) * (1.95 * stages + 2);                  // the matrix instructions bound it: two on a compute unit take twice as long
+    else us = std::fmax(1, tiles / (2 * kUnits)) * ((tiles <= kUnits ? 0.62 : tiles <= 2 * kUnits ? 0.72 : 1.05) * stages + 2);
+    return {loose ? Kind::kLoose : Kind::kSmall, 1, 0, kLaunchUs + (loose ? (w == 4 ? 1.3 : 1.5) : 1) * us};
+}
+
+// Parts of a small kernel's sums where its tiles do not fill the compute units.  most: tiles at most.
+Choice solo_choice(Kind kind, size_t most, double tiles, size_t stages, size_t slots, double stage_us, double item_us) {
+    const size_t rows = kind == Kind::kSolo16 ? 16 : 64;
+    size_t parts = tiles < 1 ? 1 : static_cast<size_t>(2 * kUnits / tiles);
     if (parts > stages / (2 * kSoloWaves)) parts = stages / (2 * kSoloWaves);
     if (parts > 16) parts = 16;
-    if (parts < 2) return {kind, 1, 0};
-    return {kind, static_cast<unsigned>(parts), parts * tiles * rows * kSoloCols * sizeof(float)};
+    if (parts < 2) parts = 1;
+    const size_t sums = parts > 1 ? parts * most * rows * kSoloCols * sizeof(float) : 0;
+    const double each = item_us + stage_us * static_cast<double>(stages) / parts;
+    return {kind, static_cast<unsigned>(parts), sums, kLaunchUs + std::fmax(1, tiles * parts / slots) * each + (parts > 1 ? kJoinUs + sums / kSumsPerUs : 0)};
 }
+
+Choice cheaper(const Choice& a, const Choice& b) { return b.cost < a.cost ? b : a; }
 
 // Of y or dx: `cols` columns, sums over `length`.
 Choice choose_rows(size_t m, size_t experts, size_t cols, size_t length, size_t w, bool loose) {
-    const size_t average = m / experts, stages = div_up(length, kStageBytes / w), across = div_up(cols, kSoloCols);
-    if (average <= 16) return solo_choice(Kind::kSolo16, row_tiles(m, experts, 16) * across, 16, stages);
-    const size_t tiles = row_tiles(m, experts, 64) * across;
-    if (average <= 64 || tiles <= 4 * kUnits) return solo_choice(Kind::kSolo64, tiles, 64, stages);
-    if (loose) return {Kind::kLoose, 1, 0};
-    return {w == 2 && average >= 256 ? Kind::kLarge : Kind::kSmall, 1, 0};
+    const size_t stages = div_up(length, kStageBytes / w), across = div_up(cols, kSoloCols);
+    Choice best = small_choice(expected_tiles(m, experts, 128) * div_up(cols, 128), stages, w, loose);
+    if (w == 2 && !loose) best = cheaper(best, large_choice(expected_tiles(m, experts, 256) * div_up(cols, 256), stages));
+    best = cheaper(best, solo_choice(Kind::kSolo16, row_tiles(m, experts, 16) * across, expected_tiles(m, experts, 16) * across, stages, 2 * kUnits,
+                                     w == 4 ? 0.34 : 0.23, w == 4 ? 3.4 : 2.8));
+    return cheaper(best, solo_choice(Kind::kSolo64, row_tiles(m, experts, 64) * across, expected_tiles(m, experts, 64) * across, stages, kUnits,
+                                     w == 4 ? 0.6 : 0.15, 4.7));
 }
 
 // Of dW.
 Choice choose_dw(size_t m, size_t experts, size_t n, size_t k, size_t w, bool loose) {
-    const size_t average = m / experts, stages = div_up(average, kStageBytes / w), tiles = div_up(n, 64) * div_up(k, kSoloCols) * experts;
-    if (stages <= 4) return {Kind::kEach, 1, 0};
-    if (tiles <= 4 * kUnits) return solo_choice(Kind::kSolo64, tiles, 64, stages);
-    if (loose) return {Kind::kLoose, 1, 0};
-    return {w == 2 && average >= 256 ? Kind::kLarge : Kind::kSmall, 1, 0};
+    const size_t stages = div_up(div_up(m, experts), kStageBytes / w), tiles = div_up(n, 64) * div_up(k, kSoloCols) * experts;
+    Choice best = small_choice(static_cast<double>(div_up(n, 128) * div_up(k, 128) * experts), stages, w, loose);
+    if (w == 2 && !loose) best = cheaper(best, large_choice(static_cast<double>(div_up(n, 256) * div_up(k, 256) * experts), stages));
+    return cheaper(best, solo_choice(Kind::kSolo64, tiles, static_cast<double>(tiles), stages, kUnits, w == 4 ? 1.4 : 0.55, w == 4 ? 4 : 3));
 }
 
 unsigned grid_of(size_t items, unsigned room) { return static_cast<unsigned>(items < room ? items : room); }
@@ -1126,20 +1147,19 @@ zvc_status loose_of(const ExpertArgs<T>& p, hipStream_t stream) {
     return launch(loose_kernel<T, DOES, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, p, static_cast<unsigned>(dw_tiles));
 }
 
-template <typename T, Does DOES, int QB, bool SPLIT, bool LOOSE>
+template <typename T, Does DOES, int QB, bool LOOSE>
 zvc_status solo_as(const ExpertArgs<T>& p, unsigned parts, float* sums, hipStream_t stream) {
-    const size_t wide = SPLIT ? kSoloCols : kSoloCols * kSoloWaves, across = div_up(p.cols, wide), dw_tiles = across * div_up(p.rows, 16 * QB);
+    const size_t across = div_up(p.cols, kSoloCols), dw_tiles = across * div_up(p.rows, 16 * QB);
     const size_t tiles = DOES == Does::kDw ? dw_tiles * p.experts : row_tiles(p.m, p.experts, 16 * QB) * across;
     const SoloSplit split = {sums, static_cast<unsigned>(tiles), parts, static_cast<unsigned>(dw_tiles)};
-    const zvc_status st = launch(solo_kernel<T, DOES, QB, SPLIT, LOOSE>, dim3(static_cast<unsigned>(tiles * parts)), 64 * kSoloWaves, stream, p, split);
-    if constexpr (SPLIT)
-        if (st == ZVC_OK && parts > 1) return launch(solo_join_kernel<T, DOES, QB>, dim3(static_cast<unsigned>(tiles * QB)), 256, stream, p, split);
-    return st;
+    const zvc_status st = launch(solo_kernel<T, DOES, QB, LOOSE>, dim3(static_cast<unsigned>(tiles * parts)), 64 * kSoloWaves, stream, p, split);
+    if (st != ZVC_OK || parts == 1) return st;
+    return launch(solo_join_kernel<T, DOES, QB>, dim3(static_cast<unsigned>(tiles * QB)), 256, stream, p, split);
 }
 
-template <typename T, Does DOES, int QB, bool SPLIT>
+template <typename T, Does DOES, int QB>
 zvc_status solo_of(const ExpertArgs<T>& p, const Choice& choice, bool loose, float* sums, hipStream_t stream) {
-    return loose ? solo_as<T, DOES, QB, SPLIT, true>(p, choice.parts, sums, stream) : solo_as<T, DOES, QB, SPLIT, false>(p, choice.parts, sums, stream);
+    return loose ? solo_as<T, DOES, QB, true>(p, choice.parts, sums, stream) : solo_as<T, DOES, QB, false>(p, choice.parts, sums, stream);
 }
 
 // Whether an operand's rows take 16-byte accesses.
@@ -1150,8 +1170,8 @@ template <typename T>
 zvc_status forward_as(const ExpertArgs<T>& p, float* sums, hipStream_t stream) {
     const bool loose = !takes_16(p.p, p.ldp, p.sp) || !takes_16(p.q, p.ldq, 0) || p.length * sizeof(T) % 16 != 0;
     const Choice choice = choose_rows(p.m, p.experts, p.cols, p.length, sizeof(T), loose);
-    if (choice.kind == Kind::kSolo16) return solo_of<T, Does::kForward, 1, true>(p, choice, loose, sums, stream);
-    if (choice.kind == Kind::kSolo64) return solo_of<T, Does::kForward, 4, true>(p, choice, loose, sums, stream);
+    if (choice.kind == Kind::kSolo16) return solo_of<T, Does::kForward, 1>(p, choice, loose, sums, stream);
+    if (choice.kind == Kind::kSolo64) return solo_of<T, Does::kForward, 4>(p, choice, loose, sums, stream);
     if (choice.kind == Kind::kLoose) return loose_of<T, Does::kForward>(p, stream);
     if constexpr (sizeof(T) == 2)
         if (choice.kind == Kind::kLarge) return product_of<T, Large>(p, stream);
@@ -1166,16 +1186,15 @@ zvc_status backward_as(ExpertArgs<T> dx, ExpertArgs<T> dw, float* sums, hipStrea
     const Choice of_dw = choose_dw(dw.m, dw.experts, dw.rows, dw.cols, sizeof(T), loose_dw);
     const auto tiles = [](const Choice& c) { return c.kind == Kind::kLarge || c.kind == Kind::kSmall; };
     if (dx.cols != 0 && !tiles(of_dx)) {
-        const zvc_status st = of_dx.kind == Kind::kSolo16   ? solo_of<T, Does::kDx, 1, true>(dx, of_dx, loose_dx, sums, stream)
-                              : of_dx.kind == Kind::kSolo64 ? solo_of<T, Does::kDx, 4, true>(dx, of_dx, loose_dx, sums, stream)
+        const zvc_status st = of_dx.kind == Kind::kSolo16   ? solo_of<T, Does::kDx, 1>(dx, of_dx, loose_dx, sums, stream)
+                              : of_dx.kind == Kind::kSolo64 ? solo_of<T, Does::kDx, 4>(dx, of_dx, loose_dx, sums, stream)
                                                             : loose_of<T, Does::kDx>(dx, stream);
         if (st != ZVC_OK) return st;
         dx.cols = 0;
     }
     if (dw.cols != 0 && !tiles(of_dw)) {
-        const zvc_status st = of_dw.kind == Kind::kEach     ? solo_of<T, Does::kDw, 4, false>(dw, of_dw, loose_dw, sums, stream)
-                              : of_dw.kind == Kind::kSolo64 ? solo_of<T, Does::kDw, 4, true>(dw, of_dw, loose_dw, sums, stream)
-                                                            : loose_of<T, Does::kDw>(dw, stream);
+        const zvc_status st = of_dw.kind == Kind::kSolo64 ? solo_of<T, Does::kDw, 4>(dw, of_dw, loose_dw, sums, stream)
+                                                          : loose_of<T, Does::kDw>(dw, stream);
         if (st != ZVC_OK) return st;
         dw.cols = 0;
     }
