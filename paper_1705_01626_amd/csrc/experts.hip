@@ -712,26 +712,40 @@ struct LooseOperand {
     Op op;
     int4v v[Op::kLoads];
 
-    // `left`: of the reduction; `side`: rows (kAlong) or columns (kAcross) that exist; `shorter`: rows have less than 16 bytes in all.
+    // Elements of unit i that exist: `left` of the reduction, `side` rows (kAlong) or columns (kAcross).
+    __device__ __forceinline__ int there(int i, int side, int left, int* row) const {
+        *row = (op.first + i) * Op::kRowsPerLoad + op.lane_row;
+        const int col = op.logical(*row) / static_cast<int>(sizeof(T));
+        return *row < (LIES == Lies::kAlong ? side : left) ? (LIES == Lies::kAlong ? left : side) - col : 0;
+    }
+    // `shorter`: rows have less than 16 bytes in all.
     __device__ __forceinline__ void load(const T* base, size_t ld, int side, int left, bool shorter) {
 #pragma unroll
         for (int i = 0; i < Op::kLoads; ++i) {
-            const int row = (op.first + i) * Op::kRowsPerLoad + op.lane_row, col = op.logical(row) / static_cast<int>(sizeof(T));
-            const int rows = LIES == Lies::kAlong ? side : left, there = (LIES == Lies::kAlong ? left : side) - col;
+            int row;
+            const int have = there(i, side, left, &row);
             v[i] = int4v{0, 0, 0, 0};
-            if (row >= rows || there <= 0) continue;
-            const T* const at = base + row * ld + col;
+            if (have <= 0) continue;
+            const T* const at = base + row * ld + op.logical(row) / static_cast<int>(sizeof(T));
             if (!shorter) {
-                const int missing = there < kPer ? kPer - there : 0;
-                __builtin_memcpy(&v[i], at - missing, 16);
-                if (missing != 0) v[i] = moved_down(v[i], missing * static_cast<int>(sizeof(T)));
+                __builtin_memcpy(&v[i], at - (have < kPer ? kPer - have : 0), 16);
             } else {
                 Pack<T> one = {};
 #pragma unroll
                 for (int j = 0; j < kPer; ++j)
-                    if (j < there) one.v[j] = at[j];
+                    if (j < have) one.v[j] = at[j];
                 v[i] = __builtin_bit_cast(int4v, one);
             }
+        }
+    }
+    // With load's arguments: what was read too far in front goes into place.  (Not in load, where each load would be waited for.)
+    __device__ __forceinline__ void settle(int side, int left, bool shorter) {
+        if (shorter || (LIES == Lies::kAlong ? left >= Op::kSteps : side >= SIDE)) return;
+#pragma unroll
+        for (int i = 0; i < Op::kLoads; ++i) {
+            int row;
+            const int have = there(i, side, left, &row);
+            if (have > 0 && have < kPer) v[i] = moved_down(v[i], (kPer - have) * static_cast<int>(sizeof(T)));
         }
     }
     __device__ __forceinline__ void store(unsigned lds, int lane) const {
@@ -774,6 +788,9 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void loose_kernel(ExpertA
             in_q.load(tile.q + step_q, p.ldq, side_q, left, short_q);
         };
         const auto store = [&](unsigned s) {
+            const int left = static_cast<int>(tile.length - s * kSteps);
+            in_p.settle(side_p, left, short_p);
+            in_q.settle(side_q, left, short_q);
             in_p.store(base + (s & 1) * S::kStage, lane);
             in_q.store(base + (s & 1) * S::kStage + S::PT * kStageBytes, lane);
         };
@@ -870,17 +887,21 @@ struct SoloSplit {
     unsigned tiles, parts, dw_tiles;     // at most, of all experts; of a tile's sum; dW: of one expert
 };
 
-// Tiles of 64 columns and 16 QB rows.  The workgroup's waves take turns along the reduction, each with a ring of its own in LDS, and meet there at the end;
-// no wave waits for another.  LOOSE: operands come by way of registers.
+// Tiles of 64 columns and 16 QB rows.  The workgroup's waves take turns along the reduction, each with a place of its own in LDS for a stage, and meet there at
+// the end; no wave waits for another.  What hides a wave's wait for its next stage are the other waves: four workgroups of 16 rows fit a compute unit, two of
+// 64.  (With two places a wave, and half as many waves, 16 x 512 rows, 1024 x 1024, bf16 took 58.8 instead of 40.0; 8 x 128, 2048 x 2048 29.3 and 24.6.)
+// LOOSE: operands come by way of registers.
 template <typename T, Does DOES, int QB, bool LOOSE>
-__global__ __launch_bounds__(64 * kSoloWaves) void solo_kernel(ExpertArgs<T> p, SoloSplit split) {
+__global__ __launch_bounds__(64 * kSoloWaves, QB == 1 ? (LOOSE ? 3 : 4) : 2) void solo_kernel(ExpertArgs<T> p, SoloSplit split) {
     using S = Shape<1, 1, 4, QB, 2>;
     constexpr Lies kP = DOES == Does::kForward ? Lies::kAlong : Lies::kAcross, kQ = DOES == Does::kDw ? Lies::kAcross : Lies::kAlong;
-    constexpr int W = sizeof(T), kSteps = kStageBytes / W, kRing = LOOSE ? 1 : 2, kRow = kSoloCols + 4;
-    constexpr int kSums = kSoloWaves * S::QT * kRow * 4, kStages = kSoloWaves * kRing * S::kStage;
+    constexpr int W = sizeof(T), kSteps = kStageBytes / W, kRow = kSoloCols + 4;
+    constexpr int kSums = kSoloWaves * S::QT * kRow * 4, kStages = kSoloWaves * S::kStage;
     __shared__ alignas(1024) unsigned char lds[kSums > kStages ? kSums : kStages];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned tp = (p.cols + kSoloCols - 1) / kSoloCols, id = place_of(blockIdx.x, gridDim.x), item = id / split.parts, part = id - item * split.parts;
+    // (dW: an expert's tiles are spread over the XCDs, since experts differ in what a tile costs)
+    const unsigned tp = (p.cols + kSoloCols - 1) / kSoloCols, id = DOES == Does::kDw ? blockIdx.x : place_of(blockIdx.x, gridDim.x);
+    const unsigned item = id / split.parts, part = id - item * split.parts;
     Place place;
     unsigned length, rows_end, row0, col0;
     const T *from_p, *from_q;
@@ -909,15 +930,11 @@ __global__ __launch_bounds__(64 * kSoloWaves) void solo_kernel(ExpertArgs<T> p, 
                    end = static_cast<unsigned>(uint64_t{stages} * (part + 1) / split.parts);
     const unsigned first = begin + wave, mine = first < end ? (end - first + kSoloWaves - 1) / kSoloWaves : 0;
     const size_t step_p = size_t{kSteps} * (DOES == Does::kForward ? 1 : p.ldp), step_q = size_t{kSteps} * (DOES == Does::kDw ? p.ldq : 1);
-    const unsigned base = address(lds) + wave * (kRing * S::kStage);
+    const unsigned base = address(lds) + wave * S::kStage;
     const int side_p = min(static_cast<int>(p.cols - col0), kSoloCols), side_q = min(static_cast<int>(rows_end - row0), S::QT);
     Multiplier<T, DOES, S> x;
     x.init(base, 0, 0, lane);
     x.clear();
-    const auto multiply_stage = [&](unsigned stage) {
-        x.template read<0>(stage);
-        x.template read<1>(stage);
-    };
     if constexpr (LOOSE) {
         LooseOperand<T, kP, S::PT, 1> in_p;
         LooseOperand<T, kQ, S::QT, 1> in_q;
@@ -932,11 +949,15 @@ __global__ __launch_bounds__(64 * kSoloWaves) void solo_kernel(ExpertArgs<T> p, 
         };
         if (mine != 0) load(0);
         for (unsigned i = 0; i < mine; ++i) {
+            const int left = static_cast<int>(length - (first + i * kSoloWaves) * kSteps);
+            in_p.settle(side_p, left, short_p);
+            in_q.settle(side_q, left, short_q);
             in_p.store(base, lane);
             in_q.store(base + S::PT * kStageBytes, lane);
             if (i + 1 < mine) load(i + 1);
             wait_reads();                                            // (what was stored is there)
-            multiply_stage(0);
+            x.template read<0>(0);
+            x.template read<1>(0);
             x.template product<0>();
             x.template product<1>();
         }
@@ -945,22 +966,19 @@ __global__ __launch_bounds__(64 * kSoloWaves) void solo_kernel(ExpertArgs<T> p, 
         Operand<T, kQ, S::QT, 1, false> in_q;
         in_p.init(0, lane, p.ldp, side_p);
         in_q.init(0, lane, p.ldq, side_q);
-        constexpr int kLoads = decltype(in_p)::kLoads + decltype(in_q)::kLoads;
         const auto fetch = [&](unsigned i) {
-            const unsigned s = first + i * kSoloWaves, to = base + (i % kRing) * S::kStage;
+            const unsigned s = first + i * kSoloWaves;
             const int left = static_cast<int>(length - s * kSteps);
-            in_p.fetch(reinterpret_cast<uint64_t>(from_p + s * step_p), 0, left, to);
-            in_q.fetch(reinterpret_cast<uint64_t>(from_q + s * step_q), 0, left, to + S::PT * kStageBytes);
+            in_p.fetch(reinterpret_cast<uint64_t>(from_p + s * step_p), 0, left, base);
+            in_q.fetch(reinterpret_cast<uint64_t>(from_q + s * step_q), 0, left, base + S::PT * kStageBytes);
         };
-#pragma unroll
-        for (unsigned i = 0; i < kRing; ++i)
-            if (i < mine) fetch(i);
+        if (mine != 0) fetch(0);
         for (unsigned i = 0; i < mine; ++i) {
-            if (i + kRing <= mine) wait_loads<(kRing - 1) * kLoads>();
-            else wait_loads<0>();
-            multiply_stage((i % kRing) * S::kStage);
-            wait_reads();                                            // before their place is written again
-            if (i + kRing < mine) fetch(i + kRing);
+            wait_loads<0>();
+            x.template read<0>(0);
+            x.template read<1>(0);
+            wait_reads();                                            // before the place is written again
+            if (i + 1 < mine) fetch(i + 1);
             x.template product<0>();
             x.template product<1>();
         }
@@ -1075,10 +1093,10 @@ double expected_tiles(size_t m, size_t experts, size_t tile) {
 
 // The account that chooses, in us: tiles in rounds of those that run at a time, each its stages and something to begin and finish.  Fitted to calls
 // with every kernel forced in turn (m rows evenly over E experts, n, k; weights from memory), L large, S small tiles, s16 and s64 the small kernels:
-//   bf16 forward  8 x 32, 2048, 2048: S 25.6, s16 18.9, s64 21.5    8 x 128, 2048, 2048: S 27.3, s16 36.4, s64 29.3    64 x 64, 2048, 128: S 14.2, s16 59.1, s64 64.7
-//                 2 x 256, 512, 2048: S 24.0, s16 10.0, s64 16.5    16 x 512, 1024, 1024: L 30.7, S 29.4, s64 58.8    16 x 512, 5632, 2048: L 229, S 251
-//   fp32 forward  8 x 64, 2048, 2048: S 134, s16 72.5, s64 79.7     8 x 256, 2048, 2048: S 241, s16 195, s64 193      16 x 512, 1024, 1024: S 188, s16 209, s64 195
-//   dW            bf16 1 x 4000, 256, 512: S 43.5, s64 12.6         bf16 8 x 256, 2048, 2048: L 33.6, S 31.5, s64 168  fp32 2 x 1024, 512, 2048: S 80.9, s64 52.5
+//   bf16 forward  8 x 32, 2048, 2048: S 25.6, s16 18.3, s64 25.5    8 x 128, 2048, 2048: S 27.3, s16 34.9, s64 24.6    64 x 64, 2048, 128: S 14.2, s16 35.5, s64 38.1
+//                 2 x 256, 512, 2048: S 24.0, s16 9.4, s64 13.1     16 x 512, 1024, 1024: L 30.7, S 29.4, s64 40.0     16 x 512, 5632, 2048: L 229, S 251
+//   fp32 forward  8 x 32, 2048, 2048: S 132, s16 43.6, s64 81.9     8 x 128, 2048, 2048: S 136, s16 109, s64 131       16 x 512, 1024, 1024: S 188, s16 195, s64 181
+//   dW            bf16 5 x 600, 1024, 512: S 17.2, s64 14.4         bf16 8 x 128, 2048, 2048: S 26.3, s64 69.6         fp32 5 x 600, 1024, 512: S 80.2, s64 47.6
 //   (tiles of 256 x 32 and small kernels with a tile for each wave were slower than these or the same everywhere)
 constexpr double kLaunchUs = 5, kJoinUs = 3, kSumsPerUs = 3e6;
 
@@ -1110,18 +1128,20 @@ Choice choose_rows(size_t m, size_t experts, size_t cols, size_t length, size_t 
     const size_t stages = div_up(length, kStageBytes / w), across = div_up(cols, kSoloCols);
     Choice best = small_choice(expected_tiles(m, experts, 128) * div_up(cols, 128), stages, w, loose);
     if (w == 2 && !loose) best = cheaper(best, large_choice(expected_tiles(m, experts, 256) * div_up(cols, 256), stages));
-    best = cheaper(best, solo_choice(Kind::kSolo16, row_tiles(m, experts, 16) * across, expected_tiles(m, experts, 16) * across, stages, 2 * kUnits,
-                                     w == 4 ? 0.34 : 0.23, w == 4 ? 3.4 : 2.8));
-    return cheaper(best, solo_choice(Kind::kSolo64, row_tiles(m, experts, 64) * across, expected_tiles(m, experts, 64) * across, stages, kUnits,
-                                     w == 4 ? 0.6 : 0.15, 4.7));
+    best = cheaper(best, solo_choice(Kind::kSolo16, row_tiles(m, experts, 16) * across, expected_tiles(m, experts, 16) * across, stages, 4 * kUnits,
+                                     w == 4 ? 0.65 : 0.3, w == 4 ? 4.1 : 2.8));
+    return cheaper(best, solo_choice(Kind::kSolo64, row_tiles(m, experts, 64) * across, expected_tiles(m, experts, 64) * across, stages, 2 * kUnits,
+                                     w == 4 ? 1.2 : 0.25, w == 4 ? 7.8 : 5));
 }
 
-// Of dW.
+// Of dW.  An expert may have several times the average of rows: a kernel does not end before its tiles have.
 Choice choose_dw(size_t m, size_t experts, size_t n, size_t k, size_t w, bool loose) {
     const size_t stages = div_up(div_up(m, experts), kStageBytes / w), tiles = div_up(n, 64) * div_up(k, kSoloCols) * experts;
+    const double longest = experts > 1 ? 3.0 * stages : stages;
     Choice best = small_choice(static_cast<double>(div_up(n, 128) * div_up(k, 128) * experts), stages, w, loose);
+    best.cost = std::fmax(best.cost, kLaunchUs + longest * (w == 4 ? 1.95 : 0.72) * (loose ? 1.4 : 1));
     if (w == 2 && !loose) best = cheaper(best, large_choice(static_cast<double>(div_up(n, 256) * div_up(k, 256) * experts), stages));
-    return cheaper(best, solo_choice(Kind::kSolo64, tiles, static_cast<double>(tiles), stages, kUnits, w == 4 ? 1.4 : 0.55, w == 4 ? 4 : 3));
+    return cheaper(best, solo_choice(Kind::kSolo64, tiles, static_cast<double>(tiles), stages, 2 * kUnits, w == 4 ? 1.3 : 0.42, w == 4 ? 3.6 : 2.9));
 }
 
 unsigned grid_of(size_t items, unsigned room) { return static_cast<unsigned>(items < room ? items : room); }
