@@ -472,11 +472,12 @@ struct Tile {
     }
 };
 
-// Two numbers of 16 bits in a word.
+// Two numbers of 16 bits in a word: one instruction for bf16, as a vector (two and more of a structure's members).
 template <typename T>
-__device__ __forceinline__ unsigned pack(float a, float b) {
-    struct Two { T a, b; };
-    return __builtin_bit_cast(unsigned, Two{static_cast<T>(a), static_cast<T>(b)});
+__device__ __forceinline__ int pack(float a, float b) {
+    using Two = T __attribute__((ext_vector_type(2)));
+    using Floats = float __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(int, __builtin_convertvector(Floats{a, b}, Two));
 }
 
 // A lane's sums of 16 rows of a strip, as they go out: `pieces` of 16 bytes at (row, column of the strip).
@@ -522,12 +523,23 @@ struct Strip {
     }
 };
 
-// A wave's strip of a tile goes out.
+// A wave's strip of a tile goes out, by straight code where it is whole: a branch for each store, and what is rare between them, cost 2 us a tile.
 template <typename T, class S>
 __device__ __forceinline__ void store_strip(T* out, unsigned ldo, unsigned rows, unsigned cols, unsigned row0, unsigned col0, int lane, const float4v (&acc)[S::PB][S::QB]) {
     using Out = Strip<T, S>;
     constexpr int kPer = 16 / sizeof(T);
-    const bool whole = row0 + S::QB * 16 <= rows && col0 + S::PB * 16 <= cols;
+    if (row0 + S::QB * 16 <= rows && col0 + S::PB * 16 <= cols) {
+        T* at = cell(out, row0 + Out::row(0, lane), ldo, col0 + Out::col(0, lane));
+        const size_t next = Out::kNarrow ? ldo : 16, step = size_t{16} * ldo;
+#pragma unroll
+        for (int j = 0; j < S::QB; ++j, at += step) {
+            Out strip;
+            strip.take(acc, j, lane);
+#pragma unroll
+            for (int i = 0; i < Out::kPieces; ++i) __builtin_memcpy(at + i * next, &strip.v[i], 16);
+        }
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < S::QB; ++j) {
         Out strip;
@@ -535,18 +547,15 @@ __device__ __forceinline__ void store_strip(T* out, unsigned ldo, unsigned rows,
 #pragma unroll
         for (int i = 0; i < Out::kPieces; ++i) {
             const unsigned row = row0 + j * 16 + Out::row(i, lane), col = col0 + Out::col(i, lane);
+            if (row >= rows) continue;
             T* const at = cell(out, row, ldo, col);
-            if (whole) {
-                __builtin_memcpy(at, &strip.v[i], 16);
-            } else if (row < rows) {
-                const Pack<T> f = __builtin_bit_cast(Pack<T>, strip.v[i]);
-                if (col + kPer <= cols) {
-                    __builtin_memcpy(at, &f, 16);
-                } else {
+            const Pack<T> f = __builtin_bit_cast(Pack<T>, strip.v[i]);
+            if (col + kPer <= cols) {
+                __builtin_memcpy(at, &f, 16);
+            } else {
 #pragma unroll
-                    for (int e = 0; e < kPer; ++e)
-                        if (col + e < cols) at[e] = f.v[e];
-                }
+                for (int e = 0; e < kPer; ++e)
+                    if (col + e < cols) at[e] = f.v[e];
             }
         }
     }
@@ -1105,7 +1114,7 @@ Choice large_choice(double tiles, double stages) { return {Kind::kLarge, 1, 0, k
 Choice small_choice(double tiles, double stages, size_t w, bool loose) {
     double us;
     if (w == 4) us = std::ceil(tiles / kUnits) * (1.95 * stages + 2);                  // the matrix instructions bound it: two on a compute unit take twice as long
-    else us = std::fmax(1, tiles / (2 * kUnits)) * ((tiles <= kUnits ? 0.62 : tiles <= 2 * kUnits ? 0.72 : 1.05) * stages + 2);
+    else us = std::fmax(1, tiles / (2 * kUnits)) * ((tiles <= kUnits ? 0.62 : tiles <= 2 * kUnits ? 0.72 : 1.2) * stages + 2);
     return {loose ? Kind::kLoose : Kind::kSmall, 1, 0, kLaunchUs + (loose ? (w == 4 ? 1.3 : 1.5) : 1) * us};
 }
 
