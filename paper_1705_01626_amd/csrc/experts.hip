@@ -398,18 +398,29 @@ __device__ __forceinline__ Groups groups_of(const int64_t* offsets, unsigned exp
     return g;
 }
 
+__host__ __device__ inline unsigned parts_of(unsigned tiles) { return (tiles + 7) / 8; }
+
 // dW's tiles: workgroups go to the eight XCDs in turn, and each XCD takes a part of every expert's, since experts differ in what a tile costs.
-// Parts are rounded up; what they have too much is no tile.
+// Parts are rounded up; what they have too much is no tile.  Of the `width` workgroups of an XCD the first `idle` have nothing else to do at the beginning and take `ahead`
+// tiles each before the others take their first.
 struct Parts {
-    unsigned at, items, each, tiles;
+    unsigned xcd, width, mine, idle, ahead, each, tiles, count, turn;     // each: of an expert; count: of all experts
+    __device__ __forceinline__ Parts(unsigned of_expert, unsigned experts, unsigned busy, unsigned ahead_)
+        : xcd(blockIdx.x % 8), width(gridDim.x / 8), ahead(ahead_), each(parts_of(of_expert)), tiles(of_expert), count(each * experts) {
+        const unsigned at = blockIdx.x / 8, first = busy % width;         // (busy: items that the XCD's workgroups have before)
+        idle = width - first;
+        mine = at >= first ? at - first : at + idle;
+        turn = mine < idle ? 0 : ahead;
+    }
     __device__ __forceinline__ unsigned operator()() {
-        while (at < items && at % 8 * each + at / 8 % each >= tiles) at += gridDim.x;
-        const unsigned item = at;
-        at += gridDim.x;
-        return item < items ? item : kNone;
+        while (true) {
+            const unsigned at = turn < ahead ? mine + turn * idle : ahead * idle + mine + (turn - ahead) * width;
+            ++turn;
+            if (at >= count) return kNone;
+            if (xcd * each + at % each < tiles) return at * 8 + xcd;
+        }
     }
 };
-__host__ __device__ inline unsigned parts_of(unsigned tiles) { return (tiles + 7) / 8; }
 
 // One workgroup's view of a tile.
 template <typename T, Does DOES, class S>
@@ -700,9 +711,13 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void gradients_kernel(Exp
     const Groups g = tables<S>(dx.offsets, dx.experts, dx.m, dx.cols, lds);
     // (a lane's number that is had again at any time: no register holds the thread's through both)
     const int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
-    const unsigned first = g.items % gridDim.x, mine = blockIdx.x >= first ? blockIdx.x - first : blockIdx.x + gridDim.x - first;
     work<T, Does::kDx, S>(dx, g, g.items, address(lds), lane, Turns{blockIdx.x, g.items});
-    work<T, Does::kDw, S>(dw, g, dw_tiles, address(lds), lane, Parts{mine, 8 * parts_of(dw_tiles) * dw.experts, parts_of(dw_tiles), dw_tiles});
+    // (a tile's time: its stages, and as much as seven to begin and finish)
+    constexpr unsigned kSteps = Tile<T, Does::kDw, S>::kSteps;
+    const unsigned stages_dx = (dx.length + kSteps - 1) / kSteps + 7, stages_dw = (g.end / dx.experts + kSteps - 1) / kSteps + 7;
+    const unsigned xcd = blockIdx.x % 8, busy = g.items / 8 + (xcd < g.items % 8 ? 1 : 0), width = gridDim.x / 8;
+    const unsigned ahead = busy % width != 0 ? (stages_dx + stages_dw / 2) / stages_dw : 0;
+    work<T, Does::kDw, S>(dw, g, dw_tiles, address(lds), lane, Parts(dw_tiles, dw.experts, busy, ahead));
 }
 
 // ------------------------------------------------------------------ operands that do not take 16-byte accesses
@@ -781,9 +796,8 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void loose_kernel(ExpertA
     LooseOperand<T, Where::kQ, S::QT, S::kWavesAll> in_q;
     in_p.op.init(wave, lane, 0, 0);
     in_q.op.init(wave, lane, 0, 0);
-    const unsigned each = parts_of(dw_tiles);
     Turns turns{blockIdx.x, g.items};
-    Parts parts{blockIdx.x, 8 * each * p.experts, each, dw_tiles};
+    Parts parts(dw_tiles, p.experts, 0, 0);
     const auto next = [&]() { return DOES == Does::kDw ? parts() : turns(); };
     for (unsigned item = next(); item != kNone; item = next()) {
         tile.init(p, g, g.items, item, wave, lane);
@@ -1153,7 +1167,8 @@ Choice choose_dw(size_t m, size_t experts, size_t n, size_t k, size_t w, bool lo
     return cheaper(best, solo_choice(Kind::kSolo64, tiles, static_cast<double>(tiles), stages, 2 * kUnits, w == 4 ? 1.3 : 0.42, w == 4 ? 3.6 : 2.9));
 }
 
-unsigned grid_of(size_t items, unsigned room) { return static_cast<unsigned>(items < room ? items : room); }
+// (as many workgroups on each XCD: `room` is a multiple of 8)
+unsigned grid_of(size_t items, unsigned room) { return static_cast<unsigned>(items < room ? round_up(items, 8) : room); }
 
 template <typename T, class S>
 zvc_status product_of(const ExpertArgs<T>& p, hipStream_t stream) {
