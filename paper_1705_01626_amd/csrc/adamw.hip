@@ -13,13 +13,14 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr unsigned kPiece = 8 * kThreads;              // elements of a workgroup
+constexpr uint64_t kCacheBytes = uint64_t{256} << 20;   // in front of the memory
 constexpr uint64_t kMostPieces = (1u << 24) - 1;       // a dimension of a grid holds fewer than 2^32 lanes
 constexpr uint64_t kMagic = 0x7a76635f6164616dull;
 
 // A plan: this, then the first piece of each tensor and the number of pieces behind the last one (64 entries of filling), then the
 // tensors as the caller described them.
 struct Header {
-    uint64_t magic, tensors, pieces, bytes;
+    uint64_t magic, tensors, pieces, bytes, weights, unused;      // weights: their bytes
 };
 inline size_t starts_bytes(size_t tensors) { return round_up((tensors + 65) * sizeof(unsigned), 16); }
 
@@ -29,6 +30,7 @@ struct Now {
     uint64_t step, seed;
     const uint64_t* d_step;
     const float* d_factors;
+    bool past;                            // weights go past the caches
 };
 
 // beta^t by squaring: the same on the host and on the device.
@@ -73,8 +75,12 @@ __device__ __forceinline__ Codes load_codes(const unsigned char* at, int there, 
     }
     return c;
 }
-__device__ __forceinline__ void store_codes(unsigned char* at, const Codes& c, int there, bool full) {
-    if (full) {
+__device__ __forceinline__ void store_codes(unsigned char* at, const Codes& c, int there, bool full, bool past) {
+    if (full && past) {
+        uint64_t all;
+        __builtin_memcpy(&all, &c, 8);
+        __builtin_nontemporal_store(all, reinterpret_cast<uint64_t*>(at));
+    } else if (full) {
         __builtin_memcpy(at, &c, 8);
     } else {
 #pragma unroll
@@ -117,11 +123,21 @@ __device__ __forceinline__ Codes narrow(const Eight& e, const Words& random, flo
     return c;
 }
 
+// past: past the caches' replacement; `at` is then a multiple of 16 bytes.
+template <typename T>
+__device__ __forceinline__ void store_past(T* at, const Eight& e, int there, bool full, bool past) {
+    if (full && past) store8(at, e, true);
+    else store_some(at, e, there, full);
+}
+
 // Eight neighbouring elements from `i` on, `there` of which exist.
 template <typename P, typename G, bool MASTER, int BITS>
 __device__ __forceinline__ void update(const zvc_adamw_tensor& t, const Now& now, unsigned number, uint64_t i, int there) {
 #pragma clang fp contract(off)
     const bool full = __all(there == 8);
+    // What no one reads before the next step goes past the caches.
+    const auto address = [](const void* at) { return reinterpret_cast<uintptr_t>(at); };
+    const bool past = (address(t.d_m) | address(t.d_v) | address(t.d_master)) % 16 == 0;
     P* const param = static_cast<P*>(t.d_param) + i;
     float* const master = t.d_master + i;
     const Eight grad = load_some(static_cast<const G*>(t.d_grad) + i, there, full);
@@ -146,20 +162,20 @@ __device__ __forceinline__ void update(const zvc_adamw_tensor& t, const Now& now
         m.v[j] = now.beta1 * m.v[j] + now.gain1 * g;
         v.v[j] = now.beta2 * v.v[j] + now.gain2 * (g * g);
         root.v[j] = sqrtf(v.v[j]);
-        p.v[j] = p.v[j] * shrink - now.step_size * (m.v[j] / (root.v[j] * now.root_scale + now.eps));
+        p.v[j] = p.v[j] * shrink - now.step_size * (m.v[j] * __builtin_amdgcn_rcpf(root.v[j] * now.root_scale + now.eps));
     }
-    if constexpr (MASTER) store_some(master, p, there, full);
-    store_some(param, p, there, full);
+    if constexpr (MASTER) store_past(master, p, there, full, past);
+    store_past(param, p, there, full, now.past && address(param) % 16 == 0);
     if constexpr (BITS == 8) {
         const Words random = philox(i / 8 | static_cast<uint64_t>(number) << 32, now.step, now.seed);
         float scale_m, scale_r;
         const Codes cm = narrow<false>(m, random, &scale_m), cr = narrow<true>(root, random, &scale_r);
-        store_codes(static_cast<unsigned char*>(t.d_m) + i, cm, there, full);
-        store_codes(static_cast<unsigned char*>(t.d_v) + i, cr, there, full);
+        store_codes(static_cast<unsigned char*>(t.d_m) + i, cm, there, full, past);
+        store_codes(static_cast<unsigned char*>(t.d_v) + i, cr, there, full, past);
         if (i % ZVC_ADAMW_BLOCK == 0 && there > 0) t.d_m_scale[block] = scale_m, t.d_v_scale[block] = scale_r;
     } else {
-        store_some(static_cast<float*>(t.d_m) + i, m, there, full);
-        store_some(static_cast<float*>(t.d_v) + i, v, there, full);
+        store_past(static_cast<float*>(t.d_m) + i, m, there, full, past);
+        store_past(static_cast<float*>(t.d_v) + i, v, there, full, past);
     }
 }
 
@@ -255,10 +271,11 @@ zvc_status zvc_adamw_plan(const zvc_adamw_tensor* tensors, size_t count, void* p
     if (!aligned_to(plan, 8)) return ZVC_E_ALIGN;
     const size_t need = zvc_adamw_plan_bytes(count);
     if (bytes < need) return ZVC_E_CAPACITY;
-    uint64_t pieces = 0;
+    uint64_t pieces = 0, weights = 0;
     for (size_t i = 0; i < count; ++i) {
         if (zvc_status st = check_tensor(tensors[i])) return st;
         pieces += div_up(tensors[i].count, kPiece);
+        weights += tensors[i].count * type_bytes(tensors[i].type);
     }
     if (pieces > kMostPieces) return ZVC_E_ARG;
     Span* const spans = new (std::nothrow) Span[7 * count + 1];
@@ -284,7 +301,7 @@ zvc_status zvc_adamw_plan(const zvc_adamw_tensor* tensors, size_t count, void* p
     delete[] spans;
     if (bad) return ZVC_E_ARG;
     unsigned char* const out = static_cast<unsigned char*>(plan);
-    const Header header = {kMagic, count, pieces, need};
+    const Header header = {kMagic, count, pieces, need, weights, 0};
     std::memcpy(out, &header, sizeof header);
     unsigned* const starts = reinterpret_cast<unsigned*>(out + sizeof header);
     unsigned at = 0;
@@ -320,6 +337,7 @@ zvc_status zvc_adamw(const void* plan, const void* d_plan, const zvc_adamw_now* 
     n.seed = now->seed, n.d_step = now->d_step, n.d_factors = now->d_factors;
     settle(&n, now->step == 0 ? 1 : now->step, n.rate, static_cast<float>(now->factor));
     n.step = now->step;
+    n.past = header.weights >= kCacheBytes;
     const unsigned char* const at = static_cast<const unsigned char*>(d_plan) + sizeof(Header);
     return launch(adamw_kernel, dim3(static_cast<unsigned>(header.pieces)), kThreads, stream, reinterpret_cast<const unsigned*>(at),
                   reinterpret_cast<const zvc_adamw_tensor*>(at + starts_bytes(header.tensors)), static_cast<unsigned>(header.tensors), n);
