@@ -18,8 +18,8 @@ from typing import Optional, Sequence, Tuple
 
 import torch
 
-from .ffn import TYPES, _on_gpu, _refuse
-from .zvc import ZVC_E_ARG, ZvcError, _check, _stream_handle
+from .ffn import TYPES, _refuse
+from .zvc import _check, _stream_handle
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIBRARY = os.path.join(_PKG, "libzvc_adamw.so")
@@ -166,6 +166,8 @@ def zvc_adamw(plan: Plan, rate: float, step: int, beta1: float = 0.9, beta2: flo
     8-bit states' rounding.  d_step (int64) is added to step, and rate and factor are multiplied by d_factors[0] and [1]
     (float32), when the work runs."""
     where = "zvc_adamw"
+    if plan.device.index != torch.cuda.current_device():
+        _refuse(where, "the plan is on %s, the current device is cuda:%d" % (plan.device, torch.cuda.current_device()))
     now = _Now(rate, beta1, beta2, eps, decay, factor, 0, 0, 0, 0)
     if not 0 <= step < 1 << 64:
         _refuse(where, "step = %r, a number from 1 on expected" % (step,))

@@ -78,7 +78,9 @@ struct RouteArgs {
     bool normalize;
 };
 
-__device__ __forceinline__ float weight_of(float logit, float most) { return logit > kOut ? expf(logit - most) : 0.f; }
+// 16-bit gradients take the shorter exp, which loses |logit - most| x 2^-24 of the result.
+template <typename T = float>
+__device__ __forceinline__ float weight_of(float logit, float most) { return logit > kOut ? (sizeof(T) == 4 ? expf(logit - most) : __expf(logit - most)) : 0.f; }
 
 // Chooses a token's experts: lane s of the 16 gets choice s (-1: none) and its weight.
 template <typename T, int CHUNKS>
@@ -95,13 +97,15 @@ __device__ __forceinline__ void choose(const RouteArgs& p, unsigned token, int l
     *expert = -1;
     for (unsigned s = 0; s < p.top; ++s) {
         const float best = s == 0 ? most : row_max(l.most());
-        int at = 1 << 30;
+        // (columns counted from the lane's first: constants)
+        constexpr int kNone = 1 << 20;
+        int first = kNone;
 #pragma unroll
-        for (int i = l.kAll - 1; i >= 0; --i) at = l.v[i] == best ? l.column(i, lane) : at;
-        at = row_min(at);
+        for (int i = l.kAll - 1; i >= 0; --i) first = l.v[i] == best ? l.column(i, 0) : first;
+        const int at = row_min(first + l.column(0, lane)), taken = at - l.column(0, lane);
         if (static_cast<unsigned>(lane) == s && best > kOut) *expert = at, logit = best;
 #pragma unroll
-        for (int i = 0; i < l.kAll; ++i) l.v[i] = l.column(i, lane) == at ? kOut : l.v[i];
+        for (int i = 0; i < l.kAll; ++i) l.v[i] = l.column(i, 0) == taken ? kOut : l.v[i];
     }
     const float e = weight_of(logit, most);
     if (p.normalize) sum = row_sum(e);
@@ -182,20 +186,34 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs p) {
     }
 }
 
-// A wave an expert: its counts by workgroup become sums of those before, and their total is written behind all counts.
-__global__ __launch_bounds__(64) void route_sums_kernel(RouteArgs p) {
+// A workgroup an expert: its counts by workgroup become sums of those before, and their total is written behind all counts.
+constexpr int kSumThreads = 256;
+__global__ __launch_bounds__(kSumThreads) void route_sums_kernel(RouteArgs p) {
+    constexpr unsigned kEach = 4;
+    __shared__ unsigned room[kSumThreads / 64], total;
     unsigned* const counts = p.counts + static_cast<size_t>(blockIdx.x) * p.blocks;
     unsigned before = 0;
-    for (unsigned at = 0; at < p.blocks; at += 64) {
-        const unsigned b = at + threadIdx.x, own = b < p.blocks ? counts[b] : 0;
-        unsigned x = own;
+    for (unsigned at = 0; at < p.blocks; at += kSumThreads * kEach) {
+        unsigned own[kEach], sum = 0;
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const unsigned other = __shfl_up(x, d);
-            x += static_cast<int>(threadIdx.x) >= d ? other : 0;
+        for (unsigned j = 0; j < kEach; ++j) {
+            const unsigned b = at + threadIdx.x * kEach + j;
+            own[j] = b < p.blocks ? counts[b] : 0;
         }
-        if (b < p.blocks) counts[b] = before + x - own;
-        before += __shfl(x, 63);
+#pragma unroll
+        for (unsigned j = 0; j < kEach; ++j) sum += own[j];
+        const unsigned through = running_sum<kSumThreads>(sum, room);
+        unsigned x = before + through - sum;
+#pragma unroll
+        for (unsigned j = 0; j < kEach; ++j) {
+            const unsigned b = at + threadIdx.x * kEach + j;
+            if (b < p.blocks) counts[b] = x;
+            x += own[j];
+        }
+        if (threadIdx.x == kSumThreads - 1) total = x;
+        __syncthreads();
+        before = total;
+        __syncthreads();
     }
     if (threadIdx.x == 0) p.counts[static_cast<size_t>(p.experts) * p.blocks + blockIdx.x] = before;
 }
@@ -231,7 +249,8 @@ struct RouteBackArgs {
     bool normalize;
 };
 
-// Lane s of a token's 16 has its choice s; every lane has some columns and looks all choices over for each.
+// Lane s of a token's 16 has its choice s.  The row is written as if nothing had been chosen, and then the chosen experts' elements over it, once the
+// row is there.  (Every lane looking all choices over for its columns instead: 16384 x 256 bf16, 8 choices, 8.9.)
 template <typename T, int CHUNKS>
 __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs p) {
     const int lane = threadIdx.x % kRowLanes;
@@ -243,46 +262,41 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs p) {
     const size_t entry = static_cast<size_t>(token) * p.top + lane;
     int expert = mine ? p.chosen[entry] : -1;
     if (expert < 0 || static_cast<unsigned>(expert) >= p.experts) expert = -1;
-    const float logit = expert >= 0 ? static_cast<float>(row[expert]) : kOut;
+    const float given = expert >= 0 ? static_cast<float>(row[expert]) : kOut;
+    const float logit = given > kOut ? given : kOut;
     const float dw = expert >= 0 ? p.dweights[entry] : 0.f;
     using L = Logits<T, CHUNKS>;
     L l;
-    float share;                             // of this lane's choice
-    float most, sum;
+    float most, sum = 0.f;
     if (p.normalize) {
-        const float live = logit > kOut ? logit : kOut;
-        most = row_max(live);
-        share = weight_of(live, most);
-        sum = row_sum(share);
+        most = row_max(logit);
     } else {
         l.load(row, p.experts, lane);
         most = row_max(l.most());
-        sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < L::kAll; ++i) sum += l.v[i] = weight_of(l.v[i], most);
-        sum = row_sum(sum);
-        share = logit > kOut ? weight_of(logit, most) : 0.f;
+        for (int i = 0; i < L::kAll; ++i) sum += l.v[i] = weight_of<T>(l.v[i], most);
     }
+    float share = weight_of<T>(logit, most);                         // of this lane's choice
+    sum = row_sum(p.normalize ? share : sum);
     const float over = sum != 0.f ? 1.f / sum : 0.f;
     share *= over;
     const float mean = row_sum(share != 0.f ? share * dw : 0.f);
-    float grad[L::kAll];
-#pragma unroll
-    for (int i = 0; i < L::kAll; ++i) grad[i] = p.normalize ? 0.f : l.v[i] * over * -mean;
     const float own = p.normalize ? share * (dw - mean) : share * dw;
+    float grad = p.normalize ? 0.f : -share * mean;                  // with what other choices of the same expert add
     const int first = (threadIdx.x & 63) - lane;
     for (unsigned s = 0; s < p.top; ++s) {
         const int of = __shfl(expert, first + s);
         const float g = __shfl(own, first + s);
-#pragma unroll
-        for (int i = 0; i < L::kAll; ++i) grad[i] += L::column(i, lane) == of ? g : 0.f;
+        grad += of == expert ? g : 0.f;
     }
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         const int at = L::column(c * L::kPer, lane);
-        Pack<T> q;
+        Pack<T> q = {};
+        if (!p.normalize) {
 #pragma unroll
-        for (int j = 0; j < L::kPer; ++j) q.v[j] = static_cast<T>(grad[c * L::kPer + j]);
+            for (int j = 0; j < L::kPer; ++j) q.v[j] = static_cast<T>(l.v[c * L::kPer + j] * over * -mean);
+        }
         if (at + L::kPer <= static_cast<int>(p.experts)) {
             __builtin_memcpy(out + at, &q, 16);
         } else {
@@ -291,6 +305,8 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs p) {
                 if (at + j < static_cast<int>(p.experts)) out[at + j] = q.v[j];
         }
     }
+    wait_loads<0>();                                                 // (and stores)
+    if (expert >= 0) out[expert] = static_cast<T>(logit > kOut ? grad : 0.f);
 }
 
 // ------------------------------------------------------------------ the experts' products
@@ -1080,7 +1096,7 @@ zvc_status route_as(const RouteArgs& p, hipStream_t stream) {
         constexpr int kChunks = decltype(chunks)::value;
         if (p.blocks <= 1) return launch(route_kernel<T, kChunks, true>, dim3(1), kRouteThreads, stream, p);
         if (zvc_status st = launch(route_kernel<T, kChunks, false>, dim3(p.blocks), kRouteThreads, stream, p)) return st;
-        if (zvc_status st = launch(route_sums_kernel, dim3(p.experts), 64, stream, p)) return st;
+        if (zvc_status st = launch(route_sums_kernel, dim3(p.experts), kSumThreads, stream, p)) return st;
         return launch(route_places_kernel, dim3(p.blocks), kRouteThreads, stream, p);
     });
 }
@@ -1134,6 +1150,7 @@ Choice small_choice(double tiles, double stages, size_t w, bool loose) {
 
 // Parts of a small kernel's sums where its tiles do not fill the compute units.  most: tiles at most.
 Choice solo_choice(Kind kind, size_t most, double tiles, size_t stages, size_t slots, double stage_us, double item_us) {
+    if (most > size_t{1} << 20) return {kind, 1, 0, HUGE_VAL};      // (a dimension of a grid holds fewer than 2^32 lanes)
     const size_t rows = kind == Kind::kSolo16 ? 16 : 64;
     size_t parts = tiles < 1 ? 1 : static_cast<size_t>(2 * kUnits / tiles);
     if (parts > stages / (2 * kSoloWaves)) parts = stages / (2 * kSoloWaves);

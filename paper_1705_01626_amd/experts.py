@@ -18,8 +18,8 @@ from typing import Optional, Tuple
 
 import torch
 
-from .ffn import TYPES, _matrix, _on_gpu, _refuse, _room, _type
-from .zvc import _check, _stream_handle
+from .ffn import TYPES, _matrix, _refuse, _room, _type
+from .zvc import _check, _current_device, _stream_handle
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIBRARY = os.path.join(_PKG, "libzvc_experts.so")
@@ -93,15 +93,23 @@ def _stack(t: torch.Tensor, experts: int, n: int, k: int, like: torch.Tensor, wh
     return row, between if experts > 1 and n and k else n * row
 
 
-def _plain(t: torch.Tensor, shape: tuple, dtype: torch.dtype, like: torch.Tensor, where: str, name: str) -> int:
+def _plain(t: torch.Tensor, shape: tuple, dtype: torch.dtype, device: int, where: str, name: str) -> int:
     """The address of a contiguous tensor."""
+    # (what nearly every call has, with few of the attribute lookups that a call's host time goes to)
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
     if tuple(t.shape) != shape or t.dtype != dtype:
         _refuse(where, "%s is %s %s, %s %s expected" % (name, t.dtype, tuple(t.shape), dtype, shape))
-    if t.get_device() != like.get_device():
-        _refuse(where, "%s is on %s, the first tensor is on %s" % (name, t.device, like.device))
-    if not t.is_contiguous():
-        _refuse(where, "%s has strides %s: it has to be contiguous" % (name, t.stride()))
-    return t.data_ptr()
+    if t.get_device() != device:
+        _refuse(where, "%s is on %s, the first tensor is on another device" % (name, t.device))
+    _refuse(where, "%s has strides %s: it has to be contiguous" % (name, t.stride()))
+
+
+def _here(where: str, device: int, ws: Optional[torch.Tensor] = None) -> None:
+    if device < 0 or (ws is not None and ws.get_device() != device):
+        _refuse(where, "the tensors and the workspace have to be on one GPU")
+    if device != (torch.cuda.current_device() if _current_device is None else _current_device()):
+        _refuse(where, "the tensors are on cuda:%d, the current device is cuda:%d" % (device, torch.cuda.current_device()))
 
 
 # ---- the router -------------------------------------------------------------------
@@ -125,11 +133,12 @@ def zvc_route(logits: torch.Tensor, chosen: torch.Tensor, weights: torch.Tensor,
         _refuse(where, "logits and chosen have to be 2-D")
     (m, experts), top = logits.shape, chosen.shape[1]
     ldl = _matrix(logits, m, experts, logits, where, "logits")
-    at = [_plain(chosen, (m, top), torch.int32, logits, where, "chosen"), _plain(weights, (m, top), torch.float32, logits, where, "weights"),
-          _plain(offsets, (experts + 1,), torch.int64, logits, where, "offsets"),
-          _plain(order, (m * top,), torch.int64, logits, where, "order"), _plain(place, (m, top), torch.int64, logits, where, "place")]
+    device, entries = logits.get_device(), (m, top)
+    at = (_plain(chosen, entries, torch.int32, device, where, "chosen"), _plain(weights, entries, torch.float32, device, where, "weights"),
+          _plain(offsets, (experts + 1,), torch.int64, device, where, "offsets"),
+          _plain(order, (m * top,), torch.int64, device, where, "order"), _plain(place, entries, torch.int64, device, where, "place"))
     room = _room(ws, where)
-    _on_gpu(where, logits, ws)
+    _here(where, device, ws)
     _check(_native().zvc_route(logits.data_ptr(), ldl, *at, m, experts, top, code, int(normalize), ws.data_ptr(), room,
                                _stream_handle(stream)), where)
 
@@ -144,9 +153,10 @@ def zvc_route_backward(dweights: torch.Tensor, logits: torch.Tensor, chosen: tor
     (m, experts), top = logits.shape, chosen.shape[1]
     ldl = _matrix(logits, m, experts, logits, where, "logits")
     ldd = _matrix(dlogits, m, experts, logits, where, "dlogits")
-    dw = _plain(dweights, (m, top), torch.float32, logits, where, "dweights")
-    at = _plain(chosen, (m, top), torch.int32, logits, where, "chosen")
-    _on_gpu(where, logits)
+    device = logits.get_device()
+    dw = _plain(dweights, (m, top), torch.float32, device, where, "dweights")
+    at = _plain(chosen, (m, top), torch.int32, device, where, "chosen")
+    _here(where, device)
     _check(_native().zvc_route_backward(dw, logits.data_ptr(), ldl, at, dlogits.data_ptr(), ldd, m, experts, top, code, int(normalize),
                                         _stream_handle(stream)), where)
 
@@ -174,9 +184,10 @@ def zvc_expert_product(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, 
     ldx = _matrix(x, m, k, x, where, "x")
     ldw, sw = _stack(w, experts, n, k, x, where, "w")
     ldy = _matrix(y, m, n, x, where, "y")
-    at = _plain(offsets, (experts + 1,), torch.int64, x, where, "offsets")
+    device = x.get_device()
+    at = _plain(offsets, (experts + 1,), torch.int64, device, where, "offsets")
     room = _room(ws, where)
-    _on_gpu(where, x, ws)
+    _here(where, device, ws)
     _check(_native().zvc_expert_product(x.data_ptr(), ldx, w.data_ptr(), ldw, sw, at, y.data_ptr(), ldy, m, experts, n, k, code,
                                         ws.data_ptr(), room, _stream_handle(stream)), where)
 
@@ -194,9 +205,10 @@ def zvc_expert_gradients(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, off
     lddy = _matrix(dy, m, n, x, where, "dy")
     lddx = k if dx is None else _matrix(dx, m, k, x, where, "dx")
     lddw, sdw = (k, n * k) if dw is None else _stack(dw, experts, n, k, x, where, "dw")
-    at = _plain(offsets, (experts + 1,), torch.int64, x, where, "offsets")
+    device = x.get_device()
+    at = _plain(offsets, (experts + 1,), torch.int64, device, where, "offsets")
     room = _room(ws, where)
-    _on_gpu(where, x, ws)
+    _here(where, device, ws)
     _check(_native().zvc_expert_gradients(dy.data_ptr(), lddy, x.data_ptr(), ldx, w.data_ptr(), ldw, sw, at,
                                           0 if dx is None else dx.data_ptr(), lddx, 0 if dw is None else dw.data_ptr(), lddw, sdw, m,
                                           experts, n, k, code, ws.data_ptr(), room, _stream_handle(stream)), where)
