@@ -27,7 +27,7 @@ extern "C" {
 /* The most experts, choices of a token, and choices of all tokens (m * top). */
 #define ZVC_EXPERTS_MAX 1024
 #define ZVC_EXPERTS_MAX_TOP 16
-#define ZVC_EXPERTS_MAX_ENTRIES ((size_t)1 << 28)
+#define ZVC_EXPERTS_MAX_ENTRIES ((size_t)1 << 27)
 
 /* Bytes of device workspace that zvc_route needs (256-byte aligned, no initialisation).  0 for a bad size. */
 size_t zvc_route_workspace_bytes(size_t m, size_t experts, size_t top);

@@ -714,7 +714,7 @@ __device__ __forceinline__ Groups tables(const int64_t* offsets, unsigned expert
 __device__ __forceinline__ unsigned address(unsigned char* lds) { return static_cast<unsigned>(reinterpret_cast<uintptr_t>((LdsByte*)lds)); }
 
 template <typename T, class S>
-__global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(ExpertArgs<T> p) {
+__global__ __launch_bounds__(S::kThreads, S::kPerUnit) void expert_product_kernel(ExpertArgs<T> p) {
     unsigned char* const lds = room_of<S>();
     const Groups g = tables<S>(p.offsets, p.experts, p.m, p.cols, lds);
     work<T, Does::kForward, S>(p, g, g.items, address(lds), threadIdx.x & 63, Turns{blockIdx.x, g.items});
@@ -722,7 +722,7 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void product_kernel(Exper
 
 // dx, and behind it dW, in one go: either alone leaves compute units idle in its last round.  dw_tiles: of one expert; it, and dx.cols, may be 0.
 template <typename T, class S>
-__global__ __launch_bounds__(S::kThreads, S::kPerUnit) void gradients_kernel(ExpertArgs<T> dx, ExpertArgs<T> dw, unsigned dw_tiles) {
+__global__ __launch_bounds__(S::kThreads, S::kPerUnit) void expert_gradients_kernel(ExpertArgs<T> dx, ExpertArgs<T> dw, unsigned dw_tiles) {
     unsigned char* const lds = room_of<S>();
     const Groups g = tables<S>(dx.offsets, dx.experts, dx.m, dx.cols, lds);
     // (a lane's number that is had again at any time: no register holds the thread's through both)
@@ -1190,14 +1190,14 @@ unsigned grid_of(size_t items, unsigned room) { return static_cast<unsigned>(ite
 template <typename T, class S>
 zvc_status product_of(const ExpertArgs<T>& p, hipStream_t stream) {
     const size_t items = row_tiles(p.m, p.experts, S::QT) * div_up(p.cols, S::PT);
-    return launch(product_kernel<T, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, p);
+    return launch(expert_product_kernel<T, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, p);
 }
 
 template <typename T, class S>
 zvc_status gradients_of(const ExpertArgs<T>& dx, const ExpertArgs<T>& dw, hipStream_t stream) {
     const size_t dw_tiles = div_up(dw.cols, S::PT) * div_up(dw.rows, S::QT);
     const size_t items = row_tiles(dx.m, dx.experts, S::QT) * div_up(dx.cols, S::PT) + dw_tiles * dw.experts;
-    return launch(gradients_kernel<T, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, dx, dw, static_cast<unsigned>(dw_tiles));
+    return launch(expert_gradients_kernel<T, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, dx, dw, static_cast<unsigned>(dw_tiles));
 }
 
 template <typename T, Does DOES>
