@@ -438,13 +438,16 @@ struct Parts {
     }
 };
 
-// One workgroup's view of a tile.
-template <typename T, Does DOES, class S>
+// One workgroup's view of a tile.  OF: tiles of which this is a quarter, or S.
+template <typename T, Does DOES, class S, class OF = S>
 struct Tile {
     static constexpr Lies kP = DOES == Does::kForward ? Lies::kAlong : Lies::kAcross, kQ = DOES == Does::kDw ? Lies::kAcross : Lies::kAlong;
     static constexpr int W = sizeof(T), kSteps = kStageBytes / W;
     using InP = Operand<T, kP, S::PT, S::kWavesAll, false>;
     using InQ = Operand<T, kQ, S::QT, S::kWavesAll, false>;
+
+    static constexpr bool kQuarter = !std::is_same_v<S, OF>;
+    static_assert(!kQuarter || (OF::PT == 2 * S::PT && OF::QT == 2 * S::QT), "quarters");
 
     unsigned col0, row0, end;            // of the output; the first row that is not the tile's expert's
     unsigned length, stages;
@@ -457,11 +460,12 @@ struct Tile {
     __device__ __forceinline__ void locate(unsigned at, unsigned tp, unsigned tq) {
         constexpr unsigned kBand = DOES == Does::kForward ? 8 : 4;
         const unsigned band = at / (kBand * tp), in_band = at % (kBand * tp), height = tq - band * kBand < kBand ? tq - band * kBand : kBand;
-        col0 = in_band / height * S::PT;
-        row0 = (band * kBand + in_band % height) * S::QT;
+        col0 = in_band / height * OF::PT;
+        row0 = (band * kBand + in_band % height) * OF::QT;
     }
-    __device__ __forceinline__ void init(const ExpertArgs<T>& a, const Groups& g, unsigned items, unsigned item, int wave, int lane) {
-        const unsigned tp = (a.cols + S::PT - 1) / S::PT;
+    // from: the tile that the first four quarters are of.
+    __device__ __forceinline__ void init(const ExpertArgs<T>& a, const Groups& g, unsigned items, unsigned from, unsigned item, int wave, int lane) {
+        const unsigned tp = (a.cols + OF::PT - 1) / OF::PT;
         unsigned e;
         if constexpr (DOES == Does::kDw) {
             const unsigned tq = (a.rows + S::QT - 1) / S::QT, each = parts_of(tp * tq);
@@ -474,13 +478,17 @@ struct Tile {
             q = cell(a.q, begin, a.ldq, row0);
             out = a.out + e * a.so;
         } else {
-            const unsigned at = place_of(item, items);
+            const unsigned place = place_of(item, items), at = kQuarter ? from + place / 4 : place;
             e = g.expert_of(at, lane);
             const unsigned begin = __builtin_amdgcn_readfirstlane(g.start(e));
             end = __builtin_amdgcn_readfirstlane(g.start(e + 1));
-            locate(at - __builtin_amdgcn_readfirstlane(g.firsts[e]), tp, (end - begin + S::QT - 1) / S::QT);
+            locate(at - __builtin_amdgcn_readfirstlane(g.firsts[e]), tp, (end - begin + OF::QT - 1) / OF::QT);
             row0 += begin;
             length = a.length;
+            if constexpr (kQuarter) {
+                col0 += place % 2 * S::PT, row0 += place / 2 % 2 * S::QT;
+                if (col0 >= a.cols || row0 >= end) length = 0, col0 = min(col0, a.cols), row0 = min(row0, end);       // (nothing)
+            }
             p = a.p + e * a.sp;
             p = DOES == Does::kForward ? cell(p, col0, a.ldp, 0) : p + col0;
             q = cell(a.q, row0, a.ldq, 0);
@@ -644,10 +652,13 @@ struct Multiplier {
     }
 };
 
+using Large = Shape<4, 2, 4, 8, 2>;             // 256 x 256, eight waves
+using Quarter = Shape<2, 4, 4, 2, 4>;           // 128 x 128, eight waves, four stages in the same room
+
 // Workgroups take tiles until there are none left; the next tile's first stages are on their way while a tile is finished.
-template <typename T, Does DOES, class S, typename Next>
-__device__ __forceinline__ void work(const ExpertArgs<T>& p, const Groups& groups, unsigned items, unsigned base, int lane, Next next) {
-    using Where = Tile<T, DOES, S>;
+template <typename T, Does DOES, class S, class OF = S, typename Next>
+__device__ __forceinline__ void work(const ExpertArgs<T>& p, const Groups& groups, unsigned items, unsigned base, int lane, Next next, unsigned from = 0) {
+    using Where = Tile<T, DOES, S, OF>;
     constexpr int kRing = S::kRing;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wp = wave % S::WP, wq = wave / S::WP;
@@ -655,7 +666,7 @@ __device__ __forceinline__ void work(const ExpertArgs<T>& p, const Groups& group
     x.init(base, wp, wq, lane);
     Where tile;
     const auto begin = [&](unsigned item) {
-        tile.init(p, groups, items, item, wave, lane);
+        tile.init(p, groups, items, from, item, wave, lane);
 #pragma unroll
         for (unsigned i = 0; i < kRing; ++i)
             if (i < tile.stages) tile.fetch(p, i, base + i * S::kStage);
@@ -713,11 +724,20 @@ __device__ __forceinline__ Groups tables(const int64_t* offsets, unsigned expert
 }
 __device__ __forceinline__ unsigned address(unsigned char* lds) { return static_cast<unsigned>(reinterpret_cast<uintptr_t>((LdsByte*)lds)); }
 
+// Large tiles that do not fill a round go in quarters, with a deeper ring, where those are two rounds or less: one of large tiles takes 57 with a sum over 2048,
+// one of quarters some 20 (16 x 512 rows, 5632 x 2048, 3.4 rounds: 229.6 without, 217).
 template <typename T, class S>
 __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void expert_product_kernel(ExpertArgs<T> p) {
     unsigned char* const lds = room_of<S>();
     const Groups g = tables<S>(p.offsets, p.experts, p.m, p.cols, lds);
-    work<T, Does::kForward, S>(p, g, g.items, address(lds), threadIdx.x & 63, Turns{blockIdx.x, g.items});
+    const int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
+    if constexpr (std::is_same_v<S, Large>) {
+        const unsigned over = g.items % gridDim.x, rest = 2 * over <= gridDim.x ? over : 0, whole = g.items - rest;
+        work<T, Does::kForward, S>(p, g, whole, address(lds), lane, Turns{blockIdx.x, whole});
+        work<T, Does::kForward, Quarter, Large>(p, g, 4 * rest, address(lds), lane, Turns{blockIdx.x, 4 * rest}, whole);
+    } else {
+        work<T, Does::kForward, S>(p, g, g.items, address(lds), lane, Turns{blockIdx.x, g.items});
+    }
 }
 
 // dx, and behind it dW, in one go: either alone leaves compute units idle in its last round.  dw_tiles: of one expert; it, and dx.cols, may be 0.
@@ -816,7 +836,7 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void loose_kernel(ExpertA
     Parts parts(dw_tiles, p.experts, 0, 0);
     const auto next = [&]() { return DOES == Does::kDw ? parts() : turns(); };
     for (unsigned item = next(); item != kNone; item = next()) {
-        tile.init(p, g, g.items, item, wave, lane);
+        tile.init(p, g, g.items, 0, item, wave, lane);
         const int side_p = min(static_cast<int>(p.cols - tile.col0), S::PT), side_q = min(static_cast<int>(tile.end - tile.row0), S::QT);
         const bool short_p = (DOES == Does::kForward ? p.length : p.cols) * sizeof(T) < 16;
         const bool short_q = (DOES == Does::kDw ? p.rows : p.length) * sizeof(T) < 16;
@@ -1108,7 +1128,6 @@ zvc_status route_backward_as(const RouteBackArgs& p, hipStream_t stream) {
     });
 }
 
-using Large = Shape<4, 2, 4, 8, 2>;             // 256 x 256, eight waves
 using Eights = Shape<2, 4, 4, 2, 2>;            // 128 x 128, eight waves
 using Small = Shape<2, 2, 4, 4, 2>;             // 128 x 128, four waves
 
@@ -1133,13 +1152,18 @@ double expected_tiles(size_t m, size_t experts, size_t tile) {
 // The account that chooses, in us: tiles in rounds of those that run at a time, each its stages and something to begin and finish.  Fitted to calls
 // with every kernel forced in turn (m rows evenly over E experts, n, k; weights from memory), L large, S small tiles, s16 and s64 the small kernels:
 //   bf16 forward  8 x 32, 2048, 2048: S 25.6, s16 18.3, s64 25.5    8 x 128, 2048, 2048: S 27.3, s16 34.9, s64 24.6    64 x 64, 2048, 128: S 14.2, s16 35.5, s64 38.1
-//                 2 x 256, 512, 2048: S 24.0, s16 9.4, s64 13.1     16 x 512, 1024, 1024: L 30.7, S 29.4, s64 40.0     16 x 512, 5632, 2048: L 229, S 251
+//                 2 x 256, 512, 2048: S 24.0, s16 9.4, s64 13.1     16 x 512, 1024, 1024: L 30.7, S 29.4, s64 40.0     16 x 512, 5632, 2048: L 217, S 251
 //   fp32 forward  8 x 32, 2048, 2048: S 132, s16 43.6, s64 81.9     8 x 128, 2048, 2048: S 136, s16 109, s64 131       16 x 512, 1024, 1024: S 188, s16 195, s64 181
 //   dW            bf16 5 x 600, 1024, 512: S 17.2, s64 14.4         bf16 8 x 128, 2048, 2048: S 26.3, s64 69.6         fp32 5 x 600, 1024, 512: S 80.2, s64 47.6
 //   (tiles of 256 x 32 and small kernels with a tile for each wave were slower than these or the same everywhere)
 constexpr double kLaunchUs = 5, kJoinUs = 3, kSumsPerUs = 3e6;
 
-Choice large_choice(double tiles, double stages) { return {Kind::kLarge, 1, 0, kLaunchUs + std::ceil(tiles / kUnits) * (1.45 * stages + 10)}; }
+// (a part of a round of large tiles goes in quarters, see expert_product_kernel)
+Choice large_choice(double tiles, double stages, bool quarters) {
+    const double whole = std::floor(tiles / kUnits), part = tiles / kUnits - whole;
+    const double rounds = whole + (part == 0 ? 0 : quarters && part <= 0.5 ? 0.4 * std::ceil(4 * part) : 1);
+    return {Kind::kLarge, 1, 0, kLaunchUs + rounds * (1.45 * stages + 10)};
+}
 
 Choice small_choice(double tiles, double stages, size_t w, bool loose) {
     double us;
@@ -1163,11 +1187,11 @@ Choice solo_choice(Kind kind, size_t most, double tiles, size_t stages, size_t s
 
 Choice cheaper(const Choice& a, const Choice& b) { return b.cost < a.cost ? b : a; }
 
-// Of y or dx: `cols` columns, sums over `length`.
-Choice choose_rows(size_t m, size_t experts, size_t cols, size_t length, size_t w, bool loose) {
+// Of y (forward) or dx: `cols` columns, sums over `length`.
+Choice choose_rows(size_t m, size_t experts, size_t cols, size_t length, size_t w, bool loose, bool forward) {
     const size_t stages = div_up(length, kStageBytes / w), across = div_up(cols, kSoloCols);
     Choice best = small_choice(expected_tiles(m, experts, 128) * div_up(cols, 128), stages, w, loose);
-    if (w == 2 && !loose) best = cheaper(best, large_choice(expected_tiles(m, experts, 256) * div_up(cols, 256), stages));
+    if (w == 2 && !loose) best = cheaper(best, large_choice(expected_tiles(m, experts, 256) * div_up(cols, 256), stages, forward));
     best = cheaper(best, solo_choice(Kind::kSolo16, row_tiles(m, experts, 16) * across, expected_tiles(m, experts, 16) * across, stages, 4 * kUnits,
                                      w == 4 ? 0.65 : 0.3, w == 4 ? 4.1 : 2.8));
     return cheaper(best, solo_choice(Kind::kSolo64, row_tiles(m, experts, 64) * across, expected_tiles(m, experts, 64) * across, stages, 2 * kUnits,
@@ -1180,7 +1204,7 @@ Choice choose_dw(size_t m, size_t experts, size_t n, size_t k, size_t w, bool lo
     const double longest = experts > 1 ? 3.0 * stages : stages;
     Choice best = small_choice(static_cast<double>(div_up(n, 128) * div_up(k, 128) * experts), stages, w, loose);
     best.cost = std::fmax(best.cost, kLaunchUs + longest * (w == 4 ? 1.95 : 0.72) * (loose ? 1.4 : 1));
-    if (w == 2 && !loose) best = cheaper(best, large_choice(static_cast<double>(div_up(n, 256) * div_up(k, 256) * experts), stages));
+    if (w == 2 && !loose) best = cheaper(best, large_choice(static_cast<double>(div_up(n, 256) * div_up(k, 256) * experts), stages, false));
     return cheaper(best, solo_choice(Kind::kSolo64, tiles, static_cast<double>(tiles), stages, 2 * kUnits, w == 4 ? 1.3 : 0.42, w == 4 ? 3.6 : 2.9));
 }
 
@@ -1190,7 +1214,7 @@ unsigned grid_of(size_t items, unsigned room) { return static_cast<unsigned>(ite
 template <typename T, class S>
 zvc_status product_of(const ExpertArgs<T>& p, hipStream_t stream) {
     const size_t items = row_tiles(p.m, p.experts, S::QT) * div_up(p.cols, S::PT);
-    return launch(expert_product_kernel<T, S>, dim3(grid_of(items, kUnits * S::kPerUnit)), S::kThreads, stream, p);
+    return launch(expert_product_kernel<T, S>, dim3(grid_of(std::is_same_v<S, Large> ? 4 * items : items, kUnits * S::kPerUnit)), S::kThreads, stream, p);
 }
 
 template <typename T, class S>
@@ -1230,7 +1254,7 @@ bool takes_16(const T* at, size_t ld, size_t stride) { return aligned_to(at, 16)
 template <typename T>
 zvc_status forward_as(const ExpertArgs<T>& p, float* sums, hipStream_t stream) {
     const bool loose = !takes_16(p.p, p.ldp, p.sp) || !takes_16(p.q, p.ldq, 0) || p.length * sizeof(T) % 16 != 0;
-    const Choice choice = choose_rows(p.m, p.experts, p.cols, p.length, sizeof(T), loose);
+    const Choice choice = choose_rows(p.m, p.experts, p.cols, p.length, sizeof(T), loose, true);
     if (choice.kind == Kind::kSolo16) return solo_of<T, Does::kForward, 1>(p, choice, loose, sums, stream);
     if (choice.kind == Kind::kSolo64) return solo_of<T, Does::kForward, 4>(p, choice, loose, sums, stream);
     if (choice.kind == Kind::kLoose) return loose_of<T, Does::kForward>(p, stream);
@@ -1243,7 +1267,7 @@ template <typename T>
 zvc_status backward_as(ExpertArgs<T> dx, ExpertArgs<T> dw, float* sums, hipStream_t stream) {
     const bool loose_dx = !takes_16(dx.p, dx.ldp, dx.sp) || !takes_16(dx.q, dx.ldq, 0) || dx.length * sizeof(T) % 16 != 0;
     const bool loose_dw = !takes_16(dw.p, dw.ldp, 0) || !takes_16(dw.q, dw.ldq, 0);
-    const Choice of_dx = choose_rows(dx.m, dx.experts, dx.cols, dx.length, sizeof(T), loose_dx);
+    const Choice of_dx = choose_rows(dx.m, dx.experts, dx.cols, dx.length, sizeof(T), loose_dx, false);
     const Choice of_dw = choose_dw(dw.m, dw.experts, dw.rows, dw.cols, sizeof(T), loose_dw);
     const auto tiles = [](const Choice& c) { return c.kind == Kind::kLarge || c.kind == Kind::kSmall; };
     if (dx.cols != 0 && !tiles(of_dx)) {
@@ -1347,8 +1371,8 @@ size_t zvc_expert_workspace_bytes(size_t m, size_t experts, size_t n, size_t k, 
     size_t sums = 0;
     for (const bool loose : {false, true}) {
         const auto most = [&](const Choice& c) { sums = c.sums > sums ? c.sums : sums; };
-        if (backward == 0) most(choose_rows(m, experts, n, k, w, loose));
-        else most(choose_rows(m, experts, k, n, w, loose)), most(choose_dw(m, experts, n, k, w, loose));
+        if (backward == 0) most(choose_rows(m, experts, n, k, w, loose, true));
+        else most(choose_rows(m, experts, k, n, w, loose, false)), most(choose_dw(m, experts, n, k, w, loose));
     }
     return 256 + round_up(sums, 256);
 }
