@@ -99,6 +99,7 @@ class Plan:
     def __init__(self, tensors, host, device_bytes):
         self.tensors, self.host, self.device_bytes = tensors, host, device_bytes
         self.device = device_bytes.device
+        self.streams = {_stream_handle(None)}       # that device_bytes are known to be read on
 
 
 def _flat(t: torch.Tensor, count: int, types, device, where: str, name: str) -> int:
@@ -116,7 +117,9 @@ def _flat(t: torch.Tensor, count: int, types, device, where: str, name: str) -> 
 
 def new_plan(tensors: Sequence[tuple], decay: Optional[Sequence[bool]] = None) -> Plan:
     """A plan for a step over tensors, each (param, grad, state, master): state from new_adamw_state(), master
-    a float32 tensor with the weights of a 16-bit param, or None.  decay: for each, whether weight decay applies (default: to all)."""
+    a float32 tensor with the weights of a 16-bit param, or None.  decay: for each, whether weight decay applies (default: to all).
+    The plan holds addresses: gradients are written into these tensors (a new tensor in `.grad` is not seen), none is resized, and a
+    captured graph with a step of it needs the plan for as long as it is replayed."""
     where = "new_plan"
     tensors = [tuple(t) for t in tensors]
     if not tensors:
@@ -181,5 +184,8 @@ def zvc_adamw(plan: Plan, rate: float, step: int, beta1: float = 0.9, beta2: flo
                 or not d_factors.is_contiguous()):
             _refuse(where, "d_factors has to be two contiguous floats on the plan's device")
         now.d_factors = d_factors.data_ptr()
-    _check(_native().zvc_adamw(plan.host.data_ptr(), plan.device_bytes.data_ptr(), ctypes.addressof(now),
-                               _stream_handle(stream)), where)
+    handle = _stream_handle(stream)
+    if handle not in plan.streams:          # its memory may not go to another tensor before this stream has read it
+        plan.device_bytes.record_stream(torch.cuda.current_stream() if stream is None else stream)
+        plan.streams.add(handle)
+    _check(_native().zvc_adamw(plan.host.data_ptr(), plan.device_bytes.data_ptr(), ctypes.addressof(now), handle), where)

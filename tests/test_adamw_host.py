@@ -4,6 +4,7 @@ import ctypes
 import math
 import os
 import re
+import sys
 
 import numpy as np
 import pytest
@@ -142,6 +143,14 @@ def test_python_refuses():
 
 
 # ---- the reference ------------------------------------------------------------------
+def test_calls_through_ctypes_give_the_same(lib, monkeypatch):
+    want = adamw._native().zvc_adamw(0, 0, 0, 0)
+    monkeypatch.setattr(adamw, "_calls", None)
+    monkeypatch.setitem(sys.modules, "paper_1705_01626_amd._calls", None)
+    with pytest.warns(RuntimeWarning, match="ctypes"):
+        assert adamw._native().zvc_adamw(0, 0, 0, 0) == want == zvc.ZVC_E_ARG
+
+
 def test_numbers_of_the_codes():
     """As torch reads e4m3."""
     want = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()

@@ -160,6 +160,15 @@ def test_strides_of_a_stack():
     assert experts._stack(far, 3, 1, 8, far, "call", "w") == (8, 64)
 
 
+def test_calls_through_ctypes_give_the_same(lib, monkeypatch):
+    bad = [0] * 12
+    want = experts._native().zvc_route_backward(*bad)
+    monkeypatch.setattr(experts, "_calls", None)
+    monkeypatch.setitem(sys.modules, "paper_1705_01626_amd._calls", None)
+    with pytest.warns(RuntimeWarning, match="ctypes"):
+        assert experts._native().zvc_route_backward(*bad) == want == zvc.ZVC_E_ARG
+
+
 # ---- which kernels, and their workspace ------------------------------------------------
 def aligned(x):
     return (x + 7) // 8 * 8

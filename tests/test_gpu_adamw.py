@@ -214,6 +214,25 @@ def test_streams_and_a_plan_that_outlives_its_tensors_names():
     assert plan.tensors[0][0] is tensors[0][0]
 
 
+def test_a_plan_that_is_dropped_before_its_step_has_run():
+    """Its memory goes to no other tensor while a step on another stream has still to read it."""
+    gen = generator("dropped")
+    tensors = [make(5000, KINDS[3], 8, 0, gen)]
+    old = snapshot(tensors)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    plan = adamw.new_plan(tensors)
+    at, size = plan.device_bytes.data_ptr(), plan.device_bytes.numel()
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(200_000_000)
+    adamw.zvc_adamw(plan, step=1, seed=1, stream=stream, **HYPER)
+    del plan
+    others = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(50)]
+    assert not stream.query() and at not in [t.data_ptr() for t in others]
+    stream.synchronize()
+    check(tensors, old, 1, 1)
+
+
 def test_a_large_tensor():
     """More elements than 2^31 bytes of them; the last ones against the definition."""
     count = (1 << 30) + 1000

@@ -183,6 +183,14 @@ def test_products(size, dtype):
             run_products(*size, dtype, how, loose)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("how", ["even", "all", "some", "wild"])
+@pytest.mark.parametrize("size", [(6165, 3, 2469, 416), (3884, 3, 3749, 496), (5424, 4, 2797, 456)])
+def test_a_part_of_a_round_of_large_tiles(size, how, dtype):
+    """Even: 270 and 264 tiles of 256 x 256 for 256 workgroups, the last ones in quarters, at a ragged right and lower edge."""
+    run_products(*size, dtype, how, 0)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("n,k", [(1, 1), (3, 5), (8, 8), (15, 17), (64, 64), (65, 33), (129, 250)])
 @pytest.mark.parametrize("m,e", [(1, 1), (1, 5), (2, 1), (17, 3), (64, 64), (65, 1024), (130, 2), (513, 5)])
@@ -299,3 +307,37 @@ def test_tensors_elsewhere_are_refused():
     x = torch.zeros(4, 8, device=DEV)
     with pytest.raises(zvc.ZvcError, match="device|one GPU"):
         experts.zvc_expert_product(x, torch.zeros(2, 8, 8, device=DEV), torch.zeros(3, dtype=torch.int64), x.clone(), torch.empty(256, dtype=torch.uint8, device=DEV))
+
+
+def test_two_calls_at_once():
+    """On streams of their own, with workspaces of their own, both of kernels that split their sums; and a router beside them."""
+    m, e, n, k = 40, 8, 256, 4096
+    gen = generator("at once")
+    sets = []
+    for _ in range(2):
+        x, dy, w = draw(m, k, torch.bfloat16, gen), draw(m, n, torch.bfloat16, gen), stack(e, n, k, torch.bfloat16, gen, k ** -0.5, k)
+        off = torch.tensor(offsets_of(m, e, "all", gen), dtype=torch.int64, device=DEV)
+        logits = draw(3000, 65, torch.float32, gen)
+        sets.append((x, dy, w, off, logits, experts.new_expert_workspace(x, w, backward=True), experts.new_route_workspace(logits, 4)))
+
+    def run(s, stream):
+        x, dy, w, off, logits, ws, rws = s
+        new = lambda *shape, dtype=torch.bfloat16: torch.zeros(shape, dtype=dtype, device=DEV)
+        with torch.cuda.stream(stream):
+            y, dx, dw = new(m, n), new(m, k), new(e, n, k)
+            chosen, weights, offsets, order, place = (new(3000, 4, dtype=torch.int32), new(3000, 4, dtype=torch.float32), new(66, dtype=torch.int64),
+                                                      new(12000, dtype=torch.int64), new(3000, 4, dtype=torch.int64))
+            for _ in range(20):
+                experts.zvc_expert_product(x, w, off, y, ws)
+                experts.zvc_expert_gradients(dy, x, w, off, dx, dw, ws)
+                experts.zvc_route(logits, chosen, weights, offsets, order, place, rws)
+        return y, dx, dw, chosen, weights, offsets, order, place
+
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    together = [run(s, stream) for s, stream in zip(sets, streams)]
+    torch.cuda.synchronize()
+    for s, got in zip(sets, together):
+        alone = run(s, torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, alone))
