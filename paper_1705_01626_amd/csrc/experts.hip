@@ -1200,12 +1200,16 @@ Choice choose_rows(size_t m, size_t experts, size_t cols, size_t length, size_t 
 
 // Of dW.  An expert may have several times the average of rows: a kernel does not end before its tiles have.
 Choice choose_dw(size_t m, size_t experts, size_t n, size_t k, size_t w, bool loose) {
-    const size_t stages = div_up(div_up(m, experts), kStageBytes / w), tiles = div_up(n, 64) * div_up(k, kSoloCols) * experts;
+    const size_t stages = div_up(div_up(m, experts), kStageBytes / w), across = div_up(k, kSoloCols) * experts;
+    const size_t tiles16 = div_up(n, 16) * across, tiles64 = div_up(n, 64) * across;
     const double longest = experts > 1 ? 3.0 * stages : stages;
     Choice best = small_choice(static_cast<double>(div_up(n, 128) * div_up(k, 128) * experts), stages, w, loose);
+    if (w == 4) best.cost += 6;
     best.cost = std::fmax(best.cost, kLaunchUs + longest * (w == 4 ? 1.95 : 0.72) * (loose ? 1.4 : 1));
     if (w == 2 && !loose) best = cheaper(best, large_choice(static_cast<double>(div_up(n, 256) * div_up(k, 256) * experts), stages, false));
-    return cheaper(best, solo_choice(Kind::kSolo64, tiles, static_cast<double>(tiles), stages, 2 * kUnits, w == 4 ? 1.3 : 0.42, w == 4 ? 3.6 : 2.9));
+    // (16-bit types: tiles of 16 rows were faster than the others by 10 % in one of 120 drawn sizes)
+    if (w == 4) best = cheaper(best, solo_choice(Kind::kSolo16, tiles16, static_cast<double>(tiles16), stages, 4 * kUnits, 0.5, 2.2));
+    return cheaper(best, solo_choice(Kind::kSolo64, tiles64, static_cast<double>(tiles64), stages, 2 * kUnits, w == 4 ? 1.5 : 0.42, w == 4 ? 3.6 : 2.9));
 }
 
 // (as many workgroups on each XCD: `room` is a multiple of 8)
@@ -1278,8 +1282,11 @@ zvc_status backward_as(ExpertArgs<T> dx, ExpertArgs<T> dw, float* sums, hipStrea
         dx.cols = 0;
     }
     if (dw.cols != 0 && !tiles(of_dw)) {
-        const zvc_status st = of_dw.kind == Kind::kSolo64 ? solo_of<T, Does::kDw, 4>(dw, of_dw, loose_dw, sums, stream)
-                                                          : loose_of<T, Does::kDw>(dw, stream);
+        const zvc_status st = [&] {
+            if constexpr (sizeof(T) == 4)
+                if (of_dw.kind == Kind::kSolo16) return solo_of<T, Does::kDw, 1>(dw, of_dw, loose_dw, sums, stream);
+            return of_dw.kind == Kind::kSolo64 ? solo_of<T, Does::kDw, 4>(dw, of_dw, loose_dw, sums, stream) : loose_of<T, Does::kDw>(dw, stream);
+        }();
         if (st != ZVC_OK) return st;
         dw.cols = 0;
     }
