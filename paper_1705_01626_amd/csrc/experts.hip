@@ -1,5 +1,15 @@
 // Router and matrix products for mixtures of experts, forward and backward, for AMD gfx950 (wave64): kernels and C ABI
 // (include/zvc_experts.h has the formulas).
+//
+//   * route_kernel, route_sums_kernel, route_places_kernel: the choice; counts of each expert's entries by workgroup, their sums, and with these each
+//     entry's row.  Up to 32 tokens are one workgroup's, which does all three.  route_backward_kernel: the logits' gradient.
+//   * expert_product_kernel, expert_gradients_kernel: persistent workgroups over all experts' tiles, on the matrix cores, staged straight to LDS.
+//     Every workgroup makes a table of the experts' rows and tiles from the offsets first, so that the host has to know neither.
+//   * loose_kernel: the same tiles where operands do not take 16-byte accesses, staged by way of registers.
+//   * solo_kernel, solo_join_kernel: few rows, few tiles or short sums; workgroups whose waves take turns along the sum.
+//
+// Times in the comments are us on one MI355X, where a large copy moves 5.0 TB/s and a large bf16 product of the vendor's library
+// reaches 1180 to 1460 TFLOP/s (fp32 155): calls one behind the other over several sets of tensors, both sides of a comparison in turn.
 
 #include "tiles.h"
 #include "zvc_experts.h"
@@ -9,6 +19,10 @@
 namespace {
 
 // ------------------------------------------------------------------ the router
+// A token's logits lie over 16 lanes, a row of the cross-lane instructions, so that a maximum over all experts is a few instructions for each
+// of a lane's logits and four for the rest, without LDS.  16384 tokens of 256 experts, fp32, 8 choices: 19.4 in all, 13.0 for the choice, 3.8 for the
+// sums and 5.0 for the rows; reading the logits is 3.4 of them, and the rest of the choice is its 8 rounds of maximum, search and removal over a lane's 16 logits, one behind
+// the other.  8 tokens of 64 experts: 4.1, a launch and one chain from the load to the rows.
 constexpr int kRowLanes = 16;                   // lanes that share a token
 constexpr int kRouteThreads = 512;
 constexpr unsigned kRouteTokens = kRouteThreads / kRowLanes;        // of a workgroup: a bit for each in a word
@@ -186,7 +200,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs p) {
     }
 }
 
-// A workgroup an expert: its counts by workgroup become sums of those before, and their total is written behind all counts.
+// A workgroup an expert: its counts by workgroup become sums of those before, and their total is written behind all counts.  Counts lie expert by expert,
+// since these sums run along them (512 counts of each of 256 experts: 3.8, latency of one load and two barriers).
 constexpr int kSumThreads = 256;
 __global__ __launch_bounds__(kSumThreads) void route_sums_kernel(RouteArgs p) {
     constexpr unsigned kEach = 4;
@@ -218,7 +233,7 @@ __global__ __launch_bounds__(kSumThreads) void route_sums_kernel(RouteArgs p) {
     if (threadIdx.x == 0) p.counts[static_cast<size_t>(p.experts) * p.blocks + blockIdx.x] = before;
 }
 
-// Ranks become rows.
+// Ranks become rows, by the workgroups that made them (16384 x 8 entries: 5.0; each workgroup sums the experts' totals again, which spares a launch).
 __global__ __launch_bounds__(kRouteThreads) void route_places_kernel(RouteArgs p) {
     __shared__ unsigned starts[ZVC_EXPERTS_MAX + 1], room[kRouteThreads / 64];
     const unsigned* const totals = p.counts + static_cast<size_t>(p.experts) * p.blocks;
@@ -249,6 +264,8 @@ struct RouteBackArgs {
     bool normalize;
 };
 
+// The gradient of a softmax over the chosen, or over all with only the chosen ones' gradients: dl_j = p_j ([j chosen] dw_j - sum p_i dw_i).  Bound by the
+// launch and one pass over the row: 16384 x 256, bf16, 6.4 on the GPU, 8.2 MB in and out each.
 // Lane s of a token's 16 has its choice s.  The row is written as if nothing had been chosen, and then the chosen experts' elements over it, once the
 // row is there.  (Every lane looking all choices over for its columns instead: 16384 x 256 bf16, 8 choices, 8.9.)
 template <typename T, int CHUNKS>
@@ -656,6 +673,12 @@ using Large = Shape<4, 2, 4, 8, 2>;             // 256 x 256, eight waves
 using Quarter = Shape<2, 4, 4, 2, 4>;           // 128 x 128, eight waves, four stages in the same room
 
 // Workgroups take tiles until there are none left; the next tile's first stages are on their way while a tile is finished.
+//
+// A stage of 128 bytes along the sum goes straight to LDS.  In large tiles, 256 x 256 by eight waves, a wave reads 24 KB of it for 64 products of
+// 16 x 16 x 32, and a stage takes 1.45, which is 1480 TFLOP/s: there the matrix cores bound the loop, at the clock that power leaves them.  What a tile
+// costs beside it, 10 of the 57 that a sum over 2048 takes, is the latency of its first stage and 128 KB that go out through L2 (dW of 8192 x 5632 x 2048: 443, without
+// its stores 334).  Tried and slower for that dW: stores past the caches (745 where it took 576 without), stores before the next tile's first loads (484), tiles of
+// 256 x 128 by four waves, two workgroups a compute unit (484).  Tiles cut to the rows that an expert has left gain nothing.
 template <typename T, Does DOES, class S, class OF = S, typename Next>
 __device__ __forceinline__ void work(const ExpertArgs<T>& p, const Groups& groups, unsigned items, unsigned base, int lane, Next next, unsigned from = 0) {
     using Where = Tile<T, DOES, S, OF>;
@@ -724,6 +747,8 @@ __device__ __forceinline__ Groups tables(const int64_t* offsets, unsigned expert
 }
 __device__ __forceinline__ unsigned address(unsigned char* lds) { return static_cast<unsigned>(reinterpret_cast<uintptr_t>((LdsByte*)lds)); }
 
+// y.  8192 x 5632 x 2048 of 16 experts, bf16: 217, 870 TFLOP/s; were every expert's rows a multiple of 256, it would be 157 in full rounds.  The matrix cores are
+// busy for half of the dispatch, ragged tiles' empty rows included.
 // Large tiles that do not fill a round go in quarters, with a deeper ring, where those are two rounds or less: one of large tiles takes 57 with a sum over 2048,
 // one of quarters some 20 (16 x 512 rows, 5632 x 2048, 3.4 rounds: 229.6 without, 217).
 template <typename T, class S>
@@ -740,7 +765,8 @@ __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void expert_product_kerne
     }
 }
 
-// dx, and behind it dW, in one go: either alone leaves compute units idle in its last round.  dw_tiles: of one expert; it, and dx.cols, may be 0.
+// dx, and behind it dW, in one go: either alone leaves compute units idle in its last round (16384 x 5632 x 2048 of 32 experts, bf16: 810, 930 TFLOP/s;
+// 849 where idle workgroups do not go ahead with dW).  dw_tiles: of one expert; it, and dx.cols, may be 0.
 template <typename T, class S>
 __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void expert_gradients_kernel(ExpertArgs<T> dx, ExpertArgs<T> dw, unsigned dw_tiles) {
     unsigned char* const lds = room_of<S>();
@@ -815,6 +841,8 @@ struct LooseOperand {
     }
 };
 
+// The next stage is in registers while one is multiplied.  16-byte loads at any element take the loads' unit longer, and every 16 bytes pass the registers: dW of
+// 1956 rows, 32 experts, 2672 x 704, bf16, takes 56 here and 44 straight to LDS, which an operand that is not aligned has no other way to.
 template <typename T, Does DOES, class S>
 __global__ __launch_bounds__(S::kThreads, S::kPerUnit) void loose_kernel(ExpertArgs<T> p, unsigned dw_tiles) {
     static_assert(S::kRing == 2, "one stage is read while the next is written");
@@ -948,8 +976,11 @@ struct SoloSplit {
 
 // Tiles of 64 columns and 16 QB rows.  The workgroup's waves take turns along the reduction, each with a place of its own in LDS for a stage, and meet there at
 // the end; no wave waits for another.  What hides a wave's wait for its next stage are the other waves: four workgroups of 16 rows fit a compute unit, two of
-// 64.  (With two places a wave, and half as many waves, 16 x 512 rows, 1024 x 1024, bf16 took 58.8 instead of 40.0; 8 x 128, 2048 x 2048 29.3 and 24.6.)
-// LOOSE: operands come by way of registers.
+// 64.  One token's 8 rows through 8 of 64 experts, 2816 x 1024, bf16: 9.9, reading the weights at 4.7 TB/s.  (With two places a wave, and half as
+// many waves, 16 x 512 rows, 1024 x 1024, bf16 took 58.8 instead of 40.0; 8 x 128, 2048 x 2048 29.3 and 24.6.)
+// LOOSE: operands come by way of registers, a stage ahead (two ahead: the dx of 777 x 1000 x 682 of 7 experts, fp32, 40.1 instead of 28.2, other products 0 to
+// 17 % slower: not their latency bounds them, but what unaligned loads cost).  An expert's tiles of dW lie side by side in the grid: taken from all experts in
+// turn, both gradients of that size took 73.8 instead of 65.7; a run of them for each XCD gains nothing.
 template <typename T, Does DOES, int QB, bool LOOSE>
 __global__ __launch_bounds__(64 * kSoloWaves, QB == 1 ? (LOOSE ? 3 : 4) : 2) void solo_kernel(ExpertArgs<T> p, SoloSplit split) {
     using S = Shape<1, 1, 4, QB, 2>;
@@ -1065,7 +1096,7 @@ __global__ __launch_bounds__(64 * kSoloWaves, QB == 1 ? (LOOSE ? 3 : 4) : 2) voi
     }
 }
 
-// The parts' sums of tiles of 64 columns and 16 QB rows, joined in the order of the parts: a workgroup takes 16 rows of a tile.
+// The parts' sums of tiles of 64 columns and 16 QB rows, joined in the order of the parts: a workgroup takes 16 rows of a tile.  A launch and a read of the sums, 3 to 5.
 template <typename T, Does DOES, int QB>
 __global__ __launch_bounds__(256) void solo_join_kernel(ExpertArgs<T> p, SoloSplit split) {
     constexpr unsigned kRows = 16 * QB;
@@ -1155,6 +1186,8 @@ double expected_tiles(size_t m, size_t experts, size_t tile) {
 //                 2 x 256, 512, 2048: S 24.0, s16 9.4, s64 13.1     16 x 512, 1024, 1024: L 30.7, S 29.4, s64 40.0     16 x 512, 5632, 2048: L 217, S 251
 //   fp32 forward  8 x 32, 2048, 2048: S 132, s16 43.6, s64 81.9     8 x 128, 2048, 2048: S 136, s16 109, s64 131       16 x 512, 1024, 1024: S 188, s16 195, s64 181
 //   dW            bf16 5 x 600, 1024, 512: S 17.2, s64 14.4         bf16 8 x 128, 2048, 2048: S 26.3, s64 69.6         fp32 5 x 600, 1024, 512: S 80.2, s64 47.6
+//                 fp32 11 x 271, 256, 512: S 48.0, s16 17.6, s64 22.2     fp32 8 x 816, 3656, 520: S 258, s16 339, s64 276
+// Against the fastest kernel forced, the one that is chosen takes, over 120 drawn sizes each: y and dx 1.01 (fp32) and 1.03 (16 bits) times as long, dW 1.03 and 1.05.
 //   (tiles of 256 x 32 and small kernels with a tile for each wave were slower than these or the same everywhere)
 constexpr double kLaunchUs = 5, kJoinUs = 3, kSumsPerUs = 3e6;
 
