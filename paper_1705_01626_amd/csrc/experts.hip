@@ -747,8 +747,8 @@ __device__ __forceinline__ Groups tables(const int64_t* offsets, unsigned expert
 }
 __device__ __forceinline__ unsigned address(unsigned char* lds) { return static_cast<unsigned>(reinterpret_cast<uintptr_t>((LdsByte*)lds)); }
 
-// y.  8192 x 5632 x 2048 of 16 experts, bf16: 217, 870 TFLOP/s; were every expert's rows a multiple of 256, it would be 157 in full rounds.  The matrix cores are
-// busy for half of the dispatch, ragged tiles' empty rows included.
+// y.  8192 x 5632 x 2048 of 16 experts, bf16: 217, 870 TFLOP/s.  The rows would fill 2.75 rounds of tiles; the experts' ragged ends make them 3.4.  The matrix
+// cores are busy for half of the dispatch.
 // Large tiles that do not fill a round go in quarters, with a deeper ring, where those are two rounds or less: one of large tiles takes 57 with a sum over 2048,
 // one of quarters some 20 (16 x 512 rows, 5632 x 2048, 3.4 rounds: 229.6 without, 217).
 template <typename T, class S>
