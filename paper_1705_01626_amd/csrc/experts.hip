@@ -1220,15 +1220,25 @@ Choice solo_choice(Kind kind, size_t most, double tiles, size_t stages, size_t s
 
 Choice cheaper(const Choice& a, const Choice& b) { return b.cost < a.cost ? b : a; }
 
-// Of y (forward) or dx: `cols` columns, sums over `length`.
+// No sooner than the weights, `bytes`, are read at `rate` bytes a us.
+Choice reading(Choice c, double bytes, double rate) {
+    c.cost = std::fmax(c.cost, bytes / rate);
+    return c;
+}
+
+// Of y (forward) or dx: `cols` columns, sums over `length`.  Small kernels read dx's weights in pieces of 64 columns of a row, and slower than others (dx of 645 rows, 28
+// experts, 3248 x 2776, bf16: s16 167, S 89; y of 991 rows, 94 experts, 2336 x 1608: s16 161, S 114).
 Choice choose_rows(size_t m, size_t experts, size_t cols, size_t length, size_t w, bool loose, bool forward) {
     const size_t stages = div_up(length, kStageBytes / w), across = div_up(cols, kSoloCols);
-    Choice best = small_choice(expected_tiles(m, experts, 128) * div_up(cols, 128), stages, w, loose);
-    if (w == 2 && !loose) best = cheaper(best, large_choice(expected_tiles(m, experts, 256) * div_up(cols, 256), stages, forward));
-    best = cheaper(best, solo_choice(Kind::kSolo16, row_tiles(m, experts, 16) * across, expected_tiles(m, experts, 16) * across, stages, 4 * kUnits,
-                                     w == 4 ? 0.65 : 0.3, w == 4 ? 4.1 : 2.8));
-    return cheaper(best, solo_choice(Kind::kSolo64, row_tiles(m, experts, 64) * across, expected_tiles(m, experts, 64) * across, stages, 2 * kUnits,
-                                     w == 4 ? 1.2 : 0.25, w == 4 ? 7.8 : 5));
+    const double bytes = static_cast<double>((experts < m ? experts : m) * cols * length * w);
+    Choice best = reading(small_choice(expected_tiles(m, experts, 128) * div_up(cols, 128), stages, w, loose), bytes, 5.5e6);
+    if (w == 2 && !loose)
+        best = cheaper(best, reading(large_choice(expected_tiles(m, experts, 256) * div_up(cols, 256), stages, forward), bytes, 5e6));
+    const Choice by16 = solo_choice(Kind::kSolo16, row_tiles(m, experts, 16) * across, expected_tiles(m, experts, 16) * across, stages, 4 * kUnits,
+                                    w == 4 ? 0.65 : 0.3, w == 4 ? 4.1 : 2.8);
+    const Choice by64 = solo_choice(Kind::kSolo64, row_tiles(m, experts, 64) * across, expected_tiles(m, experts, 64) * across, stages, 2 * kUnits,
+                                    w == 4 ? 1.2 : 0.25, w == 4 ? 7.8 : 5);
+    return cheaper(cheaper(best, reading(by16, bytes, forward ? 5e6 : 3.5e6)), reading(by64, bytes, forward ? 5.2e6 : 3.2e6));
 }
 
 // Of dW.  An expert may have several times the average of rows: a kernel does not end before its tiles have.
