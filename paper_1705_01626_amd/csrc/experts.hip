@@ -676,8 +676,8 @@ using Quarter = Shape<2, 4, 4, 2, 4>;           // 128 x 128, eight waves, four 
 //
 // A stage of 128 bytes along the sum goes straight to LDS.  In large tiles, 256 x 256 by eight waves, a wave reads 24 KB of it for 64 products of
 // 16 x 16 x 32, and a stage takes 1.45, which is 1480 TFLOP/s: there the matrix cores bound the loop, at the clock that power leaves them.  What a tile
-// costs beside it, 10 of the 57 that a sum over 2048 takes, is the latency of its first stage and 128 KB that go out through L2 (dW of 8192 x 5632 x 2048: 443, without
-// its stores 334).  Tried and slower for that dW: stores past the caches (745 where it took 576 without), stores before the next tile's first loads (484), tiles of
+// costs beside it, 10 of the 57 that a sum over 2048 takes, is the latency of its first stage and 128 KB that go out through L2 (dW of 16384 x 5632 x 2048 of 32 experts: 443,
+// without its stores 334).  Tried and slower for that dW: stores past the caches (745 where it took 576 without), stores before the next tile's first loads (484), tiles of
 // 256 x 128 by four waves, two workgroups a compute unit (484).  Tiles cut to the rows that an expert has left gain nothing.
 template <typename T, Does DOES, class S, class OF = S, typename Next>
 __device__ __forceinline__ void work(const ExpertArgs<T>& p, const Groups& groups, unsigned items, unsigned base, int lane, Next next, unsigned from = 0) {
@@ -1187,7 +1187,8 @@ double expected_tiles(size_t m, size_t experts, size_t tile) {
 //   fp32 forward  8 x 32, 2048, 2048: S 132, s16 43.6, s64 81.9     8 x 128, 2048, 2048: S 136, s16 109, s64 131       16 x 512, 1024, 1024: S 188, s16 195, s64 181
 //   dW            bf16 5 x 600, 1024, 512: S 17.2, s64 14.4         bf16 8 x 128, 2048, 2048: S 26.3, s64 69.6         fp32 5 x 600, 1024, 512: S 80.2, s64 47.6
 //                 fp32 11 x 271, 256, 512: S 48.0, s16 17.6, s64 22.2     fp32 8 x 816, 3656, 520: S 258, s16 339, s64 276
-// Against the fastest kernel forced, the one that is chosen takes, over 120 drawn sizes each: y and dx 1.01 (fp32) and 1.03 (16 bits) times as long, dW 1.03 and 1.05.
+// Against the fastest kernel forced, the one that is chosen takes, over 120 drawn sizes and more: y and dx 1.01 times as long in fp32, with 16 bits
+// 1.04 (y) and 1.02 (dx), dW 1.03 and 1.05.
 //   (tiles of 256 x 32 and small kernels with a tile for each wave were slower than these or the same everywhere)
 constexpr double kLaunchUs = 5, kJoinUs = 3, kSumsPerUs = 3e6;
 
@@ -1201,7 +1202,7 @@ Choice large_choice(double tiles, double stages, bool quarters) {
 Choice small_choice(double tiles, double stages, size_t w, bool loose) {
     double us;
     if (w == 4) us = std::ceil(tiles / kUnits) * (1.95 * stages + 2);                  // the matrix instructions bound it: two on a compute unit take twice as long
-    else us = std::fmax(1, tiles / (2 * kUnits)) * ((tiles <= kUnits ? 0.62 : tiles <= 2 * kUnits ? 0.72 : 1.2) * stages + 2);
+    else us = std::fmax(1, tiles / (2 * kUnits)) * ((tiles <= 2 * kUnits ? 0.72 : 1.35) * stages + 2);
     return {loose ? Kind::kLoose : Kind::kSmall, 1, 0, kLaunchUs + (loose ? (w == 4 ? 1.3 : 1.5) : 1) * us};
 }
 
@@ -1235,9 +1236,9 @@ Choice choose_rows(size_t m, size_t experts, size_t cols, size_t length, size_t 
     if (w == 2 && !loose)
         best = cheaper(best, reading(large_choice(expected_tiles(m, experts, 256) * div_up(cols, 256), stages, forward), bytes, 5e6));
     const Choice by16 = solo_choice(Kind::kSolo16, row_tiles(m, experts, 16) * across, expected_tiles(m, experts, 16) * across, stages, 4 * kUnits,
-                                    w == 4 ? 0.65 : 0.3, w == 4 ? 4.1 : 2.8);
+                                    w == 4 ? 0.65 : 0.4, w == 4 ? 4.1 : 2.8);
     const Choice by64 = solo_choice(Kind::kSolo64, row_tiles(m, experts, 64) * across, expected_tiles(m, experts, 64) * across, stages, 2 * kUnits,
-                                    w == 4 ? 1.2 : 0.25, w == 4 ? 7.8 : 5);
+                                    w == 4 ? 1.2 : 0.4, w == 4 ? 7.8 : 5);
     return cheaper(cheaper(best, reading(by16, bytes, forward ? 5e6 : 3.5e6)), reading(by64, bytes, forward ? 5.2e6 : 3.2e6));
 }
 
