@@ -6,7 +6,8 @@ with states in 32 bits or in 8.
     adamw.zvc_adamw(plan, rate=3e-4, step=t)                        # t = 1, 2, ...
 
 Argument marshalling only, in the manner of `zvc`: the caller owns every tensor, and work is enqueued
-on the given or the current stream.  A plan keeps its tensors alive.  There is no CPU fallback.
+on the given or the current stream.  A plan keeps its tensors alive, and dropped behind a call it keeps their memory
+until that step has run.  There is no CPU fallback.
 """
 from __future__ import annotations
 
@@ -99,7 +100,16 @@ class Plan:
     def __init__(self, tensors, host, device_bytes):
         self.tensors, self.host, self.device_bytes = tensors, host, device_bytes
         self.device = device_bytes.device
-        self.streams = {_stream_handle(None)}       # that device_bytes are known to be read on
+        self.streams = set()                        # that the tensors' allocator knows to be used
+
+    def used_on(self, stream) -> None:
+        """No memory of the plan's tensors, nor its own, goes to another tensor before what is on `stream` by then has run.  (Of the gradients
+        and weights too: the plan may be the last to hold them.)"""
+        for param, grad, state, master in self.tensors:
+            for t in (param, grad, *state, master):
+                if t is not None:
+                    t.record_stream(stream)
+        self.device_bytes.record_stream(stream)
 
 
 def _flat(t: torch.Tensor, count: int, types, device, where: str, name: str) -> int:
@@ -185,7 +195,7 @@ def zvc_adamw(plan: Plan, rate: float, step: int, beta1: float = 0.9, beta2: flo
             _refuse(where, "d_factors has to be two contiguous floats on the plan's device")
         now.d_factors = d_factors.data_ptr()
     handle = _stream_handle(stream)
-    if handle not in plan.streams:          # its memory may not go to another tensor before this stream has read it
-        plan.device_bytes.record_stream(torch.cuda.current_stream() if stream is None else stream)
+    if handle not in plan.streams:          # (the first one too: the tensors may have been made on another)
+        plan.used_on(torch.cuda.current_stream() if stream is None else stream)
         plan.streams.add(handle)
     _check(_native().zvc_adamw(plan.host.data_ptr(), plan.device_bytes.data_ptr(), ctypes.addressof(now), handle), where)
