@@ -98,6 +98,33 @@ def test_route_backward(dtype, m, e, top):
         assert (out[:, e:] == 77).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("e", [5, 16, 130, 1024])
+def test_route_backward_of_what_is_not_finite(dtype, e):
+    """An expert that is out gets 0 whatever the others' gradients are, and an infinity or a NaN stays in its token."""
+    gen = generator("not finite", e, str(dtype))
+    m, top = 12, 2
+    logits = torch.randn(m, e, generator=gen, device=DEV).to(dtype)
+    out = torch.rand(m, e, generator=gen, device=DEV) < 0.4
+    out[:, :3], out[:, 3] = False, True
+    logits[out] = -math.inf
+    logits[:, 3] = NAN
+    chosen = torch.tensor([[1, 0]] * m, dtype=torch.int32, device=DEV)
+    dw = torch.randn(m, top, generator=gen, device=DEV)
+    dw[1, 0], dw[3, 1], dw[5, 0] = math.inf, -math.inf, NAN
+    logits[7, 2] = math.inf                       # (not a chosen one: a softmax over all is NaN)
+    for normalize in (True, False):
+        got = torch.full((m, e), 77.0, dtype=dtype, device=DEV)
+        experts.zvc_route_backward(dw, logits, chosen, got, normalize=normalize)
+        assert (got[out] == 0).all()
+        odd = [1, 3, 5] if normalize else [1, 3, 5, 7]
+        fine = [t for t in range(m) if t not in odd]
+        assert torch.isfinite(got[fine]).all() and (got[fine][:, :2] != 0).all()
+        assert not torch.isfinite(got[odd][:, :2]).any()
+        if not normalize:
+            assert not torch.isfinite(got[[1, 3, 5]][:, 2]).any() and got[7].isnan().logical_or(out[7]).all()
+
+
 # ---- the products -----------------------------------------------------------------
 def offsets_of(m, experts_, how, gen):
     """Where the experts' rows begin: dealt unevenly, all to one, evenly, with rows of no expert at both ends, or out of order."""
