@@ -53,7 +53,9 @@ class Mixture:
         self.hidden.clamp_(min=0)
         self.kept.leave(self.hidden)
         experts.zvc_expert_product(self.hidden, self.w2, self.offsets, self.out, self.ws[1])
-        self.picked = self.out[self.place].float()                   # tokens x top x width
+        # (an entry without a row has place -1: what lies in the last row is another token's, and of another step)
+        self.there = (self.place >= 0)[..., None]
+        self.picked = torch.where(self.there, self.out[self.place].float(), 0.0)     # tokens x top x width
         return x + (self.picked * self.shares[..., None]).sum(1).to(x.dtype)
 
     def backward(self, x, dy):
@@ -68,7 +70,8 @@ class Mixture:
         experts.zvc_expert_gradients(self.dhidden, self.rows, self.w1, self.offsets, self.drows, self.dw1, self.ws[0])
         experts.zvc_route_backward(dshares, self.logits, self.chosen, self.dlogits)
         self.drouter.copy_(self.dlogits.t() @ x.float())
-        return (dy.float() + self.drows[self.place].float().sum(1) + self.dlogits @ self.router.float()).to(x.dtype)
+        drows = torch.where(self.there, self.drows[self.place].float(), 0.0)
+        return (dy.float() + drows.sum(1) + self.dlogits @ self.router.float()).to(x.dtype)
 
     def update(self, rate):
         self.step += 1

@@ -116,3 +116,34 @@ def test_a_step_of_padded_tokens_from_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(one.results(), other.results()))
         rows = int(one.route[2][-1])
         assert (one.route[3][rows:] == -1).all() and int((one.route[0] >= 0).sum()) == rows
+
+
+def test_tokens_without_experts(example, monkeypatch):
+    """They pass as they are in both directions, and what other tokens left in rows that are no expert's now reaches neither them nor any weight."""
+    tokens, width, inner, count = 300, 72, 136, 5
+    block = example.Mixture(tokens, width, inner, count, seed=5)
+    gen = generator("without")
+    draw = lambda: torch.randn(tokens, width, generator=gen, device="cuda").bfloat16()
+    x, dy = draw(), draw()
+    block.forward(x)
+    block.backward(x, dy)
+    away = torch.rand(tokens, generator=gen, device="cuda") < 0.4
+    plain = example.experts.zvc_route
+
+    def masked(logits, *args):
+        logits[away] = -float("inf")
+        plain(logits, *args)
+
+    monkeypatch.setattr(example.experts, "zvc_route", masked)
+    for stale in (None, float("nan")):
+        x, dy = draw(), draw()
+        rows = int((~away).sum()) * block.top
+        if stale is not None:
+            block.out[rows:], block.drows[rows:] = stale, stale
+        y = block.forward(x)
+        dx = block.backward(x, dy)
+        assert int(block.offsets[-1]) == rows and (block.place[away] == -1).all()
+        assert torch.equal(y[away], x[away]) and torch.equal(dx[away], dy[away])
+        for t in (y, dx, *block.grads):
+            assert torch.isfinite(t).all()
+        assert not torch.equal(dx[~away], dy[~away]) and not torch.equal(y[~away], x[~away])
