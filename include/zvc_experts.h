@@ -29,7 +29,7 @@ extern "C" {
 #define ZVC_EXPERTS_MAX_TOP 16
 #define ZVC_EXPERTS_MAX_ENTRIES ((size_t)1 << 27)
 
-/* Bytes of device workspace that zvc_route needs (256-byte aligned, no initialisation).  0 for a bad size. */
+/* Bytes of device workspace that zvc_route needs for m tokens or fewer (256-byte aligned, no initialisation).  0 for a bad size. */
 size_t zvc_route_workspace_bytes(size_t m, size_t experts, size_t top);
 
 /* The router.  d_logits: m x experts, row stride ldl.  An expert whose logit is minus infinity or a NaN is out of that token's choice.
@@ -52,7 +52,7 @@ zvc_status zvc_route_backward(const float* d_dweights, const void* d_logits, siz
                               size_t m, size_t experts, size_t top, int type, int normalize, hipStream_t stream);
 
 /* Bytes of device workspace that zvc_expert_product (backward = 0) or zvc_expert_gradients (backward = 1) needs
- * (256-byte aligned, no initialisation).  0 for a bad type or size. */
+ * for m rows or fewer of the same experts, n, k and type (256-byte aligned, no initialisation).  0 for a bad type or size. */
 size_t zvc_expert_workspace_bytes(size_t m, size_t experts, size_t n, size_t k, int type, int backward);
 
 /* y[r] = x[r] W_e^T.  x: m x k; y: m x n; W: experts times n x k with row stride ldw, an expert's weight sw elements behind

@@ -1172,8 +1172,7 @@ enum class Kind { kLarge, kSmall, kLoose, kSolo16, kSolo64 };
 
 struct Choice {
     Kind kind;
-    unsigned parts;                             // of a small kernel's sums
-    size_t sums;                                // their bytes
+    unsigned parts;                             // of a small kernel's sums (their bytes: within what most_row_sums and most_dw_sums say)
     double cost;
 };
 
@@ -1201,27 +1200,32 @@ constexpr double kLaunchUs = 5, kJoinUs = 3, kSumsPerUs = 3e6;
 Choice large_choice(double tiles, double stages, bool quarters) {
     const double whole = std::floor(tiles / kUnits), part = tiles / kUnits - whole;
     const double rounds = whole + (part == 0 ? 0 : quarters && part <= 0.5 ? 0.4 * std::ceil(4 * part) : 1);
-    return {Kind::kLarge, 1, 0, kLaunchUs + rounds * (1.45 * stages + 10)};
+    return {Kind::kLarge, 1, kLaunchUs + rounds * (1.45 * stages + 10)};
 }
 
 Choice small_choice(double tiles, double stages, size_t w, bool loose) {
     double us;
     if (w == 4) us = std::ceil(tiles / kUnits) * (1.95 * stages + 2);                  // the matrix instructions bound it: two on a compute unit take twice as long
     else us = std::fmax(1, tiles / (2 * kUnits)) * ((tiles <= 2 * kUnits ? 0.72 : 1.35) * stages + 2);
-    return {loose ? Kind::kLoose : Kind::kSmall, 1, 0, kLaunchUs + (loose ? (w == 4 ? 1.3 : 1.5) : 1) * us};
+    return {loose ? Kind::kLoose : Kind::kSmall, 1, kLaunchUs + (loose ? (w == 4 ? 1.3 : 1.5) : 1) * us};
 }
 
-// Parts of a small kernel's sums where its tiles do not fill the compute units.  most: tiles at most.
-Choice solo_choice(Kind kind, size_t most, double tiles, size_t stages, size_t slots, double stage_us, double item_us) {
-    if (most > size_t{1} << 20) return {kind, 1, 0, HUGE_VAL};      // (a dimension of a grid holds fewer than 2^32 lanes)
-    const size_t rows = kind == Kind::kSolo16 ? 16 : 64;
+// Parts of a small kernel's sums where its tiles do not fill the compute units.  More tiles never make it more parts, nor do fewer stages.
+size_t solo_parts(double tiles, size_t stages) {
     size_t parts = tiles < 1 ? 1 : static_cast<size_t>(2 * kUnits / tiles);
     if (parts > stages / (2 * kSoloWaves)) parts = stages / (2 * kSoloWaves);
     if (parts > 16) parts = 16;
-    if (parts < 2) parts = 1;
-    const size_t sums = parts > 1 ? parts * most * rows * kSoloCols * sizeof(float) : 0;
+    return parts < 2 ? 1 : parts;
+}
+size_t solo_rows(Kind kind) { return kind == Kind::kSolo16 ? 16 : 64; }
+size_t solo_tile_bytes(Kind kind) { return solo_rows(kind) * kSoloCols * sizeof(float); }
+
+// most: tiles at most.
+Choice solo_choice(Kind kind, size_t most, double tiles, size_t stages, size_t slots, double stage_us, double item_us) {
+    if (most > size_t{1} << 20) return {kind, 1, HUGE_VAL};      // (a dimension of a grid holds fewer than 2^32 lanes)
+    const size_t parts = solo_parts(tiles, stages), sums = parts > 1 ? parts * most * solo_tile_bytes(kind) : 0;
     const double each = item_us + stage_us * static_cast<double>(stages) / parts;
-    return {kind, static_cast<unsigned>(parts), sums, kLaunchUs + std::fmax(1, tiles * parts / slots) * each + (parts > 1 ? kJoinUs + sums / kSumsPerUs : 0)};
+    return {kind, static_cast<unsigned>(parts), kLaunchUs + std::fmax(1, tiles * parts / slots) * each + (parts > 1 ? kJoinUs + sums / kSumsPerUs : 0)};
 }
 
 Choice cheaper(const Choice& a, const Choice& b) { return b.cost < a.cost ? b : a; }
@@ -1259,6 +1263,30 @@ Choice choose_dw(size_t m, size_t experts, size_t n, size_t k, size_t w, bool lo
     // (16-bit types: tiles of 16 rows were faster than the others by 10 % in one of 120 drawn sizes)
     if (w == 4) best = cheaper(best, solo_choice(Kind::kSolo16, tiles16, static_cast<double>(tiles16), stages, 4 * kUnits, 0.5, 2.2));
     return cheaper(best, solo_choice(Kind::kSolo64, tiles64, static_cast<double>(tiles64), stages, 2 * kUnits, w == 4 ? 1.5 : 0.42, w == 4 ? 3.6 : 2.9));
+}
+
+// Bytes that the sums' parts take of m rows at most, however many fewer there are and whichever kernel the account chooses for them.
+//
+// y and dx: the fewer rows the more parts, up to those of one expert's few.  With u experts that have rows there are t >= u tiles expected and t >= m / tile + u / 2 (each
+// times the tiles across), and parts <= 512 / t; room is made for m / tile + u tiles, at most 1.5 t of them, so for parts of 768 tiles at most.
+size_t most_row_sums(size_t m, size_t experts, size_t cols, size_t length, size_t w) {
+    const size_t across = div_up(cols, kSoloCols), parts = solo_parts(static_cast<double>(across), div_up(length, kStageBytes / w));
+    size_t most = 0;
+    for (const Kind kind : {Kind::kSolo16, Kind::kSolo64}) {
+        const size_t tiles = parts * row_tiles(m, experts, solo_rows(kind)) * across, sums = parts > 1 ? (tiles < 3 * kUnits ? tiles : 3 * kUnits) * solo_tile_bytes(kind) : 0;
+        most = sums > most ? sums : most;
+    }
+    return most;
+}
+// dW: the tiles are the same for any m, and more rows make more parts.
+size_t most_dw_sums(size_t m, size_t experts, size_t n, size_t k, size_t w) {
+    const size_t stages = div_up(div_up(m, experts), kStageBytes / w), across = div_up(k, kSoloCols) * experts;
+    size_t most = 0;
+    for (const Kind kind : {Kind::kSolo16, Kind::kSolo64}) {
+        const size_t tiles = div_up(n, solo_rows(kind)) * across, parts = solo_parts(static_cast<double>(tiles), stages), sums = parts > 1 ? parts * tiles * solo_tile_bytes(kind) : 0;
+        most = sums > most ? sums : most;
+    }
+    return most;
 }
 
 // (as many workgroups on each XCD: `room` is a multiple of 8)
@@ -1424,13 +1452,9 @@ zvc_status zvc_route_backward(const float* d_dweights, const void* d_logits, siz
 size_t zvc_expert_workspace_bytes(size_t m, size_t experts, size_t n, size_t k, int type, int backward) {
     const size_t w = type_bytes(type);
     if (w == 0 || !expert_sizes_ok(m, experts, n, k)) return 0;
-    size_t sums = 0;
-    for (const bool loose : {false, true}) {
-        const auto most = [&](const Choice& c) { sums = c.sums > sums ? c.sums : sums; };
-        if (backward == 0) most(choose_rows(m, experts, n, k, w, loose, true));
-        else most(choose_rows(m, experts, k, n, w, loose, false)), most(choose_dw(m, experts, n, k, w, loose));
-    }
-    return 256 + round_up(sums, 256);
+    const size_t rows = backward == 0 ? most_row_sums(m, experts, n, k, w) : most_row_sums(m, experts, k, n, w);
+    const size_t dw = backward == 0 ? 0 : most_dw_sums(m, experts, n, k, w);
+    return 256 + round_up(rows > dw ? rows : dw, 256);
 }
 
 zvc_status zvc_expert_product(const void* d_x, size_t ldx, const void* d_w, size_t ldw, size_t sw, const int64_t* d_offsets, void* d_y,

@@ -118,7 +118,7 @@ def zvc_route_workspace_bytes(m: int, experts: int, top: int) -> int:
 
 
 def new_route_workspace(logits: torch.Tensor, top: int) -> torch.Tensor:
-    """A workspace for zvc_route on these logits."""
+    """A workspace for zvc_route on these logits, or fewer rows."""
     need = zvc_route_workspace_bytes(logits.shape[0], logits.shape[1], top)
     return torch.empty(max(need, 256), dtype=torch.uint8, device=logits.device)
 
@@ -168,7 +168,7 @@ def zvc_expert_workspace_bytes(m: int, experts: int, n: int, k: int, dtype: torc
 
 
 def new_expert_workspace(x: torch.Tensor, w: torch.Tensor, backward: bool = False) -> torch.Tensor:
-    """A workspace for the calls on these tensors; backward: for both passes."""
+    """A workspace for the calls on these tensors, or fewer rows; backward: for both passes."""
     m, (experts, n, k) = x.shape[0], w.shape
     need = max(zvc_expert_workspace_bytes(m, experts, n, k, x.dtype, b) for b in ((False, True) if backward else (False,)))
     return torch.empty(max(need, 256), dtype=torch.uint8, device=x.device)
