@@ -62,7 +62,8 @@ zvc_status zvc_expert_product(const void* d_x, size_t ldx, const void* d_w, size
                               size_t ldy, size_t m, size_t experts, size_t n, size_t k, int type, void* d_ws, size_t ws, hipStream_t stream);
 
 /* The gradients of x and W from dy, that of y.  dW: experts times n x k with strides lddw and sdw; 0 for an expert without rows.
- * Rows of dx that are no expert's stay as they were.  d_dx or d_dw may be null: that one is not computed. */
+ * Rows of dx that are no expert's stay as they were.  d_dx or d_dw may be null: that one is not computed, and the other one's last bits
+ * need not be those that a call for both gives (which kernel is taken goes by what is wanted). */
 zvc_status zvc_expert_gradients(const void* d_dy, size_t lddy, const void* d_x, size_t ldx, const void* d_w, size_t ldw, size_t sw,
                                 const int64_t* d_offsets, void* d_dx, size_t lddx, void* d_dw, size_t lddw, size_t sdw, size_t m,
                                 size_t experts, size_t n, size_t k, int type, void* d_ws, size_t ws, hipStream_t stream);

@@ -79,7 +79,8 @@ zvc_status zvc_dropout(const void* d_x, size_t ldx, const void* d_residual, size
 /* Bytes of device workspace that zvc_glu_forward (backward = 0) or
  * zvc_glu_backward (backward = 1) needs.  `loose`: not 0 if the address or the
  * row stride of x, Wg or Wu is no multiple of 16 bytes.  The workspace must be
- * 256-byte aligned and needs no initialisation.  0 for a bad type or size. */
+ * 256-byte aligned and needs no initialisation.  0 for a bad type or size.
+ * For these sizes alone: fewer rows may need more, since few tiles are cut along their sums. */
 size_t zvc_glu_workspace_bytes(size_t m, size_t n, size_t k, int type, int backward, int loose);
 
 /* h = drop(act(x Wg^T) * (x Wu^T)).  Where d_gate and d_up are not null (both or

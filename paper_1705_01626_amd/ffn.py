@@ -181,7 +181,7 @@ def _loose(*tensors: torch.Tensor) -> bool:
 
 
 def new_glu_workspace(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, backward: bool = False) -> torch.Tensor:
-    """A workspace for the calls on these tensors; backward: for both passes."""
+    """A workspace for the calls on these tensors (not for fewer rows, which may need more); backward: for both passes."""
     m, k, n = x.shape[0], x.shape[1], w_gate.shape[0]
     loose = _loose(x, w_gate, w_up)
     need = max(zvc_glu_workspace_bytes(m, n, k, x.dtype, b, loose) for b in ((False, True) if backward else (False,)))
