@@ -147,3 +147,20 @@ def test_tokens_without_experts(example, monkeypatch):
         for t in (y, dx, *block.grads):
             assert torch.isfinite(t).all()
         assert not torch.equal(dx[~away], dy[~away]) and not torch.equal(y[~away], x[~away])
+
+
+def test_the_first_step_goes_against_the_gradient(example):
+    """m / (1 - beta1) is then the gradient and sqrt(v / (1 - beta2)) its size.  Weights lie below 8, where half a unit of 32 bits is 2^-22: three roundings of
+    them and some ten of a change of 1e-2 are below 2^-20."""
+    block = example.Mixture(256, 64, 128, 4, seed=9)
+    gen = generator("against")
+    x, dy = (torch.randn(256, 64, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    block.forward(x)
+    block.backward(x, dy)
+    before = [w.double() for w in block.masters]
+    block.update(1e-2)
+    for old, grad, new, decay in zip(before, block.grads, block.masters, (0.01, 0.01, 0.0)):
+        g = grad.double()
+        want = (1 - 1e-2 * decay) * old - 1e-2 * g / (g.abs() + 1e-8)
+        assert float(old.abs().max()) < 8 and grad.any()
+        assert float((new.double() - want).abs().max()) < 2.0 ** -20
