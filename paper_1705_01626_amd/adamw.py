@@ -101,6 +101,7 @@ class Plan:
         self.tensors, self.host, self.device_bytes = tensors, host, device_bytes
         self.device = device_bytes.device
         self.streams = set()                        # that the tensors' allocator knows to be used
+        self.used_on(torch.cuda.current_stream(self.device))        # (most steps': here and not in the first of them; the tensors may have been made on another)
 
     def used_on(self, stream) -> None:
         """No memory of the plan's tensors, nor its own, goes to another tensor before what is on `stream` by then has run.  (Of the gradients
@@ -110,6 +111,7 @@ class Plan:
                 if t is not None:
                     t.record_stream(stream)
         self.device_bytes.record_stream(stream)
+        self.streams.add(int(stream.cuda_stream))
 
 
 def _flat(t: torch.Tensor, count: int, types, device, where: str, name: str) -> int:
@@ -195,7 +197,6 @@ def zvc_adamw(plan: Plan, rate: float, step: int, beta1: float = 0.9, beta2: flo
             _refuse(where, "d_factors has to be two contiguous floats on the plan's device")
         now.d_factors = d_factors.data_ptr()
     handle = _stream_handle(stream)
-    if handle not in plan.streams:          # (the first one too: the tensors may have been made on another)
+    if handle not in plan.streams:
         plan.used_on(torch.cuda.current_stream() if stream is None else stream)
-        plan.streams.add(handle)
     _check(_native().zvc_adamw(plan.host.data_ptr(), plan.device_bytes.data_ptr(), ctypes.addressof(now), handle), where)
