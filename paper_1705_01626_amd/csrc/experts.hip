@@ -20,8 +20,8 @@ namespace {
 
 // ------------------------------------------------------------------ the router
 // A token's logits lie over 16 lanes, a row of the cross-lane instructions, so that a maximum over all experts is a few instructions for each
-// of a lane's logits and four for the rest, without LDS.  16384 tokens of 256 experts, fp32, 8 choices: 19.4 in all, 13.0 for the choice, 3.8 for the
-// sums and 5.0 for the rows; reading the logits is 3.4 of them, and the rest of the choice is its 8 rounds of maximum, search and removal over a lane's 16 logits, one behind
+// of a lane's logits and four for the rest, without LDS.  16384 tokens of 256 experts, fp32, 8 choices: 19.4; the profiler, which adds some to
+// each of three kernels, has 13.0 for the choice, 3.8 for the sums and 5.0 for the rows.  Reading the logits is 3.4 of them, and the rest of the choice is its 8 rounds of maximum, search and removal over a lane's 16 logits, one behind
 // the other.  8 tokens of 64 experts: 4.1, a launch and one chain from the load to the rows.
 constexpr int kRowLanes = 16;                   // lanes that share a token
 constexpr int kRouteThreads = 512;
@@ -680,10 +680,12 @@ using Quarter = Shape<2, 4, 4, 2, 4>;           // 128 x 128, eight waves, four 
 // Workgroups take tiles until there are none left; the next tile's first stages are on their way while a tile is finished.
 //
 // A stage of 128 bytes along the sum goes straight to LDS.  In large tiles, 256 x 256 by eight waves, a wave reads 24 KB of it for 64 products of
-// 16 x 16 x 32, and a stage takes 1.45, which is 1480 TFLOP/s: there the matrix cores bound the loop, at the clock that power leaves them.  What a tile
-// costs beside it, 10 of the 57 that a sum over 2048 takes, is the latency of its first stage and 128 KB that go out through L2 (dW of 16384 x 5632 x 2048 of 32 experts: 443,
+// 16 x 16 x 32, and a stage takes 1.47, which is 1460 TFLOP/s (4096 x 4096, one tile a compute unit: a sum over 4096 107, over 2048 60).  The matrix cores are busy for 64 % of such a
+// loop (a sum over 65536: 1797), and its waves wait for 40 % of their cycles: with two places each stage ends in a wait for all loads and a barrier.  What a tile
+// costs beside its stages, 10 of the 57 that a sum over 2048 takes, is the latency of its first stage and 128 KB that go out through L2 (dW of 16384 x 5632 x 2048 of 32 experts: 443,
 // without its stores 334).  Tried and slower for that dW: stores past the caches (745 where it took 576 without), stores before the next tile's first loads (484), tiles of
-// 256 x 128 by four waves, two workgroups a compute unit (484).  Tiles cut to the rows that an expert has left gain nothing.
+// 256 x 128 by four waves, two workgroups a compute unit (484).  Tiles cut to the rows that an expert has left gain nothing:
+// fewer products leave a stage's loads and its wait as they are.
 template <typename T, Does DOES, class S, class OF = S, typename Next>
 __device__ __forceinline__ void work(const ExpertArgs<T>& p, const Groups& groups, unsigned items, unsigned base, int lane, Next next, unsigned from = 0) {
     using Where = Tile<T, DOES, S, OF>;

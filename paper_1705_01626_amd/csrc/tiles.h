@@ -9,8 +9,8 @@ namespace {
 // ------------------------------------------------------------------ products on the matrix cores
 //
 // Every product here is  out[row][col] = sum over t of Q(row, t) P(col, t),  with `col` the output's contiguous
-// index:  forward  P = Wg and Wu, Q = x;  dx  P = Wg then Wu by columns, Q = dg then du;  dW  P = x by columns,
-// Q = dg or du by columns.  P is the matrix instruction's first operand, so a lane holds four neighbouring columns
+// index.  Gated block:  forward  P = Wg and Wu, Q = x;  dx  P = Wg then Wu by columns, Q = dg then du;  dW  P = x by columns,
+// Q = dg or du by columns.  Experts, of one expert at a time:  forward  P = W, Q = x;  dx  P = W by columns, Q = dy;  dW  P = x by columns, Q = dy by columns.  P is the matrix instruction's first operand, so a lane holds four neighbouring columns
 // of one row and stores them together.
 //
 // An operand lies either along the reduction (its rows are contiguous in t) or across it (its rows are the t).
